@@ -17,6 +17,10 @@
  *   madakv_evict          Sec. 3.3 Eq. 6-11 and the eviction itself: the first three calls in one
  *   madakv_score_lse      Sec. 3.3 Eq. 7 with the softmax normalisers of the proxy rows given
  *                         (the prefill attention of Sec. 3.1 Eq. 5 has them)
+ *   madakv_score_prompt   Eq. 7 with every position of the prompt as a proxy token: the attention weight a key has
+ *                         accumulated over the whole prompt
+ *   madakv_decode_attn_weights  a decode step that goes on accumulating it, and the eviction of one row per step by it
+ *   madakv_cache_rows     the rows of an 8-bit or 4-bit reduced cache in the type of the model
  *   madakv_window_attn_score  that prefill attention for the proxy rows (Sec. 3.1 Eq. 5) with Eq. 7, 6, 9 as
  *                         by-products of the same pass
  *
@@ -110,7 +114,16 @@ typedef struct {
   int32_t sink_tokens;     /* >= 0, used by select_mode 1 */
   int32_t cache_fp8;       /* 1 = the reduced cache k_c, v_c holds 8-bit floats (OCP E4M3: round to nearest even,
                               magnitudes above 448 saturate), one byte per element, instead of dtype; needs
-                              dtype = MADAKV_BF16.  Q, K, V, k_new, v_new and out stay in dtype. */
+                              dtype = MADAKV_BF16.  Q, K, V, k_new, v_new and out stay in dtype.
+                              4 = 4-bit floats (needs dtype = MADAKV_BF16): k_c holds capacity_tokens * (head_dim / 2 +
+                              head_dim / 32) bytes, and v_c likewise: first the codes of all rows, head_dim / 2 bytes each
+                              (element 2i of a row is the low half of its byte i), then their scales, head_dim / 32
+                              bytes per row.  An element is an E2M1 float (0, 0.5, 1, 1.5, 2, 3, 4, 6, the high bit the sign)
+                              times 2^(b - 127), b the scale byte of its block of 32 dims: the least that leaves the largest
+                              magnitude of the block at most 7, within 7 .. 252; elements are rounded to nearest even and
+                              saturate at 6; infinities and NaN are taken for the largest finite bf16.  The row numbers
+                              in kv_off, kept_idx and the page table count rows as ever.  madakv_reevict is
+                              MADAKV_ERR_UNIMPLEMENTED for it. */
   int32_t n_modalities;    /* M, 2 .. 4: modality ids in the mask are 0 .. M-1 (the paper has text = 0 and
                               image = 1; more modalities are the extension its Sec. 6 names) */
   int32_t page_rows;       /* 0 = every head's segment of the reduced cache is its kept rows followed by
@@ -210,6 +223,24 @@ int32_t madakv_window_attn_score(madakv_handle* h, int32_t layer0, int32_t n,
                                  float* psi, float* psi_pool, void* stats, int32_t* n_mod,
                                  void* ws, size_t ws_bytes, void* stream);
 
+/* Eq. 7 with every position of the prompt as a proxy token, the scores of heavy-hitter eviction: the attention weight each
+ * key has received from all queries.
+ *   q        [n, B, Hq, L, d]  queries of the whole prompt
+ *   k        [n, B, H, L, d]
+ *   row_lse  [n, B, Hq, L] float or NULL  natural log of sum_i exp(scale * q_r . k_i) over the keys i <= r, which the prefill
+ *                              attention has; without it the call forms the logits twice
+ *   psi      [n, B, H, L]      out: sum over the G * L query rows of the causal softmax weight they pay to key i
+ * mask, psi_pool, stats, n_mod: all NULL (the scores alone), or as in madakv_score, for madakv_allocate and
+ * madakv_select_gather to go on with; they are those of psi * 2^-s, s the least with W * 2^s >= L, so that they have the
+ * range that W proxy tokens give (budgets, counts and rankings do not depend on it).
+ *   ws       madakv_score_prompt_workspace_bytes(h, n) bytes (enough for calls over fewer layers as well)
+ * MADAKV_ERR_UNIMPLEMENTED unless dtype is bf16. */
+int32_t madakv_score_prompt_workspace_bytes(const madakv_handle* h, int32_t n_layers_per_call, size_t* bytes);
+int32_t madakv_score_prompt(madakv_handle* h, int32_t layer0, int32_t n,
+                            const void* q, const void* k, const uint8_t* mask, const float* row_lse,
+                            float* psi, float* psi_pool, void* stats, int32_t* n_mod,
+                            void* ws, size_t ws_bytes, void* stream);
+
 /* Eq. 8, Eq. 10-11 for layers [layer0, layer0 + n) in order.
  *   stats    [n, B, H]        from madakv_score
  *   n_mod    [B, M]
@@ -275,6 +306,43 @@ int32_t madakv_decode_attn(madakv_handle* h, int32_t layer0, int32_t n,
                            void* k_c, void* v_c, const int64_t* kv_off, int32_t* kv_len,
                            void* out, void* ws, size_t ws_bytes, void* stream);
 
+/* One decode step that keeps an account of the attention it pays (the accumulated weight by which heavy-hitter eviction
+ * ranks tokens), and the eviction of one row per step by that account.  Arguments up to out as in madakv_decode_attn; then
+ *   acc_in, acc_out [capacity_tokens] float, indexed like the rows of k_c (the same array, or two): for every row r of the
+ *            heads in the call acc_out[r] = decay * acc_in[r] + the sum over the G query heads of the weight they pay to r
+ *            in this step; of a row that is new in this step the weights alone.  Entries of other rows are left as they are.
+ *            What acc_in holds at first is the caller's choice: zeros, or psi of the kept positions.
+ *   decay    0 .. 1; 1 = the plain sum
+ *   slot_in  [n, B, H] or NULL.  NULL: k_new, v_new are appended as in madakv_decode_attn (or NULL too: attend only).  Else:
+ *            they replace row slot_in of the head's segment (0 .. kv_len - 1); the segment keeps its length.  A head whose
+ *            entry is no row of it stores nothing in this step and attends over the rows it has.
+ *   slot_out [n, B, H] or NULL (may be slot_in): the row with the smallest acc_out among those whose original position is at
+ *            most pos - recent (equal sums: the lower row), -1 if there is none: what the next step's slot_in takes.  A
+ *            sum that is NaN comes last.
+ *   kept_idx, pos  both or neither (slot_out needs them): original positions of the cache's rows, as madakv_select_gather
+ *            left them, and the position of this step's token per batch item, [B] int32 on the device.  kept_idx of the new
+ *            row becomes pos; rows appended by other calls have none until a re-eviction.
+ *   recent   >= 0: the newest tokens that slot_out spares, the one of this step among them
+ *   ws       madakv_decode_attn_weights_workspace_bytes(h, n) bytes
+ * Once rows have been replaced, a segment is no longer in order of position: madakv_reevict gives
+ * MADAKV_ERR_INVALID_ARG for its layer until the next eviction.  Nothing depends on the host from step to step: a
+ * captured replacing step can be replayed any number of times (pos is the caller's to advance on the device). */
+int32_t madakv_decode_attn_weights_workspace_bytes(const madakv_handle* h, int32_t n_layers_per_call, size_t* bytes);
+int32_t madakv_decode_attn_weights(madakv_handle* h, int32_t layer0, int32_t n,
+                                   const void* q, const void* k_new, const void* v_new,
+                                   void* k_c, void* v_c, const int64_t* kv_off, int32_t* kv_len, void* out,
+                                   const float* acc_in, float* acc_out, float decay,
+                                   const int32_t* slot_in, int32_t* slot_out,
+                                   int32_t* kept_idx, const int32_t* pos, int32_t recent,
+                                   void* ws, size_t ws_bytes, void* stream);
+
+/* The rows that the heads of layers [layer0, layer0 + n) hold in an 8-bit or 4-bit reduced cache, as values of dtype:
+ *   k_rows, v_rows [capacity_tokens, d]  out: row i holds what row i of k_c / v_c stands for (every value is exact in
+ *                  bf16); rows of no head are left as they are
+ * For a handle whose cache holds rows of dtype: MADAKV_ERR_UNIMPLEMENTED (k_c and v_c are the rows). */
+int32_t madakv_cache_rows(madakv_handle* h, int32_t layer0, int32_t n, const void* k_c, const void* v_c,
+                          const int64_t* kv_off, const int32_t* kv_len, void* k_rows, void* v_rows, void* stream);
+
 /* Re-eviction during generation (the paper evicts once, after the prefill, Sec. 3.3; its Sec. 6 leaves long
  * generation open).  After some decode steps every head's segment holds its kept rows, the W window rows and
  * the appended rows.  The call brings each head of layers [layer0, layer0 + n) back to the length the prompt
@@ -297,7 +365,7 @@ int32_t madakv_decode_attn(madakv_handle* h, int32_t layer0, int32_t n,
  *   budgets  [n, B, H, M]       out: the new split
  *   ws                          madakv_reevict_workspace_bytes(h, n) bytes
  * The decode-step counters of the layers are reset: max_new_tokens rows can be appended again.
- * An 8-bit cache is scored and moved as it is stored (E4M3 rows).  A paged cache is re-evicted as a whole
+ * An 8-bit cache is scored and moved as it is stored (E4M3 rows); MADAKV_ERR_UNIMPLEMENTED for a 4-bit one.  A paged cache is re-evicted as a whole
  * (layer0 = 0, n = n_layers, else MADAKV_ERR_INVALID_ARG): the survivors end up in the heads' initial pages
  * and every page taken since the eviction goes back to the pools, which all layers share; the work is done
  * on a linear copy of the rows in the workspace (as many rows as the cache holds).

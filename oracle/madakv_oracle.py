@@ -518,6 +518,50 @@ def dequantize_e4m3(codes: np.ndarray) -> np.ndarray:
     return e4m3_decode_table()[np.asarray(codes, dtype=np.uint8)]
 
 
+MX_VALUES = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])       # E2M1 codes 0 .. 7; 8 .. 15 are their negatives
+
+
+def quantize_mx4(x: np.ndarray):
+    """Rows [..., d] of bf16 values -> (bytes [..., d/2] of two codes each, scale bytes [..., d/32]) of the 4-bit cache: a block
+    of 32 shares 2^(byte - 127), the least power (bytes 7 .. 252) that leaves the largest magnitude at most 7; elements go to
+    the nearest code, ties to the even one, magnitudes above 6 to 6.  Infinities and NaN: the largest finite bf16."""
+    x = np.asarray(x, dtype=np.float64)
+    most = 255.0 * 2.0 ** 120
+    sign = np.signbit(x)
+    a = np.where(np.isfinite(x), np.abs(x), most).reshape(*x.shape[:-1], -1, 32)
+    top = a.max(-1)
+    byte = np.full(top.shape, 7, dtype=np.int64)
+    for b in range(8, 253):                              # the least power that is enough
+        byte = np.where(top > 7.0 * np.ldexp(1.0, byte - 127), b, byte)
+    y = a / np.ldexp(1.0, byte - 127)[..., None]
+    dist = np.abs(np.minimum(y, 6.0)[..., None] - MX_VALUES)
+    near = dist.min(-1, keepdims=True)
+    even_first = np.array([0, 2, 4, 6, 1, 3, 5, 7])
+    code = even_first[np.argmax(dist[..., even_first] == near, axis=-1)].reshape(x.shape) + 8 * sign
+    pair = code.reshape(*x.shape[:-1], -1, 2)
+    return (pair[..., 0] + 16 * pair[..., 1]).astype(np.uint8), byte.astype(np.uint8)
+
+
+def dequantize_mx4(codes: np.ndarray, scales: np.ndarray) -> np.ndarray:
+    """The values that (codes, scales) of quantize_mx4 stand for."""
+    code = np.stack([codes & 15, codes >> 4], axis=-1).reshape(*codes.shape[:-1], -1)
+    v = MX_VALUES[code & 7] * np.where(code & 8, -1.0, 1.0)
+    return (v.reshape(*v.shape[:-1], -1, 32) * np.ldexp(1.0, scales.astype(np.int64) - 127)[..., None]).reshape(v.shape)
+
+
+def prompt_scores(q: np.ndarray, k: np.ndarray, scale: float) -> np.ndarray:
+    """Eq. 7 with every position as a proxy token: q[Hq, L, d], k[H, L, d] -> psi[H, L], the softmax weight every key has
+    received from the queries at and after it, summed over the queries and the query heads of its KV head."""
+    Hq, L, _ = q.shape
+    H = k.shape[0]
+    psi = np.zeros((H, L))
+    for j in range(Hq):
+        s = np.where(np.tril(np.ones((L, L), dtype=bool)), scale * (q[j] @ k[j * H // Hq].T), -np.inf)
+        w = np.exp(s - s.max(axis=1, keepdims=True))
+        psi[j * H // Hq] += (w / w.sum(axis=1, keepdims=True)).sum(axis=0)
+    return psi
+
+
 # --------------------------------------------------------------------------- #
 # Eq. 3-5: decode over a (reduced) cache
 # --------------------------------------------------------------------------- #

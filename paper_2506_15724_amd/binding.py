@@ -65,6 +65,11 @@ def lib() -> C.CDLL:
         L.madakv_window_attn_score.argtypes = [vp, i32, i32] + [vp] * 10 + [vp, sz, vp]
         L.madakv_reevict_workspace_bytes.argtypes = [vp, i32, C.POINTER(sz)]
         L.madakv_reevict.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.madakv_decode_attn_weights_workspace_bytes.argtypes = [vp, i32, C.POINTER(sz)]
+        L.madakv_decode_attn_weights.argtypes = [vp, i32, i32] + [vp] * 10 + [C.c_float] + [vp] * 4 + [i32, vp, sz, vp]
+        L.madakv_cache_rows.argtypes = [vp, i32, i32] + [vp] * 7
+        L.madakv_score_prompt_workspace_bytes.argtypes = [vp, i32, C.POINTER(sz)]
+        L.madakv_score_prompt.argtypes = [vp, i32, i32] + [vp] * 8 + [vp, sz, vp]
         for name in EXPORTS:
             getattr(L, name).restype = i32
         _lib = L
@@ -74,6 +79,8 @@ def lib() -> C.CDLL:
 EXPORTS = ["madakv_create", "madakv_destroy", "madakv_last_hip_error", "madakv_workspace_bytes",
            "madakv_compact_capacity_tokens", "madakv_score", "madakv_score_lse", "madakv_allocate", "madakv_select_gather", "madakv_evict",
            "madakv_decode_attn", "madakv_decode_attn_static", "madakv_page_table",
+           "madakv_decode_attn_weights_workspace_bytes", "madakv_decode_attn_weights", "madakv_cache_rows",
+           "madakv_score_prompt_workspace_bytes", "madakv_score_prompt",
            "madakv_reevict_workspace_bytes", "madakv_reevict", "madakv_window_attn_workspace_bytes", "madakv_window_attn_score"]
 
 
@@ -162,6 +169,35 @@ def madakv_decode_attn_static(h, layer0, n, q, k_new, v_new, k_c, v_c, kv_off, k
         h, layer0, n, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_c), _ptr(v_c), _ptr(kv_off), _ptr(kv_len), _ptr(out), _stream()))
 
 
+def madakv_decode_attn_weights_workspace_bytes(h, n_layers_per_call: int) -> int:
+    b = C.c_size_t()
+    _check("madakv_decode_attn_weights_workspace_bytes", lib().madakv_decode_attn_weights_workspace_bytes(h, n_layers_per_call, C.byref(b)))
+    return b.value
+
+
+def madakv_decode_attn_weights(h, layer0, n, q, k_new, v_new, k_c, v_c, kv_off, kv_len, out, acc_in, acc_out, decay, slot_in, slot_out,
+                               kept_idx, pos, recent, ws):
+    _check("madakv_decode_attn_weights", lib().madakv_decode_attn_weights(
+        h, layer0, n, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_c), _ptr(v_c), _ptr(kv_off), _ptr(kv_len), _ptr(out), _ptr(acc_in),
+        _ptr(acc_out), decay, _ptr(slot_in), _ptr(slot_out), _ptr(kept_idx), _ptr(pos), recent, _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+
+
+def madakv_cache_rows(h, layer0, n, k_c, v_c, kv_off, kv_len, k_rows, v_rows):
+    _check("madakv_cache_rows", lib().madakv_cache_rows(h, layer0, n, _ptr(k_c), _ptr(v_c), _ptr(kv_off), _ptr(kv_len), _ptr(k_rows),
+                                                        _ptr(v_rows), _stream()))
+
+
+def madakv_score_prompt_workspace_bytes(h, n_layers_per_call: int) -> int:
+    b = C.c_size_t()
+    _check("madakv_score_prompt_workspace_bytes", lib().madakv_score_prompt_workspace_bytes(h, n_layers_per_call, C.byref(b)))
+    return b.value
+
+
+def madakv_score_prompt(h, layer0, n, q, k, mask, row_lse, psi, psi_pool, stats, n_mod, ws):
+    _check("madakv_score_prompt", lib().madakv_score_prompt(h, layer0, n, _ptr(q), _ptr(k), _ptr(mask), _ptr(row_lse), _ptr(psi), _ptr(psi_pool),
+                                                            _ptr(stats), _ptr(n_mod), _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+
+
 def madakv_window_attn_workspace_bytes(h, n_layers_per_call: int) -> int:
     b = C.c_size_t()
     _check("madakv_window_attn_workspace_bytes", lib().madakv_window_attn_workspace_bytes(h, n_layers_per_call, C.byref(b)))
@@ -230,8 +266,10 @@ class MadaKV:
         self.kv_off = torch.empty(NL, B, H, dtype=torch.int64, device=dev)
         self.kv_len = torch.empty(NL, B, H, dtype=torch.int32, device=dev)
         cdt = torch.uint8 if cache_fp8 else self.tdtype
-        self.k_c = torch.empty(self.capacity, head_dim, dtype=cdt, device=dev)
-        self.v_c = torch.empty(self.capacity, head_dim, dtype=cdt, device=dev)
+        # (4 bits: the codes of all rows, then their scales)
+        shape = (self.capacity * (head_dim // 2 + head_dim // 32),) if cache_fp8 == 4 else (self.capacity, head_dim)
+        self.k_c = torch.empty(shape, dtype=cdt, device=dev)
+        self.v_c = torch.empty(shape, dtype=cdt, device=dev)
 
     def close(self):
         if self.h is not None:
@@ -295,6 +333,43 @@ class MadaKV:
         self._check_out(out, n * self.cfg.batch * self.cfg.n_q_heads * self.cfg.head_dim)
         madakv_decode_attn_static(self.h, l0, n, q, k_new, v_new, self.k_c, self.v_c, self._sl(self.kv_off, l0, n),
                                   self._sl(self.kv_len, l0, n), out)
+
+    def _check_array(self, name, t, numel, dtype):
+        """Arrays that the library indexes by the shape of the call."""
+        if t is not None and (t.dtype != dtype or t.numel() < numel or t.device != self.kv_len.device):
+            raise ValueError(f"{name} must hold {numel} elements of {dtype} on {self.kv_len.device}; got {t.numel()} of {t.dtype} on {t.device}")
+
+    def decode_attn_weights(self, l0, n, q, k_new, v_new, out, acc_in, acc_out, decay=1.0, slot_in=None, slot_out=None, pos=None, recent=0):
+        """kept_idx is the holder's own, kept up where the tokens' positions `pos` are given."""
+        c, heads = self.cfg, n * self._heads
+        self._check_out(out, n * self._out_row)
+        self._check_array("acc_in", acc_in, self.capacity, torch.float32)
+        self._check_array("acc_out", acc_out, self.capacity, torch.float32)
+        self._check_array("slot_in", slot_in, heads, torch.int32)
+        self._check_array("slot_out", slot_out, heads, torch.int32)
+        self._check_array("pos", pos, c.batch, torch.int32)
+        if getattr(self, "weights_ws", None) is None:
+            need = max(madakv_decode_attn_weights_workspace_bytes(self.h, m) for m in (1, self.n_call))
+            self.weights_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        madakv_decode_attn_weights(self.h, l0, n, q, k_new, v_new, self.k_c, self.v_c, self._sl(self.kv_off, l0, n), self._sl(self.kv_len, l0, n),
+                                   out, acc_in, acc_out, decay, slot_in, slot_out, None if pos is None else self.kept_idx, pos, recent, self.weights_ws)
+
+    def cache_rows(self, l0, n, k_rows, v_rows):
+        for name, t in (("k_rows", k_rows), ("v_rows", v_rows)):
+            self._check_array(name, t, self.capacity * self.cfg.head_dim, self.tdtype)
+        madakv_cache_rows(self.h, l0, n, self.k_c, self.v_c, self._sl(self.kv_off, l0, n), self._sl(self.kv_len, l0, n), k_rows, v_rows)
+
+    def score_prompt(self, l0, n, q, k, mask=None, row_lse=None):
+        """q [n, B, Hq, L, d].  Without a mask psi alone, with one the pooled scores, statistics and counts as well (as `score`)."""
+        c = self.cfg
+        self._check_array("q", q, n * c.batch * c.n_q_heads * c.ctx_len * c.head_dim, self.tdtype)
+        self._check_array("k", k, n * self._heads * c.ctx_len * c.head_dim, self.tdtype)
+        self._check_array("mask", mask, c.batch * c.ctx_len, torch.uint8)
+        self._check_array("row_lse", row_lse, n * c.batch * c.n_q_heads * c.ctx_len, torch.float32)
+        if getattr(self, "prompt_ws", None) is None:
+            self.prompt_ws = torch.empty(max(16, madakv_score_prompt_workspace_bytes(self.h, self.n_call)), dtype=torch.uint8, device=self.device)
+        rest = (None,) * 3 if mask is None else (self._sl(self.psi_pool, l0, n), self._sl(self.stats, l0, n), self.n_mod)
+        madakv_score_prompt(self.h, l0, n, q, k, mask, row_lse, self._sl(self.psi, l0, n), *rest, self.prompt_ws)
 
     def window_attn_score(self, l0, n, q_win, k, v, mask, out, row_lse=None):
         self._check_out(out, n * self.cfg.batch * self.cfg.n_q_heads * self.cfg.window * self.cfg.head_dim)

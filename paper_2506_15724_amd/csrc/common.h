@@ -45,6 +45,14 @@ struct Meet {
   int32_t* len1;            // [n_layers * B * H] 1 + the rows the eviction left each head, 0 before the first one
 };
 
+// Element types of the reduced cache (config.cache_fp8): the type of K and V, E4M3 bytes, or 4-bit floats.  In the 4-bit cache k_c
+// (and v_c) holds the codes of all rows, d / 2 bytes each, and behind those of capacity_tokens rows the scales, d / 32 bytes per row.
+constexpr int CACHE_E4M3 = 1, CACHE_E2M1 = 4;
+constexpr int MX_BLOCK = 32;             // dims that share a scale
+inline int cache_row_bytes(const madakv_config& c) {       // of a row's elements (without scales)
+  return c.cache_fp8 == CACHE_E2M1 ? c.head_dim / 2 : c.head_dim * (c.cache_fp8 == CACHE_E4M3 ? 1 : c.dtype == MADAKV_BF16 ? 2 : 4);
+}
+
 struct ScorePlan { int nsplit; int chunk; int mpad; int group_heads; };
 struct DecodePlan { int chunk_rows; int max_chunks; int grid_chunks; };   // rows per piece of a head, most pieces of a head, pieces in the grid
 
@@ -109,9 +117,28 @@ hipError_t launch_gather(const Dims& dm, const madakv_config& c, int li0, int nl
                          const int32_t* kept_idx, const int64_t* kv_off, const int32_t* kv_len,
                          void* k_c, void* v_c, const void* ws, long long region_tokens,
                          int blocks_per_batch, int grid_blocks, hipStream_t st, bool leave_room = false);
+// Eq. 7 with every position of the prompt as a proxy token (prompt.hip)
+bool prompt_supported(const madakv_config& c);
+size_t prompt_ws_bytes(const Dims& dm);
+hipError_t launch_prompt(const Dims& dm, const madakv_config& c, const void* q, const void* k, const float* row_lse, float* psi,
+                         void* ws, float factor, float** scaled, hipStream_t st);
+hipError_t launch_cache_rows(const Dims& dm, const madakv_config& c, const void* k_c, const void* v_c, const int64_t* kv_off, const int32_t* kv_len,
+                             void* k_rows, void* v_rows, long long capacity_tokens, int longest_rows, const Paging& pg, int layer0, hipStream_t st);
+// A decode step that adds up the weights it pays (weights.hip).  The first seven are the caller's, the others point into the workspace.
+struct WeightArgs {
+  const float* acc_in; float* acc_out; const int32_t* slot_in; int32_t* slot_out; int32_t* kept_idx; const int32_t* pos;
+  float decay; int recent;
+  float* logits; float* head_ml; int32_t* fresh; unsigned long long* best;
+  int logit_rows;
+};
+size_t weights_ws_bytes(const Dims& dm, const madakv_config& c);
+void weights_ws_layout(const Dims& dm, const madakv_config& c, void* ws, WeightArgs& w);
+hipError_t launch_row_weights(const Dims& dm, const madakv_config& c, const WeightArgs& w, const int64_t* kv_off, const int32_t* kv_len,
+                              const Meet& meet, int longest_rows, const Paging& pg, int layer0, hipStream_t st);
 hipError_t launch_decode(const Dims& dm, const madakv_config& c, const void* q, const void* k_new,
                          const void* v_new, void* k_c, void* v_c, const int64_t* kv_off, int32_t* kv_len,
-                         void* out, const Meet& meet, void* ws, long long capacity_tokens, int longest_rows, const Paging& pg, int layer0, hipStream_t st);
+                         void* out, const Meet& meet, void* ws, long long capacity_tokens, int longest_rows, const Paging& pg, int layer0, hipStream_t st,
+                         const WeightArgs* w = nullptr);       // w: the attention's logits stay behind for launch_row_weights
 
 constexpr int GATHER_ROWS = 64;   // rows of the reduced cache one gather workgroup fills
 
@@ -144,6 +171,60 @@ __device__ __forceinline__ uint32_t f32_to_e4m3(float f) {
     code = ((b >> 20) & 0x7ffu) - (120u << 3);                                // exponent re-biased from 127 to 7
   }
   return sign | min(code, 0x7eu);
+}
+
+// The 4-bit cache: E2M1 elements (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives, the sign in the high bit), MX_BLOCK of them under
+// a power of two 2^(byte - 127) (the block format of the OCP microscaling specification; element 2i is the low half of byte i).  The
+// scale is the least one that leaves the block's largest magnitude at most 7, which rounds to 6: one step more than the
+// specification's own choice, under which everything between 6 and 8 saturates.  Its byte is kept within 7 .. 252, so that
+// neither scale nor any product with a code leaves the normal bf16 range; what is smaller than that rounds to zero.
+// Infinities and NaN count as the largest finite bf16.  From the largest magnitude of the block, as bf16 bits:
+__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t largest) {
+  const int e = (int)(largest >> 7) - 2 + ((largest & 0x7fu) > 0x60u ? 1 : 0);
+  return (uint32_t)min(max(e, 7), 252);
+}
+__device__ __forceinline__ float mx_scale_value(uint32_t byte) { return __uint_as_float(byte << 23); }
+typedef __attribute__((ext_vector_type(2))) unsigned short mx_u16x2_t;
+typedef __attribute__((ext_vector_type(2))) __bf16 mx_bf16x2_t;
+// 8 bf16 (a lane's 16 bytes of a row) -> 8 codes and the scale of the block, which the four lanes of a quad share.  All four
+// lanes of the quad must be active.  The conversion rounds to nearest even and saturates (checked on every bf16).
+__device__ __forceinline__ uint32_t mx_encode8(const uint32_t (&x)[4], uint32_t& scale_byte) {
+  mx_u16x2_t m = {0, 0};
+  uint32_t y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const mx_u16x2_t a = __builtin_elementwise_min(__builtin_bit_cast(mx_u16x2_t, x[i] & 0x7fff7fffu), mx_u16x2_t{0x7f7f, 0x7f7f});
+    m = __builtin_elementwise_max(m, a);
+    y[i] = __builtin_bit_cast(uint32_t, a) | (x[i] & 0x80008000u);
+  }
+  uint32_t top = max((uint32_t)m[0], (uint32_t)m[1]);
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, true));    // quad_perm [1,0,3,2]
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xF, 0xF, true));    // quad_perm [2,3,0,1]
+  scale_byte = mx_scale_byte(top);
+  const float s = mx_scale_value(scale_byte);
+  uint32_t code = 0;
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(mx_bf16x2_t, y[0]), s, 0);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(mx_bf16x2_t, y[1]), s, 1);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(mx_bf16x2_t, y[2]), s, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(mx_bf16x2_t, y[3]), s, 3);
+}
+// the scale bytes of a row's blocks as one word, in every lane of the row (LPR = d / 8 lanes, `piece` the lane's place among them)
+template <int LPR>
+__device__ __forceinline__ uint32_t mx_row_scales(uint32_t byte, int piece) {
+  uint32_t w = byte << (8 * (piece >> 2));
+  if (LPR == 16) {
+    w |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0x124, 0xF, 0xF, true);               // row_ror 4
+    w |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0x128, 0xF, 0xF, true);               // row_ror 8
+  } else {
+    w |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0x141, 0xF, 0xF, true);               // row_half_mirror: the other quad of eight lanes
+  }
+  return w;
+}
+// 8 codes -> 8 bf16 (exact)
+__device__ __forceinline__ uint4 mx_decode8(uint32_t code, uint32_t scale_byte) {
+  const float s = mx_scale_value(scale_byte);
+  return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 1)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 3)));
 }
 
 // Sum over the 16 lanes of a DPP row; every lane of the row ends with the total.

@@ -21,10 +21,11 @@ struct GatherArgs {
   void* k_c; void* v_c; const long long* call_range; const int32_t* blk2head;
   int n, B, H, L, blocks_per_batch;
   int li0, li1;          // layers [li0, li1) of the call are gathered by this launch
+  long long capacity;    // rows of the reduced cache: the scales of a 4-bit cache sit behind the codes of so many
   long long region_tokens;
 };
 
-template <int LPR, bool FP8>   // lanes per source row (row bytes / 16); FP8: bf16 rows are stored as E4M3
+template <int LPR, int KIND>   // lanes per source row (row bytes / 16); KIND: 0 = rows are stored as they are, CACHE_E4M3 / CACHE_E2M1 = bf16 rows are encoded
 __global__ __launch_bounds__(256) void gather_kernel(GatherArgs a) {
   constexpr int RPI = 64 / LPR;                 // rows per wave instruction
   constexpr int ROWS_PER_WAVE = GATHER_ROWS / 4;
@@ -106,7 +107,20 @@ __global__ __launch_bounds__(256) void gather_kernel(GatherArgs a) {
 #pragma unroll
   for (int it = 0; it < ITERS; ++it) {
     if (src[it] >= 0) {
-      if (FP8) {
+      if (KIND == CACHE_E2M1) {
+        // (a row's lanes are here together: mx_encode8 and mx_row_scales read across them)
+        const uint32_t kx[4] = {kv[it][0], kv[it][1], kv[it][2], kv[it][3]}, vx[4] = {vv[it][0], vv[it][1], vv[it][2], vv[it][3]};
+        uint32_t ks, vs;
+        reinterpret_cast<uint32_t*>(a.k_c)[dst[it] * LPR + piece] = mx_encode8(kx, ks);
+        reinterpret_cast<uint32_t*>(a.v_c)[dst[it] * LPR + piece] = mx_encode8(vx, vs);
+        ks = mx_row_scales<LPR>(ks, piece); vs = mx_row_scales<LPR>(vs, piece);
+        if (piece < 2) {                                             // lane 0 the scales of K, lane 1 those of V
+          unsigned char* to = reinterpret_cast<unsigned char*>(piece ? a.v_c : a.k_c) + a.capacity * (LPR * 4);
+          const uint32_t w = piece ? vs : ks;
+          if (LPR == 16) reinterpret_cast<uint32_t*>(to)[dst[it]] = w;
+          else reinterpret_cast<uint16_t*>(to)[dst[it]] = (uint16_t)w;
+        }
+      } else if (KIND == CACHE_E4M3) {
         // 8 bf16 -> 8 bytes per lane; a row of the reduced cache is LPR * 8 bytes
         typedef __attribute__((ext_vector_type(2))) unsigned int u32x2_t;
         u32x2_t ko, vo;
@@ -142,6 +156,7 @@ hipError_t launch_gather(const Dims& dm, const madakv_config& c, int li0, int nl
   a.n = dm.n; a.B = dm.B; a.H = dm.H; a.L = dm.L; a.blocks_per_batch = blocks_per_batch;
   a.region_tokens = region_tokens;
   a.li0 = li0; a.li1 = li0 + nli;
+  a.capacity = region_tokens * dm.B;
   const int row_bytes = dm.d * (c.dtype == MADAKV_BF16 ? 2 : 4);
   const int lpr = row_bytes / 16;
   dim3 grid(std::min(grid_blocks, blocks_per_batch), dm.B);
@@ -153,14 +168,100 @@ hipError_t launch_gather(const Dims& dm, const madakv_config& c, int li0, int nl
   // 1274, 1292.  Beside such gathers a selection took 122 us and the statistics 125 on average (alone 58 and 60), when they
   // were 73 and 58 KB large and the claim 36 KB 245 and 166; the gather 444 instead of 425.
   const size_t lds = leave_room ? GATHER_ROOM_LDS : 0;
-  if (c.cache_fp8) {
-    if (lpr == 8) hipLaunchKernelGGL((gather_kernel<8, true>), grid, dim3(256), lds, st, a);
-    else if (lpr == 16) hipLaunchKernelGGL((gather_kernel<16, true>), grid, dim3(256), lds, st, a);
+  if (c.cache_fp8 == CACHE_E2M1) {
+    if (lpr == 8) hipLaunchKernelGGL((gather_kernel<8, CACHE_E2M1>), grid, dim3(256), lds, st, a);
+    else if (lpr == 16) hipLaunchKernelGGL((gather_kernel<16, CACHE_E2M1>), grid, dim3(256), lds, st, a);
     else return hipErrorInvalidValue;
-  } else if (lpr == 8) hipLaunchKernelGGL((gather_kernel<8, false>), grid, dim3(256), lds, st, a);
-  else if (lpr == 16) hipLaunchKernelGGL((gather_kernel<16, false>), grid, dim3(256), lds, st, a);
-  else if (lpr == 32) hipLaunchKernelGGL((gather_kernel<32, false>), grid, dim3(256), lds, st, a);
+  } else if (c.cache_fp8) {
+    if (lpr == 8) hipLaunchKernelGGL((gather_kernel<8, CACHE_E4M3>), grid, dim3(256), lds, st, a);
+    else if (lpr == 16) hipLaunchKernelGGL((gather_kernel<16, CACHE_E4M3>), grid, dim3(256), lds, st, a);
+    else return hipErrorInvalidValue;
+  } else if (lpr == 8) hipLaunchKernelGGL((gather_kernel<8, 0>), grid, dim3(256), lds, st, a);
+  else if (lpr == 16) hipLaunchKernelGGL((gather_kernel<16, 0>), grid, dim3(256), lds, st, a);
+  else if (lpr == 32) hipLaunchKernelGGL((gather_kernel<32, 0>), grid, dim3(256), lds, st, a);
   else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+// Rows of an encoded reduced cache back in the model's type, at the same places: k_rows[i, :] = k_c[i, :] for the rows the heads
+// hold; the rest of k_rows and v_rows is left as it is.  A lane makes 16 bytes of a row.  Bound by HBM: a row is written with
+// 4 d bytes and read with 2 d (8 bits) or 1.06 d (4 bits).
+struct RowsArgs {
+  const void* k_c; const void* v_c; const int64_t* kv_off; const int32_t* kv_len; u32x4_t* k_rows; u32x4_t* v_rows;
+  long long capacity;
+  const int32_t* page_tbl; int entries, shift;      // of the call's first head; null without paging
+};
+constexpr int ROWS_PER_BLOCK = 64;
+
+template <int LPR, int KIND>   // lanes per row of the output
+__global__ __launch_bounds__(256) void cache_rows_kernel(RowsArgs a) {
+  constexpr int RPI = 256 / LPR, ITERS = ROWS_PER_BLOCK / RPI;
+  const int head = blockIdx.y, len = a.kv_len[head];
+  const int r0 = blockIdx.x * ROWS_PER_BLOCK;
+  if (r0 >= len) return;
+  const long long off = a.kv_off[head];
+  const int32_t* tbl = a.page_tbl ? a.page_tbl + (long long)head * a.entries : nullptr;
+  const int init_rows = tbl ? tbl[0] << a.shift : 0x7fffffff;
+  const int sub = threadIdx.x / LPR, piece = threadIdx.x % LPR;
+  long long at[ITERS];
+  u32x4_t kv[ITERS], vv[ITERS];
+#pragma unroll
+  for (int it = 0; it < ITERS; ++it) {
+    const int r = min(r0 + it * RPI + sub, len - 1);       // (past the end: the last row once more)
+    at[it] = off + r;
+    if (r >= init_rows) { const int q = r - init_rows; at[it] = ((long long)tbl[1 + (q >> a.shift)] << a.shift) + (q & ((1 << a.shift) - 1)); }
+  }
+#pragma unroll
+  for (int it = 0; it < ITERS; ++it) {
+    if (KIND == CACHE_E2M1) {
+      const long long block = a.capacity * (LPR * 4) + at[it] * (LPR / 4) + piece / 4;          // of the scales
+      const uint4 x = mx_decode8(__builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(a.k_c) + at[it] * LPR + piece), reinterpret_cast<const uint8_t*>(a.k_c)[block]);
+      const uint4 y = mx_decode8(__builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(a.v_c) + at[it] * LPR + piece), reinterpret_cast<const uint8_t*>(a.v_c)[block]);
+      kv[it] = __builtin_bit_cast(u32x4_t, x); vv[it] = __builtin_bit_cast(u32x4_t, y);
+    } else {
+      typedef __attribute__((ext_vector_type(2))) unsigned int u32x2_t;
+      typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+      const u32x2_t k8 = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(a.k_c) + at[it] * LPR + piece);
+      const u32x2_t v8 = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(a.v_c) + at[it] * LPR + piece);
+      // (every E4M3 value is a bf16: the upper half of the float is all there is of it)
+      const auto pair = [](uint32_t w, bool high) {
+        const f32x2_t f = high ? __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
+        return (__float_as_uint(f[0]) >> 16) | (__float_as_uint(f[1]) & 0xffff0000u);
+      };
+      kv[it] = u32x4_t{pair(k8[0], false), pair(k8[0], true), pair(k8[1], false), pair(k8[1], true)};
+      vv[it] = u32x4_t{pair(v8[0], false), pair(v8[0], true), pair(v8[1], false), pair(v8[1], true)};
+    }
+  }
+#pragma unroll
+  for (int it = 0; it < ITERS; ++it) {
+    if (r0 + it * RPI + sub < len) {
+      __builtin_nontemporal_store(kv[it], a.k_rows + at[it] * LPR + piece);
+      __builtin_nontemporal_store(vv[it], a.v_rows + at[it] * LPR + piece);
+    }
+  }
+}
+
+hipError_t launch_cache_rows(const Dims& dm, const madakv_config& c, const void* k_c, const void* v_c, const int64_t* kv_off, const int32_t* kv_len,
+                             void* k_rows, void* v_rows, long long capacity_tokens, int longest_rows, const Paging& pg, int layer0, hipStream_t st) {
+  RowsArgs a;
+  a.k_c = k_c; a.v_c = v_c; a.kv_off = kv_off; a.kv_len = kv_len; a.capacity = capacity_tokens;
+  a.k_rows = static_cast<u32x4_t*>(k_rows); a.v_rows = static_cast<u32x4_t*>(v_rows);
+  a.entries = pg.entries; a.shift = 0;
+  while (pg.page_rows && (1 << a.shift) < pg.page_rows) ++a.shift;
+  a.page_tbl = pg.page_rows ? pg.table + (long long)layer0 * dm.B * dm.H * pg.entries : nullptr;
+  // heads in the second dimension of the grid, which holds 65535 of them
+  for (int h0 = 0; h0 < dm.heads; h0 += 32768) {
+    RowsArgs b = a;
+    b.kv_off += h0; b.kv_len += h0;
+    if (b.page_tbl) b.page_tbl += (long long)h0 * a.entries;
+    const dim3 grid((unsigned)((std::max(longest_rows, 1) + ROWS_PER_BLOCK - 1) / ROWS_PER_BLOCK), std::min(32768, dm.heads - h0));
+    const bool four = c.cache_fp8 == CACHE_E2M1;
+    if (dm.d == 128 && four) hipLaunchKernelGGL((cache_rows_kernel<16, CACHE_E2M1>), grid, dim3(256), 0, st, b);
+    else if (dm.d == 64 && four) hipLaunchKernelGGL((cache_rows_kernel<8, CACHE_E2M1>), grid, dim3(256), 0, st, b);
+    else if (dm.d == 128) hipLaunchKernelGGL((cache_rows_kernel<16, CACHE_E4M3>), grid, dim3(256), 0, st, b);
+    else if (dm.d == 64) hipLaunchKernelGGL((cache_rows_kernel<8, CACHE_E4M3>), grid, dim3(256), 0, st, b);
+    else return hipErrorInvalidValue;
+  }
   return hipGetLastError();
 }
 

@@ -21,6 +21,7 @@ struct madakv_handle {
   int32_t* d_page_tbl;             // paged cache: [n_layers * B * H][entries] page table (null otherwise)
   void* d_split; size_t split_bytes;   // long contexts: buffer of the chunk-parallel statistics / selection (null otherwise)
   std::vector<int32_t> appended;   // decode rows appended since the last (re-)eviction, per layer
+  std::vector<uint8_t> replaced;   // per layer: rows have taken the places of others since the last eviction, so that they are not in order of position
   std::vector<int32_t> gen_base;   // tokens generated before that, per layer (their original positions are ctx_len + 0, 1, ...)
   // Longest head of each layer after eviction: stored by the layout kernel in pinned host memory (d_maxlen is its
   // device address); decode sizes its grid from it once it is known to have landed
@@ -118,7 +119,7 @@ int32_t validate(const madakv_config& c) {
   if (M > 256) return MADAKV_ERR_BAD_SHAPE;
   if (c.dtype == MADAKV_FP32 && (long long)M * c.head_dim > 12288) return MADAKV_ERR_BAD_SHAPE;   // Q tile of the FMA path must fit LDS
   if (c.n_modalities < 2 || c.n_modalities > 4) return MADAKV_ERR_BAD_SHAPE;
-  if ((c.cache_fp8 | 1) != 1) return MADAKV_ERR_INVALID_ARG;
+  if (c.cache_fp8 != 0 && c.cache_fp8 != CACHE_E4M3 && c.cache_fp8 != CACHE_E2M1) return MADAKV_ERR_INVALID_ARG;
   if (c.cache_fp8 && c.dtype != MADAKV_BF16) return MADAKV_ERR_UNSUPPORTED_DTYPE;
   if (c.pool_k < 1 || c.pool_k > 63 || (c.pool_k & 1) == 0) return MADAKV_ERR_BAD_SHAPE;
   if (c.budget < 1 || (c.budget < c.ctx_len && c.budget <= c.window)) return MADAKV_ERR_BAD_BUDGET;
@@ -270,10 +271,11 @@ hipError_t create_memory(madakv_handle* h) {
 }
 int32_t* len1_of(madakv_handle* h, int layer) { return h->meet.len1 + (size_t)layer * h->cfg.batch * h->cfg.n_kv_heads; }
 
+// w: the call adds up the weights it pays (the caller's pointers in it have been checked), ws is the workspace of that call
 int32_t decode_impl(madakv_handle* h, int32_t layer0, int32_t n,
                     const void* q, const void* k_new, const void* v_new,
                     void* k_c, void* v_c, const int64_t* kv_off, int32_t* kv_len,
-                    void* out, void* ws, size_t ws_bytes, void* stream) {
+                    void* out, void* ws, size_t ws_bytes, void* stream, WeightArgs* w = nullptr) {
   int32_t r = check_range(h, layer0, n);
   if (r != MADAKV_OK) return r;
   if (bad_ptr(q) || bad_ptr(k_c) || bad_ptr(v_c) || bad_ptr(kv_off, 8) || bad_ptr(kv_len, 4) || bad_ptr(out) || (ws_bytes != NO_WORKSPACE && bad_ptr(ws)))
@@ -286,20 +288,24 @@ int32_t decode_impl(madakv_handle* h, int32_t layer0, int32_t n,
   const int longest = longest_rows(h, layer0, n, replayed_later(reinterpret_cast<hipStream_t>(stream)));
   // a caller's workspace is sized for the worst case; the handle's scratch must hold what this launch uses
   if (ws_bytes != NO_WORKSPACE) {
-    if (ws_bytes < decode_ws_bytes(dm, h->cfg)) return MADAKV_ERR_WORKSPACE_TOO_SMALL;
+    if (ws_bytes < (w ? weights_ws_bytes(dm, h->cfg) : decode_ws_bytes(dm, h->cfg))) return MADAKV_ERR_WORKSPACE_TOO_SMALL;
   } else {
     if (decode_ws_bytes_for(dm, h->cfg, longest) > MADAKV_STATIC_SCRATCH_BYTES || decode_part_bytes(dm, h->cfg, longest) > h->scratch_bytes)
       return MADAKV_ERR_WORKSPACE_TOO_SMALL;
     ws = h->scratch;
   }
-  if (k_new) {
+  const bool appends = k_new && !(w && w->slot_in);
+  if (appends) {
     for (int l = layer0; l < layer0 + n; ++l)
       if (h->appended[l] >= h->cfg.max_new_tokens) return MADAKV_ERR_INVALID_ARG;
   }
+  if (w) weights_ws_layout(dm, h->cfg, ws, *w);
   hipError_t e = launch_decode(dm, h->cfg, q, k_new, v_new, k_c, v_c, kv_off, kv_len, out, h->meet, ws,
                                region_tokens(h->cfg) * h->cfg.batch, longest, make_paging(h), layer0,
-                               reinterpret_cast<hipStream_t>(stream));
-  if (e == hipSuccess && k_new) for (int l = layer0; l < layer0 + n; ++l) h->appended[l] += 1;
+                               reinterpret_cast<hipStream_t>(stream), w);
+  if (e == hipSuccess && appends) for (int l = layer0; l < layer0 + n; ++l) h->appended[l] += 1;
+  if (e == hipSuccess && k_new && !appends) for (int l = layer0; l < layer0 + n; ++l) h->replaced[l] = 1;
+  if (e == hipSuccess && w) e = launch_row_weights(dm, h->cfg, *w, kv_off, kv_len, h->meet, longest, make_paging(h), layer0, reinterpret_cast<hipStream_t>(stream));
   return hip_fail(h, e);
 }
 
@@ -322,6 +328,7 @@ int32_t madakv_create(const madakv_config* cfg, madakv_handle** out) {
   for (int g = 0; g < MAX_GROUPS; ++g) { h->ev_grp[g] = nullptr; h->ev_sel[g] = nullptr; }
   h->appended.assign(cfg->n_layers, 0);
   h->gen_base.assign(cfg->n_layers, 0);
+  h->replaced.assign(cfg->n_layers, 0);
   h->xchg = nullptr; h->xchg_words = 0; h->xchg_left = false;
   h->meet = Meet{}; h->scratch = nullptr; h->scratch_bytes = 0; h->d_page_tbl = nullptr;
   h->d_split = nullptr; h->split_bytes = 0;
@@ -486,6 +493,43 @@ int32_t madakv_window_attn_score(madakv_handle* h, int32_t layer0, int32_t n,
   return score_impl(h, layer0, n, q_win, k, mask, nullptr, psi, psi_pool, stats, n_mod, ws, ws_bytes, stream, v, out, row_lse);
 }
 
+// The plan of a launch follows the heads in it: what calls over fewer layers need is not always less.
+static size_t prompt_ws_for(const madakv_config& c, int n) {
+  size_t need = 0;
+  for (int m = 1; m <= n; ++m) need = std::max(need, prompt_ws_bytes(make_dims(c, m)));
+  return need;
+}
+
+int32_t madakv_score_prompt_workspace_bytes(const madakv_handle* h, int32_t n_layers_per_call, size_t* bytes) {
+  if (!h || !bytes || n_layers_per_call < 1 || n_layers_per_call > h->cfg.n_layers) return MADAKV_ERR_INVALID_ARG;
+  *bytes = prompt_ws_for(h->cfg, n_layers_per_call);
+  return MADAKV_OK;
+}
+
+int32_t madakv_score_prompt(madakv_handle* h, int32_t layer0, int32_t n,
+                            const void* q, const void* k, const uint8_t* mask, const float* row_lse,
+                            float* psi, float* psi_pool, void* stats, int32_t* n_mod,
+                            void* ws, size_t ws_bytes, void* stream) {
+  int32_t r = check_range(h, layer0, n);
+  if (r != MADAKV_OK) return r;
+  if (bad_ptr(q) || bad_ptr(k) || bad_ptr(psi, 4) || bad_ptr(ws) || (reinterpret_cast<uintptr_t>(row_lse) & 3u)) return MADAKV_ERR_INVALID_ARG;
+  const bool all = mask && psi_pool && stats && n_mod;
+  if (!all && (mask || psi_pool || stats || n_mod)) return MADAKV_ERR_INVALID_ARG;
+  if (all && (bad_ptr(psi_pool, 4) || bad_ptr(stats, 4) || bad_ptr(n_mod, 4))) return MADAKV_ERR_INVALID_ARG;
+  const madakv_config& c = h->cfg;
+  if (!prompt_supported(c)) return MADAKV_ERR_UNIMPLEMENTED;
+  const Dims dm = make_dims(c, n);
+  if (ws_bytes < prompt_ws_bytes(dm)) return MADAKV_ERR_WORKSPACE_TOO_SMALL;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  // The statistics count in fixed point up to G * W per key: they get the scores times a power of two that takes L queries
+  // to at most W.
+  float factor = 1.f, *scaled = nullptr;
+  for (long long w = c.window; w < c.ctx_len; w *= 2) factor *= 0.5f;
+  hipError_t e = launch_prompt(dm, c, q, k, row_lse, psi, ws, factor, all ? &scaled : nullptr, st);
+  if (e == hipSuccess && all) e = launch_stats(dm, c, scaled, mask, psi_pool, stats, n_mod, Exchange{h->xchg, 0}, st, h->d_split, h->split_bytes, false);
+  return hip_fail(h, e);
+}
+
 int32_t madakv_allocate(madakv_handle* h, int32_t layer0, int32_t n,
                         const void* stats, const int32_t* n_mod,
                         int32_t* budgets, void* stream) {
@@ -548,7 +592,7 @@ int32_t madakv_select_gather(madakv_handle* h, int32_t layer0, int32_t n,
     if (e == hipSuccess) e = launch_gather(dg, c, 0, ng, kg, vg, kept_idx, kv_off + heads0, kv_len + heads0, k_c, v_c, ws_g, region, bpb, bpb, st, overlap);
   }
   if (overlap && e != hipSuccess) e = join_side(h, st, e);   // an enqueue failed: whatever did reach the side stream is still joined
-  for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] = 0; h->gen_base[l] = 0; }
+  for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] = 0; h->gen_base[l] = 0; h->replaced[l] = 0; }
   e = publish_maxlen(h, layer0, n, st, e);
   return hip_fail(h, e);
 }
@@ -627,7 +671,7 @@ int32_t madakv_evict(madakv_handle* h, int32_t layer0, int32_t n,
   }
   if (e == hipSuccess) gather_group(ngroups - 1);
   if (overlap && e != hipSuccess) e = join_side(h, st, e);   // an enqueue failed: whatever did reach the side stream is still joined
-  for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] = 0; h->gen_base[l] = 0; }
+  for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] = 0; h->gen_base[l] = 0; h->replaced[l] = 0; }
   e = publish_maxlen(h, layer0, n, st, e);
   return hip_fail(h, e);
 }
@@ -647,6 +691,43 @@ int32_t madakv_decode_attn_static(madakv_handle* h, int32_t layer0, int32_t n,
   return decode_impl(h, layer0, n, q, k_new, v_new, k_c, v_c, kv_off, kv_len, out, nullptr, NO_WORKSPACE, stream);
 }
 
+int32_t madakv_decode_attn_weights_workspace_bytes(const madakv_handle* h, int32_t n_layers_per_call, size_t* bytes) {
+  if (!h || !bytes || n_layers_per_call < 1 || n_layers_per_call > h->cfg.n_layers) return MADAKV_ERR_INVALID_ARG;
+  *bytes = weights_ws_bytes(make_dims(h->cfg, n_layers_per_call), h->cfg);
+  return MADAKV_OK;
+}
+
+int32_t madakv_decode_attn_weights(madakv_handle* h, int32_t layer0, int32_t n,
+                                   const void* q, const void* k_new, const void* v_new,
+                                   void* k_c, void* v_c, const int64_t* kv_off, int32_t* kv_len, void* out,
+                                   const float* acc_in, float* acc_out, float decay,
+                                   const int32_t* slot_in, int32_t* slot_out,
+                                   int32_t* kept_idx, const int32_t* pos, int32_t recent,
+                                   void* ws, size_t ws_bytes, void* stream) {
+  auto optional = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; };
+  if (bad_ptr(acc_in, 4) || bad_ptr(acc_out, 4) || !optional(slot_in) || !optional(slot_out) || !optional(kept_idx) || !optional(pos)) return MADAKV_ERR_INVALID_ARG;
+  if (!(decay >= 0.f) || decay > 1.f || recent < 0) return MADAKV_ERR_INVALID_ARG;
+  if (slot_in && !k_new) return MADAKV_ERR_INVALID_ARG;                                  // nothing to put there
+  if ((kept_idx == nullptr) != (pos == nullptr) || (slot_out && !kept_idx)) return MADAKV_ERR_INVALID_ARG;
+  WeightArgs w = {};
+  w.acc_in = acc_in; w.acc_out = acc_out; w.decay = decay; w.slot_in = slot_in; w.slot_out = slot_out;
+  w.kept_idx = kept_idx; w.pos = pos; w.recent = recent;
+  if (ws_bytes == NO_WORKSPACE) return MADAKV_ERR_INVALID_ARG;
+  return decode_impl(h, layer0, n, q, k_new, v_new, k_c, v_c, kv_off, kv_len, out, ws, ws_bytes, stream, &w);
+}
+
+int32_t madakv_cache_rows(madakv_handle* h, int32_t layer0, int32_t n, const void* k_c, const void* v_c,
+                          const int64_t* kv_off, const int32_t* kv_len, void* k_rows, void* v_rows, void* stream) {
+  int32_t r = check_range(h, layer0, n);
+  if (r != MADAKV_OK) return r;
+  if (bad_ptr(k_c) || bad_ptr(v_c) || bad_ptr(kv_off, 8) || bad_ptr(kv_len, 4) || bad_ptr(k_rows) || bad_ptr(v_rows)) return MADAKV_ERR_INVALID_ARG;
+  const madakv_config& c = h->cfg;
+  if (!c.cache_fp8) return MADAKV_ERR_UNIMPLEMENTED;                        // the cache holds the rows as they are
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  return hip_fail(h, launch_cache_rows(make_dims(c, n), c, k_c, v_c, kv_off, kv_len, k_rows, v_rows, region_tokens(c) * c.batch,
+                                       longest_rows(h, layer0, n, replayed_later(st)), make_paging(h), layer0, st));
+}
+
 namespace {
 // workspace of madakv_reevict: per-row arrays over the whole reduced cache (rows are addressed as in k_c),
 // the per-head records of the call, the exchange array of the scoring kernel
@@ -663,7 +744,7 @@ ReevictWs reevict_layout(const madakv_handle* h, int n) {
   w.stats = w.rowmod + up(cap);
   w.score = w.stats + up((size_t)dm.heads * 8 * c.n_modalities);
   w.lin_k = w.score + up(score_ragged_ws_bytes(dm, c, c.ctx_len + c.max_new_tokens, (long long)cap));
-  const size_t row_bytes = (size_t)c.head_dim * (c.cache_fp8 ? 1 : (c.dtype == MADAKV_BF16 ? 2 : 4));
+  const size_t row_bytes = (size_t)cache_row_bytes(c);
   const size_t lin = c.page_rows ? up(cap * row_bytes) : 0;
   w.lin_v = w.lin_k + lin; w.lin_idx = w.lin_v + lin; w.lin_off = w.lin_idx + (c.page_rows ? up(cap * 4) : 0);
   w.total = w.lin_off + (c.page_rows ? up((size_t)dm.heads * 8) : 0);
@@ -686,7 +767,10 @@ int32_t madakv_reevict(madakv_handle* h, int32_t layer0, int32_t n,
   const madakv_config& c = h->cfg;
   if (bad_ptr(q_recent) || bad_ptr(mask, 1) || bad_ptr(k_c) || bad_ptr(v_c) || bad_ptr(kept_idx, 4) || bad_ptr(kv_off, 8) ||
       bad_ptr(kv_len, 4) || bad_ptr(budgets, 4) || bad_ptr(ws)) return MADAKV_ERR_INVALID_ARG;
+  if (c.cache_fp8 == CACHE_E2M1) return MADAKV_ERR_UNIMPLEMENTED;
   if (c.budget >= c.ctx_len) return MADAKV_ERR_BAD_BUDGET;                 // nothing was evicted, nothing to bring back
+  for (int l = layer0; l < layer0 + n; ++l)
+    if (h->replaced[l]) return MADAKV_ERR_INVALID_ARG;                     // the last rows of a segment are no longer the newest
   // a paged cache hands the pages taken since the eviction back to the pools, which all layers share
   if (c.page_rows && (layer0 != 0 || n != c.n_layers)) return MADAKV_ERR_INVALID_ARG;
   int longest = longest_rows(h, layer0, n);

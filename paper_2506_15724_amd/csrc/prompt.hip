@@ -1,0 +1,396 @@
+// Scores of every key against all queries of the prompt (paper Sec. 3.3 Eq. 7 with every position as a proxy token; the
+// accumulated attention weight of heavy-hitter eviction): for KV head h with G query heads
+//   psi(i) = sum over g, r >= i of exp(scale * q_gr . k_i - lse_gr),   lse_gr = log sum over j <= r of exp(scale * q_gr . k_j)
+// L^2 / 2 logits per query head, which are never stored: sweep 1 forms them for the normalisers (left out where the caller's
+// prefill attention has them), sweep 2 once more for the column sums.
+//
+// Both sweeps are one kernel.  A workgroup holds a block of columns in registers as operand B (sweep 1: query rows, sweep 2: keys;
+// a wave NCB blocks of 32) and streams the rows of the other side through LDS as operand A of the 32x32x16 bf16 MFMA: a lane
+// then has 16 rows of one column of a 32 x 32 tile, and maximum, sum and column sum are in-lane work.
+// What bounds it is the vector unit: a logit costs one exp2 (a quarter-rate instruction: 16 cycles of a SIMD per 64 logits), one
+// multiply-add into it and one addition, 24 cycles per 64 logits, against 16 of the matrix unit at 128 dims (8 at 64).  So the layout
+// saves vector instructions and LDS reads: sweep 1 looks for no maximum, but sums against the reference of the first tile and takes another
+// one when a sum passes 2^60; rows that no column of a wave sees are left out and the causal mask is applied in diagonal tiles only;
+// four blocks of columns share each operand read from LDS.
+// The rows come straight into LDS (16 bytes per lane, pieces of a row permuted so that operand reads do not collide), in a
+// ring of three tiles of 64 rows; LDS accesses and waits of the loop are written out, as in score.hip and for its reason.
+//
+// A head's triangle is cut into items of one column block by at most `chunk` rows, of nearly equal work but for the diagonal; the
+// items of a head go to one XCD, whose L2 then holds the head's rows (4 MB at 16K x 128).  Partial results (sweep 1: maximum and
+// sum, sweep 2: column sums) are joined in chunk order by small kernels.
+#include "common.h"
+
+#include <algorithm>
+
+namespace madakv {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 pbf16x8_t;
+typedef __attribute__((ext_vector_type(16))) float pf32x16_t;
+typedef __attribute__((ext_vector_type(4))) float pf32x4_t;
+typedef __attribute__((address_space(3))) void* plds_ptr_t;
+typedef const __attribute__((address_space(1))) void* pglobal_ptr_t;
+
+constexpr int PR_WAVES = 4, PR_TILE = 64, PR_RING = 3;
+constexpr float PR_UNSEEN = -1.0e30f;           // a masked logit, in accumulator units
+constexpr float PR_FAR = 1.152921504606846976e18f;      // 2^60: a sum beyond it has left its reference behind
+
+struct PromptArgs {
+  const uint16_t* q; const uint16_t* k;         // [n, B, Hq, L, d], [n, B, H, L, d]
+  float* lse2;                                  // [q heads][rows] log2 of the rows' normalisers; +inf past the prompt's end
+  float2* stat;                                 // [q heads][chunks][rows] (maximum, sum) per chunk, log2 units
+  float* part;                                  // [q heads][chunks][rows] column sums per chunk
+  float* psi;
+  int G, L, rows;                               // rows: L rounded up to whole tiles
+  int per_chunk, chunks, blocks;                // column blocks per chunk, chunks, column blocks
+  int items, total;                             // of a head and of all heads, in the sweep at hand
+  float scale_log2;
+};
+
+// item -> (column block, chunk).  Sweep 1: block cb (queries) against chunks 0 .. cb / per_chunk of the keys; sweep 2: block cb
+// (keys) against chunks cb / per_chunk .. of the queries.  Blocks with many chunks come first.
+template <int PASS>
+__device__ __forceinline__ void item_of(const PromptArgs& a, int i, int& cb, int& chunk) {
+  int g = 0;                                    // which stretch of per_chunk blocks, the one with the most chunks first
+  for (; g < a.chunks; ++g) {
+    const int first = (PASS == 1 ? a.chunks - 1 - g : g) * a.per_chunk;
+    const int nb = min(a.per_chunk, a.blocks - first), each = a.chunks - g;
+    if (i < nb * each) {
+      cb = first + i / each;
+      chunk = PASS == 1 ? i % each : g + i % each;
+      return;
+    }
+    i -= nb * each;
+  }
+  cb = chunk = 0;                               // (there is no such item)
+}
+
+template <int D, int NCB, int PASS>             // a wave's column blocks of 32
+__global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, NCB == 4 ? 2 : 4))) void prompt_sweep_kernel(PromptArgs a) {
+  constexpr int KS = D / 16;                    // MFMA steps over the head dimension
+  constexpr int PPR = D / 8;                    // 16-byte pieces per row
+  constexpr int ROWB = D * 2;
+  constexpr int TILEB = PR_TILE * ROWB;
+  constexpr int LPT = PR_TILE * PPR / (PR_WAVES * 64);     // load instructions per wave and tile, 1 KB each
+  constexpr int CB = PR_WAVES * NCB * 32;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];     // [ring][64 rows][D], sweep 2: [ring][waves][64] normalisers
+
+  // workgroup -> item: XCD x (workgroups go to the XCDs in turn) takes the x-th eighth of all items, heads one after the other
+  const int per_xcd = (a.total + 7) / 8;
+  const int idx = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
+  if (idx >= a.total || (int)(blockIdx.x >> 3) >= per_xcd) return;
+  const int qh = idx / a.items;
+  int cb, chunk;
+  item_of<PASS>(a, idx - qh * a.items, cb, chunk);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, col = lane & 31;
+  const uint16_t* qrows = a.q + (long long)qh * a.L * D;
+  const uint16_t* krows = a.k + (long long)(qh / a.G) * a.L * D;           // (query head j of a layer's batch item reads KV head j / G)
+  const unsigned char* cols = reinterpret_cast<const unsigned char*>(PASS == 1 ? qrows : krows);
+  const unsigned char* rows = reinterpret_cast<const unsigned char*>(PASS == 1 ? krows : qrows);
+  const int c0 = cb * CB;
+  const int my0 = c0 + wave * NCB * 32;         // the wave's first column
+  const int chunk_rows = a.per_chunk * CB;
+  const int row0 = PASS == 1 ? chunk * chunk_rows : max(chunk * chunk_rows, c0);
+  const int row1 = min((chunk + 1) * chunk_rows, PASS == 1 ? min(a.rows, (c0 + CB + PR_TILE - 1) / PR_TILE * PR_TILE) : a.rows);
+  const int ntiles = (row1 - row0) / PR_TILE;   // (all of them multiples of the tile; at least one)
+
+  const uint32_t ring = (uint32_t)(uintptr_t)smem;
+  const uint32_t ring_n = ring + PR_RING * TILEB;
+  const float* norm = a.lse2 + (long long)qh * a.rows;
+  // tile T -> ring slot T mod 3: load j of wave w fills bytes [(w LPT + j) 1024, + 1024) of the slot, lane i slot P mod PPR of row P / PPR,
+  // P = (w LPT + j) 64 + i, with that row's piece (P mod PPR) ^ (row mod PPR).  Rows past the prompt's end: its last row.
+  const auto issue = [&](int t) {
+    const int r0 = row0 + t * PR_TILE;
+    const uint32_t slot = ring + (uint32_t)(t % PR_RING) * TILEB;
+#pragma unroll
+    for (int j = 0; j < LPT; ++j) {
+      const int piece = (wave * LPT + j) * 64 + lane, row = piece / PPR;
+      const unsigned char* src = rows + (long long)min(r0 + row, a.L - 1) * ROWB + ((piece % PPR) ^ (row % PPR)) * 16;
+      const uint32_t dst = __builtin_amdgcn_readfirstlane(slot + (uint32_t)(wave * LPT + j) * 1024u);
+      __builtin_amdgcn_global_load_lds((pglobal_ptr_t)(uintptr_t)src, (plds_ptr_t)(uintptr_t)dst, 16, 0, 0);
+    }
+    if (PASS == 2) {                            // the rows' normalisers, every wave its own copy
+      const uint32_t dst = __builtin_amdgcn_readfirstlane(ring_n + (uint32_t)((t % PR_RING) * PR_WAVES + wave) * (PR_TILE * 4u));
+      __builtin_amdgcn_global_load_lds((pglobal_ptr_t)(uintptr_t)(norm + r0 + lane), (plds_ptr_t)(uintptr_t)dst, 4, 0, 0);
+    }
+  };
+  issue(0);
+  issue(min(1, ntiles - 1));
+
+  // the wave's columns; a lane holds, for step ks, elements [half * D/2 + ks * 8, + 8) of column `col` of a block
+  pbf16x8_t breg[NCB][KS];
+#pragma unroll
+  for (int b = 0; b < NCB; ++b) {
+    const unsigned char* src = cols + (long long)min(my0 + b * 32 + col, a.L - 1) * ROWB + half * D;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) breg[b][ks] = *reinterpret_cast<const pbf16x8_t*>(src + ks * 16);
+  }
+  // (here and now: a wait for them in the loop would be one for the tiles behind them as well)
+#pragma unroll
+  for (int b = 0; b < NCB; ++b)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(breg[b][ks]));
+  uint32_t frag[KS];                            // where the lane's pieces of row `col` of a subtile are
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) frag[ks] = (uint32_t)(col * ROWB + (((half * KS + ks) ^ (col % PPR)) * 16));
+
+  float ref[NCB], sum[NCB];                     // sweep 1: reference (log2 units, -inf: none yet) and sum; sweep 2: column sums
+#pragma unroll
+  for (int b = 0; b < NCB; ++b) { ref[b] = -__builtin_inff(); sum[b] = 0.f; }
+
+  pbf16x8_t areg[KS];
+  float nreg[PASS == 2 ? 16 : 1];
+  const auto logits = [&](int b) {
+    pf32x16_t x = pf32x16_t{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(areg[ks], breg[b][ks], x, 0, 0, 0);
+    return x;
+  };
+  const auto masked = [&](pf32x16_t x) {        // the tile on the diagonal: a query sees the keys up to its own
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const int row = 8 * (j >> 2) + 4 * half + (j & 3);
+      x[j] = (PASS == 1 ? row <= col : row >= col) ? x[j] : PR_UNSEEN;
+    }
+    return x;
+  };
+  const auto added = [](const float (&p)[16]) {
+    return (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]))) + (((p[8] + p[9]) + (p[10] + p[11])) + ((p[12] + p[13]) + (p[14] + p[15])));
+  };
+  const auto account = [&](int b, const pf32x16_t& x) {
+    float p[16];
+    if (PASS == 2) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(x[j], a.scale_log2, -nreg[j % (PASS == 2 ? 16 : 1)]));
+      sum[b] += added(p);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(x[j], a.scale_log2, -ref[b]));
+      float s = added(p);
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum[b] + s < PR_FAR)) != 0, 0)) {
+        // some column has no reference yet or has left it far behind: the largest logit becomes the reference
+        float top = x[0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) top = fmaxf(top, x[j]);
+        if (!(sum[b] + s < PR_FAR)) {
+          if (top > 0.5f * PR_UNSEEN) {
+            const float r = fmaxf(sum[b] < 0.5f * PR_FAR ? ref[b] : ref[b] + 59.f, top * a.scale_log2);
+            sum[b] = ref[b] == -__builtin_inff() ? 0.f : sum[b] * __builtin_amdgcn_exp2f(ref[b] - r);
+            ref[b] = r;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(x[j], a.scale_log2, -r));
+            s = added(p);
+          } else if (top == top) {
+            s = 0.f;                            // nothing but masked keys so far
+          }
+        }
+      }
+      sum[b] += s;
+    }
+  };
+
+  for (int t = 0; t < ntiles; ++t) {
+    // tile t has landed (the next one's loads may still be out); behind the barrier that holds for every wave, and nobody
+    // reads tile t - 1 any more, whose slot the next loads take
+    if (LPT + (PASS == 2) == 5) asm volatile("s_waitcnt vmcnt(5) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else if (LPT + (PASS == 2) == 4) asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else if (LPT + (PASS == 2) == 3) asm volatile("s_waitcnt vmcnt(3) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(2) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    static_assert(LPT + (PASS == 2) >= 2 && LPT + (PASS == 2) <= 5, "the waits above are written for these");
+    issue(min(t + 2, ntiles - 1));              // (past the end: the last tile once more, which keeps the count of loads in flight)
+    const uint32_t tile = ring + (uint32_t)(t % PR_RING) * TILEB;
+    const uint32_t tile_n = ring_n + (uint32_t)((t % PR_RING) * PR_WAVES + wave) * (PR_TILE * 4u) + half * 16u;
+#pragma unroll 1
+    for (int sub = 0; sub < PR_TILE / 32; ++sub) {
+      const int r = row0 + t * PR_TILE + sub * 32;
+      // sweep 1: keys behind the wave's last query; sweep 2: queries in front of its first key
+      if (PASS == 1 ? r > my0 + (NCB - 1) * 32 : r < my0) continue;
+      const uint32_t at = tile + (uint32_t)sub * (32 * ROWB);
+      if constexpr (KS == 8) {
+        asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\tds_read_b128 %2, %10\n\tds_read_b128 %3, %11\n\t"
+                     "ds_read_b128 %4, %12\n\tds_read_b128 %5, %13\n\tds_read_b128 %6, %14\n\tds_read_b128 %7, %15\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(areg[0]), "=&v"(areg[1]), "=&v"(areg[2]), "=&v"(areg[3]), "=&v"(areg[4]), "=&v"(areg[5]), "=&v"(areg[6]), "=&v"(areg[7])
+                     : "v"(at + frag[0]), "v"(at + frag[1]), "v"(at + frag[2]), "v"(at + frag[3]), "v"(at + frag[4]), "v"(at + frag[5]), "v"(at + frag[6]), "v"(at + frag[7])
+                     : "memory");
+      } else {
+        asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(areg[0]), "=&v"(areg[1]), "=&v"(areg[2]), "=&v"(areg[3])
+                     : "v"(at + frag[0]), "v"(at + frag[1]), "v"(at + frag[2]), "v"(at + frag[3]) : "memory");
+      }
+      if constexpr (PASS == 2) {
+        pf32x4_t n0, n1, n2, n3;
+        asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:32\n\tds_read_b128 %2, %4 offset:64\n\tds_read_b128 %3, %4 offset:96\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(n0), "=&v"(n1), "=&v"(n2), "=&v"(n3) : "v"(tile_n + (uint32_t)sub * 128u) : "memory");
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { nreg[j] = n0[j]; nreg[4 + j] = n1[j]; nreg[8 + j] = n2[j]; nreg[12 + j] = n3[j]; }
+      }
+      if (PASS == 1 ? r < my0 : r > my0 + (NCB - 1) * 32) {        // off the diagonal for all blocks
+#pragma unroll
+        for (int b = 0; b < NCB; ++b) account(b, logits(b));
+      } else {
+#pragma unroll
+        for (int b = 0; b < NCB; ++b) {
+          const int mine = my0 + b * 32;
+          if (PASS == 1 ? r < mine : r > mine) account(b, logits(b));
+          else if (r == mine) account(b, masked(logits(b)));
+        }
+      }
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");      // (the loads past the end write to LDS, too)
+
+  // the two halves of a column
+#pragma unroll
+  for (int b = 0; b < NCB; ++b) {
+    const int c = my0 + b * 32 + col;
+    const float other = __shfl_xor(sum[b], 32, 64);
+    if (PASS == 2) {
+      if (half == 0 && c < a.L) {
+        const float s = sum[b] + other;
+        if (a.chunks == 1 && a.G == 1) a.psi[(long long)qh * a.L + c] = s;
+        else a.part[((long long)qh * a.chunks + chunk) * a.rows + c] = s;
+      }
+    } else {
+      const float other_ref = __shfl_xor(ref[b], 32, 64);
+      // (a half that has seen no key: reference -inf, sum 0, whose weight is not asked for)
+      const float r = fmaxf(ref[b], other_ref);
+      const float w0 = ref[b] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ref[b] - r), w1 = other_ref == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(other_ref - r);
+      const float s = half == 0 ? sum[b] * w0 + other * w1 : other * w1 + sum[b] * w0;
+      if (half == 0 && c < a.rows) {
+        if (a.chunks == 1) a.lse2[(long long)qh * a.rows + c] = c < a.L ? r + log2f(s) : __builtin_inff();
+        else a.stat[((long long)qh * a.chunks + chunk) * a.rows + c] = make_float2(r, s);
+      }
+    }
+  }
+}
+
+// log2 of the rows' normalisers: from the chunks' (maximum, sum), or from the caller's natural logarithms
+__global__ __launch_bounds__(256) void prompt_normaliser_kernel(PromptArgs a, const float* row_lse, int cb_rows, long long n) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const long long qh = i / a.rows;
+  const int r = (int)(i - qh * a.rows);
+  float out = __builtin_inff();                 // rows past the prompt's end count for nothing
+  if (r < a.L) {
+    if (row_lse) {
+      out = row_lse[qh * a.L + r] * 1.4426950408889634f;
+    } else {
+      const int last = r / (a.per_chunk * cb_rows);          // the chunk with the row's own key
+      float m = -__builtin_inff(), s = 0.f;
+      for (int c = 0; c <= last; ++c) {
+        const float2 x = a.stat[(qh * a.chunks + c) * a.rows + r];
+        const float t = fmaxf(m, x.x);
+        s = (m == -__builtin_inff() ? 0.f : s * __builtin_amdgcn_exp2f(m - t)) + (x.x == -__builtin_inff() ? 0.f : x.y * __builtin_amdgcn_exp2f(x.x - t));
+        m = t;
+      }
+      out = m + log2f(s);
+    }
+  }
+  a.lse2[i] = out;
+}
+
+// psi = the column sums of the query heads and chunks, in that order; scaled: psi * factor beside it
+__global__ __launch_bounds__(256) void prompt_sum_kernel(PromptArgs a, int cb_rows, float* scaled, float factor, long long n) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const long long kvh = i / a.L;
+  const int c = (int)(i - kvh * a.L);
+  float s = 0.f;
+  if (a.chunks == 1 && a.G == 1) {
+    s = a.psi[i];
+  } else {
+    const int first = c / (a.per_chunk * cb_rows);           // the chunk with the key's own query
+    for (int g = 0; g < a.G; ++g) {
+      float sg = 0.f;
+      for (int k = first; k < a.chunks; ++k) sg += a.part[((kvh * a.G + g) * a.chunks + k) * a.rows + c];
+      s += sg;
+    }
+    a.psi[i] = s;
+  }
+  if (scaled) scaled[i] = s * factor;
+}
+
+struct PromptPlan { int ncb, per_chunk, chunks, blocks, items[2]; };      // items of a head in sweep 1 and 2 (item_of)
+// Column blocks of 512 (a wave has four blocks of 32) where those give the chip two workgroups per compute unit to work on, of 128
+// otherwise; chunks as long as leave 2048 items in the launch (four rounds of workgroups, so that the last one is a small part), at
+// least one column block.
+static PromptPlan prompt_plan(const Dims& dm) {
+  PromptPlan p;
+  const long long qheads = (long long)dm.n * dm.B * dm.Hq;
+  for (int ncb : {4, 1}) {
+    const int cb = PR_WAVES * ncb * 32;
+    p.ncb = ncb;
+    p.blocks = (dm.L + cb - 1) / cb;
+    for (p.per_chunk = p.blocks;; p.per_chunk = (p.per_chunk + 1) / 2) {
+      p.chunks = (p.blocks + p.per_chunk - 1) / p.per_chunk;
+      p.items[0] = p.items[1] = 0;
+      for (int g = 0; g < p.chunks; ++g) {
+        const int nb = std::min(p.per_chunk, p.blocks - g * p.per_chunk);
+        p.items[0] += nb * (g + 1);
+        p.items[1] += nb * (p.chunks - g);
+      }
+      if (qheads * p.items[0] >= 2048 || p.per_chunk == 1) break;
+    }
+    if (qheads * p.items[0] >= 512) break;
+  }
+  return p;
+}
+static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+static size_t rows_of(const Dims& dm) { return (size_t)(dm.L + PR_TILE - 1) / PR_TILE * PR_TILE; }
+
+bool prompt_supported(const madakv_config& c) { return c.dtype == MADAKV_BF16; }
+// normalisers, then what the chunks leave (sweep 2's column sums take the place of sweep 1's statistics), then the scaled scores
+size_t prompt_ws_bytes(const Dims& dm) {
+  const PromptPlan p = prompt_plan(dm);
+  const size_t qheads = (size_t)dm.n * dm.B * dm.Hq;
+  return up256(qheads * rows_of(dm) * 4) + up256(qheads * p.chunks * rows_of(dm) * 8) + up256((size_t)dm.heads * dm.L * 4);
+}
+
+template <int D, int NCB>
+static hipError_t launch_sweeps(const Dims& dm, const PromptPlan& p, PromptArgs& a, const float* row_lse, float* scaled, float factor, hipStream_t st) {
+  constexpr int CB = PR_WAVES * NCB * 32;
+  constexpr size_t lds1 = (size_t)PR_RING * PR_TILE * D * 2, lds2 = lds1 + (size_t)PR_RING * PR_WAVES * PR_TILE * 4;
+  const dim3 block(PR_WAVES * 64);
+  const auto grid_of = [&](int pass) {
+    a.items = p.items[pass - 1];
+    a.total = dm.n * dm.B * dm.Hq * a.items;
+    return dim3((unsigned)((a.total + 7) / 8 * 8));
+  };
+  const long long nrows = (long long)dm.n * dm.B * dm.Hq * a.rows, npsi = (long long)dm.heads * dm.L;
+  if (!row_lse) {
+    const dim3 grid = grid_of(1);
+    hipLaunchKernelGGL((prompt_sweep_kernel<D, NCB, 1>), grid, block, lds1, st, a);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
+  if (row_lse || a.chunks > 1) {
+    hipLaunchKernelGGL(prompt_normaliser_kernel, dim3((unsigned)((nrows + 255) / 256)), dim3(256), 0, st, a, row_lse, CB, nrows);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
+  const dim3 grid = grid_of(2);
+  hipLaunchKernelGGL((prompt_sweep_kernel<D, NCB, 2>), grid, block, lds2, st, a);
+  if (hipError_t e = hipGetLastError()) return e;
+  if (a.chunks > 1 || a.G > 1 || scaled) hipLaunchKernelGGL(prompt_sum_kernel, dim3((unsigned)((npsi + 255) / 256)), dim3(256), 0, st, a, CB, scaled, factor, npsi);
+  return hipGetLastError();
+}
+
+// scaled: psi * factor as well, at the workspace's end; its address is left in *scaled
+hipError_t launch_prompt(const Dims& dm, const madakv_config& c, const void* q, const void* k, const float* row_lse, float* psi,
+                         void* ws, float factor, float** scaled, hipStream_t st) {
+  const PromptPlan p = prompt_plan(dm);
+  const size_t qheads = (size_t)dm.n * dm.B * dm.Hq;
+  PromptArgs a;
+  a.q = static_cast<const uint16_t*>(q); a.k = static_cast<const uint16_t*>(k);
+  a.psi = psi; a.G = dm.G; a.L = dm.L; a.rows = (int)rows_of(dm);
+  char* w = static_cast<char*>(ws);
+  a.lse2 = reinterpret_cast<float*>(w); w += up256(qheads * a.rows * 4);
+  a.stat = reinterpret_cast<float2*>(w); a.part = reinterpret_cast<float*>(w); w += up256(qheads * p.chunks * a.rows * 8);
+  float* s = nullptr;
+  if (scaled) *scaled = s = reinterpret_cast<float*>(w);
+  a.per_chunk = p.per_chunk; a.chunks = p.chunks; a.blocks = p.blocks;
+  a.scale_log2 = (c.softmax_scale > 0.f ? c.softmax_scale : 1.0f / sqrtf((float)dm.d)) * 1.4426950408889634f;
+  if (dm.d == 128) return p.ncb == 4 ? launch_sweeps<128, 4>(dm, p, a, row_lse, s, factor, st) : launch_sweeps<128, 1>(dm, p, a, row_lse, s, factor, st);
+  return p.ncb == 4 ? launch_sweeps<64, 4>(dm, p, a, row_lse, s, factor, st) : launch_sweeps<64, 1>(dm, p, a, row_lse, s, factor, st);
+}
+
+}  // namespace madakv
