@@ -7,11 +7,17 @@
 // Both sweeps are one kernel.  A workgroup holds a block of columns in registers as operand B (sweep 1: query rows, sweep 2: keys;
 // a wave NCB blocks of 32) and streams the rows of the other side through LDS as operand A of the 32x32x16 bf16 MFMA: a lane
 // then has 16 rows of one column of a 32 x 32 tile, and maximum, sum and column sum are in-lane work.
-// What bounds it is the vector unit: a logit costs one exp2 (a quarter-rate instruction: 16 cycles of a SIMD per 64 logits), one
-// multiply-add into it and one addition, 24 cycles per 64 logits, against 16 of the matrix unit at 128 dims (8 at 64).  So the layout
-// saves vector instructions and LDS reads: sweep 1 looks for no maximum, but sums against the reference of the first tile and takes another
-// one when a sum passes 2^60; rows that no column of a wave sees are left out and the causal mask is applied in diagonal tiles only;
-// four blocks of columns share each operand read from LDS.
+// What bounds it: a 32 x 32 tile of logits is 8 matrix instructions (256 cycles of a SIMD at 128 dims), 16 exp2, 16 multiply-adds into
+// them and 16 additions (280 cycles, measured alone; 320 with the matrix instructions beside them).  That work at the chip's power
+// limit: the loop without any loads takes 200 ns per tile and SIMD on random operands (the clock falls to 1.75 - 2.1 GHz), 169 on
+// zeros (2.4 GHz), whether two, three or four waves share a SIMD and however the instructions are ordered.  So the layout saves
+// instructions: sweep 1 looks for no maximum, but sums against the reference of the first tile and takes another
+// one when a sum passes 2^60 (a tile is then formed again); rows that no column of a wave sees are left out and the causal mask is
+// applied in diagonal tiles only; four blocks of columns share each operand read from LDS; a lane's offset in a tile is the same for all tiles.
+// 16K tokens, 28 / 4 heads of 128 dims, both sweeps: 1.79 ms, 240 ns per tile and SIMD, 1.08 PFLOP/s of logits (a library product of
+// 16K x 16K x 16K bf16 runs at 1.36 on this card); 8K tokens, 32 heads, one sweep 0.27 ms.  Kept steps: address arithmetic per load -> a
+// buffer with fixed offsets 1.85 -> 1.80; a block's contraction between the vector instructions of the one before it 1.89 -> 1.85.
+// No gain: blocks of two and three waves per SIMD (1.87), heads in plain order instead of one XCD's (1.84).
 // The rows come straight into LDS (16 bytes per lane, pieces of a row permuted so that operand reads do not collide), in a
 // ring of three tiles of 64 rows; LDS accesses and waits of the loop are written out, as in score.hip and for its reason.
 //
@@ -28,11 +34,10 @@ typedef __attribute__((ext_vector_type(8))) __bf16 pbf16x8_t;
 typedef __attribute__((ext_vector_type(16))) float pf32x16_t;
 typedef __attribute__((ext_vector_type(4))) float pf32x4_t;
 typedef __attribute__((address_space(3))) void* plds_ptr_t;
-typedef const __attribute__((address_space(1))) void* pglobal_ptr_t;
 
 constexpr int PR_WAVES = 4, PR_TILE = 64, PR_RING = 3;
 constexpr float PR_UNSEEN = -1.0e30f;           // a masked logit, in accumulator units
-constexpr float PR_FAR = 1.152921504606846976e18f;      // 2^60: a sum beyond it has left its reference behind
+constexpr float PR_FAR = 0x1p60f;               // sums beyond it have left their references behind
 
 struct PromptArgs {
   const uint16_t* q; const uint16_t* k;         // [n, B, Hq, L, d], [n, B, H, L, d]
@@ -62,6 +67,15 @@ __device__ __forceinline__ void item_of(const PromptArgs& a, int i, int& cb, int
     i -= nb * each;
   }
   cb = chunk = 0;                               // (there is no such item)
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000); }
+// lane i: 16 (4) bytes from `at` + base of the buffer, zeros past its end, to LDS address dst + 16 i (4 i)
+__device__ __forceinline__ void to_lds16(__amdgpu_buffer_rsrc_t b, uint32_t dst, int at, int base) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (plds_ptr_t)(uintptr_t)dst, 16, at, base, 0, 0);
+}
+__device__ __forceinline__ void to_lds4(__amdgpu_buffer_rsrc_t b, uint32_t dst, int at, int base) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (plds_ptr_t)(uintptr_t)dst, 4, at, base, 0, 0);
 }
 
 template <int D, int NCB, int PASS>             // a wave's column blocks of 32
@@ -96,23 +110,24 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
 
   const uint32_t ring = (uint32_t)(uintptr_t)smem;
   const uint32_t ring_n = ring + PR_RING * TILEB;
-  const float* norm = a.lse2 + (long long)qh * a.rows;
   // tile T -> ring slot T mod 3: load j of wave w fills bytes [(w LPT + j) 1024, + 1024) of the slot, lane i slot P mod PPR of row P / PPR,
-  // P = (w LPT + j) 64 + i, with that row's piece (P mod PPR) ^ (row mod PPR).  Rows past the prompt's end: its last row.
+  // P = (w LPT + j) 64 + i, with that row's piece (P mod PPR) ^ (row mod PPR).  Through a buffer that ends with the prompt: rows
+  // past its end are zeros, and a lane's offset in a tile is the same for all tiles.
+  const __amdgpu_buffer_rsrc_t rows_buf = buffer_of(rows, a.L * ROWB), norm_buf = buffer_of(a.lse2 + (long long)qh * a.rows, a.rows * 4);
+  int piece_off[LPT];
+#pragma unroll
+  for (int j = 0; j < LPT; ++j) {
+    const int piece = (wave * LPT + j) * 64 + lane, row = piece / PPR;
+    piece_off[j] = row * ROWB + ((piece % PPR) ^ (row % PPR)) * 16;
+  }
   const auto issue = [&](int t) {
     const int r0 = row0 + t * PR_TILE;
-    const uint32_t slot = ring + (uint32_t)(t % PR_RING) * TILEB;
+    const uint32_t slot = (uint32_t)(t % PR_RING);
 #pragma unroll
-    for (int j = 0; j < LPT; ++j) {
-      const int piece = (wave * LPT + j) * 64 + lane, row = piece / PPR;
-      const unsigned char* src = rows + (long long)min(r0 + row, a.L - 1) * ROWB + ((piece % PPR) ^ (row % PPR)) * 16;
-      const uint32_t dst = __builtin_amdgcn_readfirstlane(slot + (uint32_t)(wave * LPT + j) * 1024u);
-      __builtin_amdgcn_global_load_lds((pglobal_ptr_t)(uintptr_t)src, (plds_ptr_t)(uintptr_t)dst, 16, 0, 0);
-    }
-    if (PASS == 2) {                            // the rows' normalisers, every wave its own copy
-      const uint32_t dst = __builtin_amdgcn_readfirstlane(ring_n + (uint32_t)((t % PR_RING) * PR_WAVES + wave) * (PR_TILE * 4u));
-      __builtin_amdgcn_global_load_lds((pglobal_ptr_t)(uintptr_t)(norm + r0 + lane), (plds_ptr_t)(uintptr_t)dst, 4, 0, 0);
-    }
+    for (int j = 0; j < LPT; ++j)
+      to_lds16(rows_buf, ring + slot * TILEB + (uint32_t)(wave * LPT + j) * 1024u, piece_off[j], r0 * ROWB);
+    if (PASS == 2)                              // the rows' normalisers, every wave its own copy
+      to_lds4(norm_buf, ring_n + (slot * PR_WAVES + wave) * (PR_TILE * 4u), lane * 4, r0 * 4);
   };
   issue(0);
   issue(min(1, ntiles - 1));
@@ -154,39 +169,30 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
     }
     return x;
   };
-  const auto added = [](const float (&p)[16]) {
+  // the sum of a column's 16 terms: against the rows' normalisers, or its own reference
+  const auto terms = [&](int b, const pf32x16_t& x) {
+    float p[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(x[j], a.scale_log2, PASS == 2 ? -nreg[j % (PASS == 2 ? 16 : 1)] : -ref[b]));
     return (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]))) + (((p[8] + p[9]) + (p[10] + p[11])) + ((p[12] + p[13]) + (p[14] + p[15])));
   };
-  const auto account = [&](int b, const pf32x16_t& x) {
-    float p[16];
-    if (PASS == 2) {
+  // sweep 1, a tile for which some column has no reference yet or has left it far behind: there the largest logit becomes the
+  // reference
+  const auto look = [&](int b, const pf32x16_t& x) {
+    float s = terms(b, x), top = x[0];
 #pragma unroll
-      for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(x[j], a.scale_log2, -nreg[j % (PASS == 2 ? 16 : 1)]));
-      sum[b] += added(p);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(x[j], a.scale_log2, -ref[b]));
-      float s = added(p);
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum[b] + s < PR_FAR)) != 0, 0)) {
-        // some column has no reference yet or has left it far behind: the largest logit becomes the reference
-        float top = x[0];
-#pragma unroll
-        for (int j = 1; j < 16; ++j) top = fmaxf(top, x[j]);
-        if (!(sum[b] + s < PR_FAR)) {
-          if (top > 0.5f * PR_UNSEEN) {
-            const float r = fmaxf(sum[b] < 0.5f * PR_FAR ? ref[b] : ref[b] + 59.f, top * a.scale_log2);
-            sum[b] = ref[b] == -__builtin_inff() ? 0.f : sum[b] * __builtin_amdgcn_exp2f(ref[b] - r);
-            ref[b] = r;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(x[j], a.scale_log2, -r));
-            s = added(p);
-          } else if (top == top) {
-            s = 0.f;                            // nothing but masked keys so far
-          }
-        }
+    for (int j = 1; j < 16; ++j) top = fmaxf(top, x[j]);
+    if (!(sum[b] + s < 0.25f * PR_FAR)) {       // (also: no number)
+      if (top > 0.5f * PR_UNSEEN) {
+        const float r = fmaxf(sum[b] < 0x1p50f ? ref[b] : ref[b] + 50.f, top * a.scale_log2);
+        sum[b] = ref[b] == -__builtin_inff() ? 0.f : sum[b] * __builtin_amdgcn_exp2f(ref[b] - r);
+        ref[b] = r;
+        s = terms(b, x);
+      } else if (top == top) {
+        s = 0.f;                                // nothing but masked keys so far
       }
-      sum[b] += s;
     }
+    sum[b] += s;
   };
 
   for (int t = 0; t < ntiles; ++t) {
@@ -226,14 +232,45 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
         for (int j = 0; j < 4; ++j) { nreg[j] = n0[j]; nreg[4 + j] = n1[j]; nreg[8 + j] = n2[j]; nreg[12 + j] = n3[j]; }
       }
       if (PASS == 1 ? r < my0 : r > my0 + (NCB - 1) * 32) {        // off the diagonal for all blocks
+        // a block's contraction is issued between the vector instructions of the block before it
+        float s[NCB];
+        pf32x16_t x = logits(0);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int b = 0; b < NCB; ++b) account(b, logits(b));
+        for (int b = 0; b < NCB; ++b) {
+          const pf32x16_t now = x;
+          if (b + 1 < NCB) x = logits(b + 1);
+          s[b] = sum[b] + terms(b, now);
+          if (b + 1 < NCB) {
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+              __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);           // one matrix instruction,
+              __builtin_amdgcn_sched_group_barrier(0x002, 32 / KS, 0);     // so many multiply-adds and additions,
+              __builtin_amdgcn_sched_group_barrier(0x400, 16 / KS, 0);     // so many exp2
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (PASS == 1) {
+          float all = s[0];
+#pragma unroll
+          for (int b = 1; b < NCB; ++b) all += s[b];
+          if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(all < PR_FAR)) != 0, 0)) {
+#pragma unroll
+            for (int b = 0; b < NCB; ++b) look(b, logits(b));
+            continue;
+          }
+        }
+#pragma unroll
+        for (int b = 0; b < NCB; ++b) sum[b] = s[b];
       } else {
 #pragma unroll
         for (int b = 0; b < NCB; ++b) {
           const int mine = my0 + b * 32;
-          if (PASS == 1 ? r < mine : r > mine) account(b, logits(b));
-          else if (r == mine) account(b, masked(logits(b)));
+          if (PASS == 1 ? r > mine : r < mine) continue;
+          const pf32x16_t x = r == mine ? masked(logits(b)) : logits(b);
+          if (PASS == 1) look(b, x);
+          else sum[b] += terms(b, x);
         }
       }
     }
@@ -313,13 +350,18 @@ __global__ __launch_bounds__(256) void prompt_sum_kernel(PromptArgs a, int cb_ro
 
 struct PromptPlan { int ncb, per_chunk, chunks, blocks, items[2]; };      // items of a head in sweep 1 and 2 (item_of)
 // Column blocks of 512 (a wave has four blocks of 32) where those give the chip two workgroups per compute unit to work on, of 128
-// otherwise; chunks as long as leave 2048 items in the launch (four rounds of workgroups, so that the last one is a small part), at
-// least one column block.
+// otherwise; chunks as long as leave enough items for the launch's last round of workgroups to be a small part of it (2300 of the
+// large ones, of which 512 run at a time; 500 of the small ones, of which 1024 do), but no shorter than 512 (256) rows: every
+// item starts with its columns and an empty ring.  us per call, 28 / 4 heads of 128 dims, at least 1200 / 2300 / 4100 large items: 16K 2112 /
+// 1788 / 1799, 32 heads of 8K with normalisers 293 / 274 / 279.  500 / 1000 small ones: 1K 36.5 / 44.7, 2K 67.4 / 66.8, 64 heads of 700
+// 33.2 / 37.4, 8 / 1 heads of 4K 74.9 / 82.9.  Chunks of at least 128 / 256 / 512 rows: 8 heads of 203 x 64 18.4 / 12.8 / 12.8 (one chunk: two launches
+// instead of four), of 1K 20.8 / 19.9 / 24.2.
+constexpr int PR_MANY = 512, PR_ITEMS4 = 2300, PR_ITEMS1 = 500;
 static PromptPlan prompt_plan(const Dims& dm) {
   PromptPlan p;
   const long long qheads = (long long)dm.n * dm.B * dm.Hq;
   for (int ncb : {4, 1}) {
-    const int cb = PR_WAVES * ncb * 32;
+    const int cb = PR_WAVES * ncb * 32, shortest = ncb == 4 ? 1 : 2;
     p.ncb = ncb;
     p.blocks = (dm.L + cb - 1) / cb;
     for (p.per_chunk = p.blocks;; p.per_chunk = (p.per_chunk + 1) / 2) {
@@ -330,9 +372,9 @@ static PromptPlan prompt_plan(const Dims& dm) {
         p.items[0] += nb * (g + 1);
         p.items[1] += nb * (p.chunks - g);
       }
-      if (qheads * p.items[0] >= 2048 || p.per_chunk == 1) break;
+      if (qheads * p.items[0] >= (ncb == 4 ? PR_ITEMS4 : PR_ITEMS1) || p.per_chunk <= shortest) break;
     }
-    if (qheads * p.items[0] >= 512) break;
+    if (qheads * p.items[0] >= PR_MANY) break;
   }
   return p;
 }
