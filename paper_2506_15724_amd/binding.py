@@ -265,6 +265,7 @@ class MadaKV:
         self.kept_idx = torch.empty(self.capacity, dtype=torch.int32, device=dev)
         self.kv_off = torch.empty(NL, B, H, dtype=torch.int64, device=dev)
         self.kv_len = torch.empty(NL, B, H, dtype=torch.int32, device=dev)
+        self._device = self.kv_len.device                # (as its tensors give it, with a number)
         cdt = torch.uint8 if cache_fp8 else self.tdtype
         # (4 bits: the codes of all rows, then their scales)
         shape = (self.capacity * (head_dim // 2 + head_dim // 32),) if cache_fp8 == 4 else (self.capacity, head_dim)
@@ -336,23 +337,31 @@ class MadaKV:
 
     def _check_array(self, name, t, numel, dtype):
         """Arrays that the library indexes by the shape of the call."""
-        if t is not None and (t.dtype != dtype or t.numel() < numel or t.device != self.kv_len.device):
-            raise ValueError(f"{name} must hold {numel} elements of {dtype} on {self.kv_len.device}; got {t.numel()} of {t.dtype} on {t.device}")
+        if t is not None and (t.dtype != dtype or t.numel() < numel or t.device != self._device):
+            raise ValueError(f"{name} must hold {numel} elements of {dtype} on {self._device}; got {t.numel()} of {t.dtype} on {t.device}")
 
     def decode_attn_weights(self, l0, n, q, k_new, v_new, out, acc_in, acc_out, decay=1.0, slot_in=None, slot_out=None, pos=None, recent=0):
         """kept_idx is the holder's own, kept up where the tokens' positions `pos` are given."""
-        c, heads = self.cfg, n * self._heads
+        # (once per layer and token, like decode_attn: no views of the own buffers)
+        heads = n * self._heads
         self._check_out(out, n * self._out_row)
         self._check_array("acc_in", acc_in, self.capacity, torch.float32)
-        self._check_array("acc_out", acc_out, self.capacity, torch.float32)
+        if acc_out is not acc_in:
+            self._check_array("acc_out", acc_out, self.capacity, torch.float32)
         self._check_array("slot_in", slot_in, heads, torch.int32)
-        self._check_array("slot_out", slot_out, heads, torch.int32)
-        self._check_array("pos", pos, c.batch, torch.int32)
+        if slot_out is not slot_in:
+            self._check_array("slot_out", slot_out, heads, torch.int32)
+        self._check_array("pos", pos, self.cfg.batch, torch.int32)
         if getattr(self, "weights_ws", None) is None:
             need = max(madakv_decode_attn_weights_workspace_bytes(self.h, m) for m in (1, self.n_call))
             self.weights_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-        madakv_decode_attn_weights(self.h, l0, n, q, k_new, v_new, self.k_c, self.v_c, self._sl(self.kv_off, l0, n), self._sl(self.kv_len, l0, n),
-                                   out, acc_in, acc_out, decay, slot_in, slot_out, None if pos is None else self.kept_idx, pos, recent, self.weights_ws)
+        heads0, ws = l0 * self._heads, self.weights_ws
+        rc = lib().madakv_decode_attn_weights(
+            self.h, l0, n, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(self.k_c), _ptr(self.v_c), _ptr(self.kv_off) + 8 * heads0, _ptr(self.kv_len) + 4 * heads0,
+            _ptr(out), _ptr(acc_in), _ptr(acc_out), decay, _ptr(slot_in), _ptr(slot_out), None if pos is None else _ptr(self.kept_idx), _ptr(pos), recent,
+            _ptr(ws), ws.numel() * ws.element_size(), _stream())
+        if rc != OK:
+            raise MadaKVError("madakv_decode_attn_weights", rc)
 
     def cache_rows(self, l0, n, k_rows, v_rows):
         for name, t in (("k_rows", k_rows), ("v_rows", v_rows)):

@@ -449,8 +449,12 @@ static int plan_chunk_rows(const Dims& dm, const madakv_config& c) {
   // (smaller chunks lose to per-workgroup start-up cost, one workgroup per head to the imbalance
   // of ragged lengths), growing to 1024 rows when the heads are long (un-evicted cache), so that
   // the chip sees about eight workgroups per CU; 512 rows once a call covers >= 1024 heads.
-  if (dm.heads >= 1024) return 512;
   const long long typical = std::min(c.budget, c.ctx_len) + c.max_new_tokens;    // rows of an average head
+  // 4-bit rows, a wave's tile of which is 4 KB: about 512 pieces in a launch.  Us per call, pieces of 256 / 512 / 1024 rows: 128 heads of
+  // 1K rows 8.7 / 9.0 / 10.0, of 2K 12.1 / 11.3 / 11.9, of 4K 20.6 / 18.4 / 17.5, of 16K 53.8 / 52.8 / 53.4, 512 of 512 12.0 / 9.7 / 10.1, 1024 of 1K
+  // 31.8 / 31.9 / 28.6; few heads: 32 of 2K 7.5 / 8.7 / 11.3, of 8K 12.6 / 11.5 / 12.2, 4 of 16K with 7 queries each 10.4 / 9.8 / 11.8.
+  if (c.cache_fp8 == CACHE_E2M1) return (int)std::min<long long>(1024, std::max<long long>(256, std::max(dm.heads * typical / 512, typical / 64) / 256 * 256));
+  if (dm.heads >= 1024) return 512;
   const long long per = ((long long)dm.heads * typical + 2047) / 2048;
   const long long by_len = typical / 64;                     // a long head is not cut into more than ~64 chunks
   return (int)std::min<long long>(1024, std::max<long long>(256, std::max(per, by_len) / 256 * 256));

@@ -13,7 +13,7 @@
 
 namespace madakv {
 
-constexpr int RW_THREADS = 256, RW_UNROLL = 4, RW_ROWS = RW_THREADS * RW_UNROLL;
+constexpr int RW_THREADS = 512, RW_UNROLL = 2, RW_ROWS = RW_THREADS * RW_UNROLL;
 
 struct RowWeightArgs {
   WeightArgs w;
@@ -41,7 +41,7 @@ __global__ __launch_bounds__(RW_THREADS) void row_weights_kernel(RowWeightArgs a
 #pragma unroll
   for (int g = 0; g < GT; ++g) {
     const float2 ml = g < a.G ? *reinterpret_cast<const float2*>(w.head_ml + ((long long)hidx * a.G + g) * 2) : make_float2(0.f, 1.f);
-    mx[g] = ml.x; inv[g] = 1.0f / ml.y;
+    mx[g] = ml.x; inv[g] = __builtin_amdgcn_rcpf(ml.y);          // (1 unit of the last place: what exp2 is off by as well)
   }
   const float* lg = w.logits + (long long)hidx * a.G * w.logit_rows;
   // all of a thread's loads in front of what uses them

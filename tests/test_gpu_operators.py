@@ -589,3 +589,78 @@ def test_two_caches_on_two_streams():
             e.close()
     for (name, a), (_, b) in zip(alone, both):
         assert torch.equal(a, b), name
+
+
+def test_fp4_eviction_of_many_layers(monkeypatch):
+    """madakv_evict over layer groups (gathers beside per-head kernels) fills the 4-bit cache with the bytes of the three calls."""
+    NL, B, H, L, W, d = 8, 2, 4, 900, 16, 64
+    monkeypatch.setenv("MADAKV_LAYER_GROUPS", "4")
+    g = torch.Generator(device=DEV).manual_seed(12)
+    q, k, v = (torch.randn(NL, B, H, n, d, generator=g, device=DEV).to(torch.bfloat16) for n in (W, L, L))
+    mask = torch.randint(0, 2, (B, L), generator=g, device=DEV).to(torch.uint8)
+    got = []
+    for fused in (True, False):
+        eng = MB.MadaKV(n_layers=NL, batch=B, n_q_heads=H, n_kv_heads=H, head_dim=d, ctx_len=L, window=W, budget=200, max_new_tokens=0, cache_fp8=4, device=DEV)
+        if fused:
+            eng.evict(0, NL, q, k, v, mask)
+        else:
+            for l in range(NL):
+                eng.score(l, 1, q[l:l + 1], k[l:l + 1], mask)
+                eng.allocate(l, 1)
+                eng.select_gather(l, 1, k[l:l + 1], v[l:l + 1], mask)
+        torch.cuda.synchronize()
+        got.append([t.clone() for t in (eng.kept_idx, eng.kv_off, eng.kv_len, eng.k_c, eng.v_c)])
+        eng.close()
+    assert all(torch.equal(a, b) for a, b in zip(*got))             # (no free rows: every byte belongs to a head)
+
+
+@pytest.mark.parametrize("d", [128, 64])
+def test_rows_far_into_a_large_cache(d):
+    """Segments behind the first 4 GiB of codes and the first 2^31 / d rows of values: the last layer's heads of a cache of 71 M
+    (142 M) rows, set up by hand."""
+    NL, B, H, Hq, L = (64 if d == 128 else 128), 16, 64, 64, 1080
+    eng = MB.MadaKV(n_layers=NL, batch=B, n_q_heads=Hq, n_kv_heads=H, head_dim=d, ctx_len=L, window=4, budget=L, max_new_tokens=2, cache_fp8=4, layers_per_call=1, device=DEV)
+    args = dict(n_layers=1, batch=B, n_kv_heads=H, n_q_heads=Hq, head_dim=d, cache_fp8=4)
+    assert eng.capacity * (d // 2) > 1 << 32
+    per = eng.capacity // B                                       # a batch item's region; the layer's heads are at its end
+    off = torch.zeros(1, B, H, dtype=torch.int64)
+    for b in range(B):
+        for h in range(H):
+            off[0, b, h] = (b + 1) * per - (H - h) * (L + 2)
+    lens = torch.randint(200, 600, (1, B, H), generator=torch.Generator().manual_seed(1)).int()
+    eng.kv_off[NL - 1:].copy_(off), eng.kv_len[NL - 1:].copy_(lens)
+    g = torch.Generator(device=DEV).manual_seed(2)
+    heads = [(0, 0), (B - 1, H - 1), (B - 1, 0), (B // 2, 7)]
+    src = {}
+    for b, h in heads:
+        o, n = int(off[0, b, h]), int(lens[0, b, h])
+        for name, cache in (("k", eng.k_c), ("v", eng.v_c)):
+            x = torch.randn(n, d, generator=g, device=DEV).to(torch.bfloat16)
+            code, scale = O.quantize_mx4(x.cpu().double().numpy())
+            cache[o * (d // 2):(o + n) * (d // 2)] = torch.from_numpy(code).view(-1).to(DEV)
+            at = eng.capacity * (d // 2) + o * (d // 32)
+            cache[at:at + n * (d // 32)] = torch.from_numpy(scale).view(-1).to(DEV)
+            src[b, h, name] = stored(x, 4)
+    q, kn, vn = (torch.randn(1, B, x, d, generator=g, device=DEV).to(torch.bfloat16) for x in (Hq, H, H))
+    out = torch.zeros(1, B, Hq, d, device=DEV)
+    acc = torch.zeros(eng.capacity, device=DEV)
+    slot, pos = torch.zeros(B * H, dtype=torch.int32, device=DEV), torch.full((B,), 5000, dtype=torch.int32, device=DEV)
+    say(f"large cache d={d}: append")
+    eng.decode_attn_weights(NL - 1, 1, q, kn, vn, out, acc, acc, slot_out=slot, pos=pos)
+    torch.cuda.synchronize()
+    for b, h in heads:
+        o, n = int(off[0, b, h]), int(lens[0, b, h])
+        k, v = (torch.cat([src[b, h, x], stored(t[0, b, h][None], 4)]) for x, t in (("k", kn), ("v", vn)))
+        ref, w = attention(q[0, b, h:h + 1], k, v, d)
+        assert float((out[0, b, h].cpu().double() - ref[0]).abs().max()) < 1e-4
+        assert float((acc[o:o + n + 1].cpu().double() - w[0]).abs().max()) < 5e-5
+        assert int(eng.kept_idx[o + n]) == 5000
+        src[b, h, "k"], src[b, h, "v"] = k, v
+    rows = [torch.zeros(eng.capacity, d, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    eng.cache_rows(NL - 1, 1, *rows)
+    torch.cuda.synchronize()
+    for b, h in heads:
+        o, n = int(off[0, b, h]), int(lens[0, b, h]) + 1
+        for x, t in zip("kv", rows):
+            assert torch.equal(t[o:o + n].cpu().double(), src[b, h, x])
+    eng.close()
