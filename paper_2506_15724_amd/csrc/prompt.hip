@@ -17,7 +17,9 @@
 // 16K tokens, 28 / 4 heads of 128 dims, both sweeps: 1.79 ms, 240 ns per tile and SIMD, 1.08 PFLOP/s of logits (a library product of
 // 16K x 16K x 16K bf16 runs at 1.36 on this card); 8K tokens, 32 heads, one sweep 0.27 ms.  Kept steps: address arithmetic per load -> a
 // buffer with fixed offsets 1.85 -> 1.80; a block's contraction between the vector instructions of the one before it 1.89 -> 1.85.
-// No gain: blocks of two and three waves per SIMD (1.87), heads in plain order instead of one XCD's (1.84).
+// No gain: blocks of two and three waves per SIMD (1.87), heads in plain order instead of one XCD's (1.84).  At 64 dims, half the
+// matrix instructions, the vector unit alone bounds it, and the registers leave room for three waves: 16K, 28 / 4 heads 1.22 ms,
+// 8K, 32 heads 0.376 (two waves 0.407, blocks of two and four waves 1.49 and 0.406, four waves with spills 1.38 and 0.437).
 // The rows come straight into LDS (16 bytes per lane, pieces of a row permuted so that operand reads do not collide), in a
 // ring of three tiles of 64 rows; LDS accesses and waits of the loop are written out, as in score.hip and for its reason.
 //
@@ -79,7 +81,7 @@ __device__ __forceinline__ void to_lds4(__amdgpu_buffer_rsrc_t b, uint32_t dst, 
 }
 
 template <int D, int NCB, int PASS>             // a wave's column blocks of 32
-__global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, NCB == 4 ? 2 : 4))) void prompt_sweep_kernel(PromptArgs a) {
+__global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(NCB == 4 && D == 64 ? 3 : 2, NCB == 4 ? (D == 64 ? 3 : 2) : 4))) void prompt_sweep_kernel(PromptArgs a) {
   constexpr int KS = D / 16;                    // MFMA steps over the head dimension
   constexpr int PPR = D / 8;                    // 16-byte pieces per row
   constexpr int ROWB = D * 2;
