@@ -71,10 +71,9 @@ __global__ __launch_bounds__(NW * 64) void decode_attn_kernel(DecodeArgs a) {
   const int r_end = min(len, r_begin + rows);
   const RowMap at = make_row_map<PAGED>(a, hidx, off, len_old, can_append, r_begin, r_end);
   const Fresh fresh = fresh_row<WEIGHTS>(a, hidx, len_old, can_append);
-  const bool has_fresh = fresh.there && fresh.row >= r_begin && fresh.row < r_end;   // uniform: the new row is in this piece
-  // (rows past an appended one are it once more, masked: no look at where the piece ends)
-  const auto is_fresh = [&](int r) { return WEIGHTS ? min(r, r_end - 1) == fresh.row : r >= len_old; };
-  if constexpr (ENCODE) { if (has_fresh) stage_new_row<D>(a, hidx, at(fresh.row), s_new); }
+  const int new_row = WEIGHTS ? fresh.row : len_old;
+  const bool has_fresh = (WEIGHTS ? fresh.there : can_append) && new_row >= r_begin && new_row < r_end;   // uniform: the new row is in this piece
+  if constexpr (ENCODE) { if (has_fresh) stage_new_row<D>(a, hidx, at(new_row), s_new); }
   // the NW waves take turns on consecutive RPI * UNROLL-row slices, so that at any moment the
   // workgroup reads one contiguous stretch of K and one of V
   constexpr int WSTEP = RPI * UNROLL;
@@ -105,7 +104,7 @@ __global__ __launch_bounds__(NW * 64) void decode_attn_kernel(DecodeArgs a) {
         kraw[u] = stream_load16(kc + o); vraw[u] = stream_load16(vc + o);
       }
     }
-    if (has_fresh && row0 <= fresh.row && fresh.row < row0 + WSTEP) {    // the new row (rows past an appended one are masked)
+    if (has_fresh && row0 <= new_row && new_row < row0 + WSTEP) {        // the new row (rows past an appended one are masked)
       uint4 knew, vnew;
       if constexpr (ENCODE) {
         knew = *reinterpret_cast<const uint4*>(s_new + piece * EPL);
@@ -114,14 +113,14 @@ __global__ __launch_bounds__(NW * 64) void decode_attn_kernel(DecodeArgs a) {
         knew = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.k_new) + hidx * D + piece * EPL);
         vnew = *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.v_new) + hidx * D + piece * EPL);
         if (sub == 0) {
-          const long long o = at(fresh.row) * D + piece * EPL;
+          const long long o = at(new_row) * D + piece * EPL;
           *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.k_c) + o) = knew;
           *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.v_c) + o) = vnew;
         }
       }
 #pragma unroll
       for (int u = 0; u < UNROLL; ++u)
-        if (is_fresh(row0 + u * RPI + sub)) { kraw[u] = knew; vraw[u] = vnew; }
+        if (WEIGHTS ? min(row0 + u * RPI + sub, r_end - 1) == new_row : row0 + u * RPI + sub >= len_old) { kraw[u] = knew; vraw[u] = vnew; }
     }
     if (row0 + WSTEP > r_end) {                                             // what is masked contributes 0 * 0
 #pragma unroll
