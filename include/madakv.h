@@ -122,8 +122,7 @@ typedef struct {
                               times 2^(b - 127), b the scale byte of its block of 32 dims: the least that leaves the largest
                               magnitude of the block at most 7, within 7 .. 252; elements are rounded to nearest even and
                               saturate at 6; infinities and NaN are taken for the largest finite bf16.  The row numbers
-                              in kv_off, kept_idx and the page table count rows as ever.  madakv_reevict is
-                              MADAKV_ERR_UNIMPLEMENTED for it. */
+                              in kv_off, kept_idx and the page table count rows as ever. */
   int32_t n_modalities;    /* M, 2 .. 4: modality ids in the mask are 0 .. M-1 (the paper has text = 0 and
                               image = 1; more modalities are the extension its Sec. 6 names) */
   int32_t page_rows;       /* 0 = every head's segment of the reduced cache is its kept rows followed by
@@ -365,7 +364,7 @@ int32_t madakv_cache_rows(madakv_handle* h, int32_t layer0, int32_t n, const voi
  *   budgets  [n, B, H, M]       out: the new split
  *   ws                          madakv_reevict_workspace_bytes(h, n) bytes
  * The decode-step counters of the layers are reset: max_new_tokens rows can be appended again.
- * An 8-bit cache is scored and moved as it is stored (E4M3 rows); MADAKV_ERR_UNIMPLEMENTED for a 4-bit one.  A paged cache is re-evicted as a whole
+ * An 8-bit or 4-bit cache is scored by the values it holds and moved as it is stored (4 bits: the workspace holds K as bf16).  A paged cache is re-evicted as a whole
  * (layer0 = 0, n = n_layers, else MADAKV_ERR_INVALID_ARG): the survivors end up in the heads' initial pages
  * and every page taken since the eviction goes back to the pools, which all layers share; the work is done
  * on a linear copy of the rows in the workspace (as many rows as the cache holds).

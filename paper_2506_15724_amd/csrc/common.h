@@ -49,6 +49,7 @@ struct Meet {
 // (and v_c) holds the codes of all rows, d / 2 bytes each, and behind those of capacity_tokens rows the scales, d / 32 bytes per row.
 constexpr int CACHE_E4M3 = 1, CACHE_E2M1 = 4;
 constexpr int MX_BLOCK = 32;             // dims that share a scale
+inline int cache_scale_bytes(const madakv_config& c) { return c.cache_fp8 == CACHE_E2M1 ? c.head_dim / MX_BLOCK : 0; }      // of a row
 inline int cache_row_bytes(const madakv_config& c) {       // of a row's elements (without scales)
   return c.cache_fp8 == CACHE_E2M1 ? c.head_dim / 2 : c.head_dim * (c.cache_fp8 == CACHE_E4M3 ? 1 : c.dtype == MADAKV_BF16 ? 2 : 4);
 }
@@ -108,7 +109,7 @@ hipError_t launch_restats(const Dims& dm, const madakv_config& c, const float* p
                           const int64_t* seg_off, const int32_t* seg_len, int appended, float* pool_c, uint8_t* rowmod,
                           void* stats, int32_t* budgets, hipStream_t st);
 hipError_t launch_compact(const Dims& dm, const madakv_config& c, void* k_c, void* v_c, int32_t* kept_idx, const int32_t* sel,
-                          const int64_t* seg_off, int32_t* kv_len, const int32_t* budgets, int appended, int gen_base, hipStream_t st);
+                          const int64_t* seg_off, int32_t* kv_len, const int32_t* budgets, long long cache_rows, int appended, int gen_base, hipStream_t st);
 hipError_t launch_linear_copy(const Dims& dm, const madakv_config& c, void* k_c, void* v_c, int32_t* kept_idx, const int64_t* seg_off,
                               const int32_t* seg_len, const Paging& pg, long long head0, int longest, void* k_lin, void* v_lin,
                               int32_t* kept_lin, int64_t* lin_off, bool back, hipStream_t st);
@@ -122,6 +123,7 @@ bool prompt_supported(const madakv_config& c);
 size_t prompt_ws_bytes(const Dims& dm);
 hipError_t launch_prompt(const Dims& dm, const madakv_config& c, const void* q, const void* k, const float* row_lse, float* psi,
                          void* ws, float factor, float** scaled, hipStream_t st);
+// v_rows null: K alone
 hipError_t launch_cache_rows(const Dims& dm, const madakv_config& c, const void* k_c, const void* v_c, const int64_t* kv_off, const int32_t* kv_len,
                              void* k_rows, void* v_rows, long long capacity_tokens, int longest_rows, const Paging& pg, int layer0, hipStream_t st);
 // A decode step that adds up the weights it pays (weights.hip).  The first seven are the caller's, the others point into the workspace.

@@ -216,13 +216,13 @@ __global__ __launch_bounds__(256) void cache_rows_kernel(RowsArgs a) {
     if (KIND == CACHE_E2M1) {
       const long long block = a.capacity * (LPR * 4) + at[it] * (LPR / 4) + piece / 4;          // of the scales
       const uint4 x = mx_decode8(reinterpret_cast<const uint32_t*>(a.k_c)[at[it] * LPR + piece], reinterpret_cast<const uint8_t*>(a.k_c)[block]);
-      const uint4 y = mx_decode8(reinterpret_cast<const uint32_t*>(a.v_c)[at[it] * LPR + piece], reinterpret_cast<const uint8_t*>(a.v_c)[block]);
-      kv[it] = __builtin_bit_cast(u32x4_t, x); vv[it] = __builtin_bit_cast(u32x4_t, y);
+      kv[it] = __builtin_bit_cast(u32x4_t, x);
+      if (a.v_rows) vv[it] = __builtin_bit_cast(u32x4_t, mx_decode8(reinterpret_cast<const uint32_t*>(a.v_c)[at[it] * LPR + piece], reinterpret_cast<const uint8_t*>(a.v_c)[block]));
     } else {
       typedef __attribute__((ext_vector_type(2))) unsigned int u32x2_t;
       typedef __attribute__((ext_vector_type(2))) float f32x2_t;
       const u32x2_t k8 = reinterpret_cast<const u32x2_t*>(a.k_c)[at[it] * LPR + piece];
-      const u32x2_t v8 = reinterpret_cast<const u32x2_t*>(a.v_c)[at[it] * LPR + piece];
+      const u32x2_t v8 = a.v_rows ? reinterpret_cast<const u32x2_t*>(a.v_c)[at[it] * LPR + piece] : u32x2_t{0u, 0u};
       // (every E4M3 value is a bf16: the upper half of the float is all there is of it)
       const auto pair = [](uint32_t w, bool high) {
         const f32x2_t f = high ? __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(256) void cache_rows_kernel(RowsArgs a) {
   for (int it = 0; it < ITERS; ++it) {
     if (r0 + it * RPI + sub < len) {
       __builtin_nontemporal_store(kv[it], a.k_rows + at[it] * LPR + piece);
-      __builtin_nontemporal_store(vv[it], a.v_rows + at[it] * LPR + piece);
+      if (a.v_rows) __builtin_nontemporal_store(vv[it], a.v_rows + at[it] * LPR + piece);
     }
   }
 }

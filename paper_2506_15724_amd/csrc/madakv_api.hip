@@ -733,7 +733,8 @@ namespace {
 // the per-head records of the call, the exchange array of the scoring kernel
 // (paged cache: the per-row arrays cover the linear copy of the heads' rows, which follows them: K, V, the
 // original positions, the heads' offsets in the copy; it has as many rows as the cache)
-struct ReevictWs { size_t psi, pool, sel, rowmod, stats, score, lin_k, lin_v, lin_idx, lin_off, total; };
+// (4-bit cache: the rows of K as bf16, for the scoring kernel, at the places they have in the cache or its copy)
+struct ReevictWs { size_t psi, pool, sel, rowmod, stats, score, lin_k, lin_v, lin_idx, lin_off, dec_k, total; };
 ReevictWs reevict_layout(const madakv_handle* h, int n) {
   const madakv_config& c = h->cfg;
   const Dims dm = make_dims(c, n);
@@ -744,10 +745,11 @@ ReevictWs reevict_layout(const madakv_handle* h, int n) {
   w.stats = w.rowmod + up(cap);
   w.score = w.stats + up((size_t)dm.heads * 8 * c.n_modalities);
   w.lin_k = w.score + up(score_ragged_ws_bytes(dm, c, c.ctx_len + c.max_new_tokens, (long long)cap));
-  const size_t row_bytes = (size_t)cache_row_bytes(c);
+  const size_t row_bytes = (size_t)(cache_row_bytes(c) + cache_scale_bytes(c));
   const size_t lin = c.page_rows ? up(cap * row_bytes) : 0;
   w.lin_v = w.lin_k + lin; w.lin_idx = w.lin_v + lin; w.lin_off = w.lin_idx + (c.page_rows ? up(cap * 4) : 0);
-  w.total = w.lin_off + (c.page_rows ? up((size_t)dm.heads * 8) : 0);
+  w.dec_k = w.lin_off + (c.page_rows ? up((size_t)dm.heads * 8) : 0);
+  w.total = w.dec_k + (c.cache_fp8 == CACHE_E2M1 ? up(cap * c.head_dim * 2) : 0);
   return w;
 }
 }  // namespace
@@ -767,7 +769,6 @@ int32_t madakv_reevict(madakv_handle* h, int32_t layer0, int32_t n,
   const madakv_config& c = h->cfg;
   if (bad_ptr(q_recent) || bad_ptr(mask, 1) || bad_ptr(k_c) || bad_ptr(v_c) || bad_ptr(kept_idx, 4) || bad_ptr(kv_off, 8) ||
       bad_ptr(kv_len, 4) || bad_ptr(budgets, 4) || bad_ptr(ws)) return MADAKV_ERR_INVALID_ARG;
-  if (c.cache_fp8 == CACHE_E2M1) return MADAKV_ERR_UNIMPLEMENTED;
   if (c.budget >= c.ctx_len) return MADAKV_ERR_BAD_BUDGET;                 // nothing was evicted, nothing to bring back
   for (int l = layer0; l < layer0 + n; ++l)
     if (h->replaced[l]) return MADAKV_ERR_INVALID_ARG;                     // the last rows of a segment are no longer the newest
@@ -810,11 +811,18 @@ int32_t madakv_reevict(madakv_handle* h, int32_t layer0, int32_t n,
     const char* qr = static_cast<const char*>(q_recent) + (size_t)(l0 - layer0) * c.batch * c.n_q_heads * c.window * c.head_dim * es;
     char* stats_r = wsb + w.stats + heads0 * 8 * c.n_modalities;
     int32_t* bud_r = budgets + heads0 * c.n_modalities;
-    e = launch_score_ragged(dr, c, qr, k_work, off_work + heads0, kv_len + heads0, longest, cache_rows, psi_c, wsb + w.score, st);
+    const void* k_score = k_work;
+    if (c.cache_fp8 == CACHE_E2M1) {
+      Paging flat = make_paging(h);
+      flat.page_rows = 0;
+      e = launch_cache_rows(dr, c, k_work, v_work, off_work + heads0, kv_len + heads0, wsb + w.dec_k, nullptr, cache_rows, longest, flat, 0, st);
+      k_score = wsb + w.dec_k;
+    }
+    if (e == hipSuccess) e = launch_score_ragged(dr, c, qr, k_score, off_work + heads0, kv_len + heads0, longest, cache_rows, psi_c, wsb + w.score, st);
     if (e == hipSuccess) e = launch_restats(dr, c, psi_c, idx_work, mask, off_work + heads0, kv_len + heads0, h->appended[l0], pool_c, rowmod,
                                             stats_r, bud_r, st);
     if (e == hipSuccess) e = launch_select(dr, c, pool_c, mask, bud_r, off_work + heads0, kv_len + heads0, sel, st, kv_len + heads0, rowmod);
-    if (e == hipSuccess) e = launch_compact(dr, c, k_work, v_work, idx_work, sel, off_work + heads0, kv_len + heads0, bud_r, h->appended[l0],
+    if (e == hipSuccess) e = launch_compact(dr, c, k_work, v_work, idx_work, sel, off_work + heads0, kv_len + heads0, bud_r, cache_rows, h->appended[l0],
                                             h->gen_base[l0], st);
     if (e == hipSuccess) for (int l = l0; l < l1; ++l) { h->gen_base[l] += h->appended[l]; h->appended[l] = 0; }
     l0 = l1;

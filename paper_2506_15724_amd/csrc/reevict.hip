@@ -19,6 +19,7 @@
 #include "common.h"
 
 #include <algorithm>
+#include <type_traits>
 #include "mpa_split.h"
 
 namespace madakv {
@@ -102,10 +103,11 @@ typedef __attribute__((ext_vector_type(4))) unsigned int ru32x4_t;
 
 struct CompactArgs {
   void* k_c; void* v_c; int32_t* kept_idx; const int32_t* sel; const int64_t* seg_off; int32_t* kv_len; const int32_t* budgets;
+  long long cache_rows;      // 4-bit cache: the scales are behind the codes of so many rows
   int W, M, L, appended, gen_base;
 };
 
-template <int LPR>   // 16-byte pieces per row
+template <int LPR, typename ST = void>   // 16-byte pieces per row; ST: the scales of a row of the 4-bit cache, as one word
 __global__ __launch_bounds__(RE_THREADS) void compact_kernel(CompactArgs a) {
   constexpr int RPI = RE_THREADS / LPR;          // rows the workgroup moves per instruction
   constexpr int UN = 4;
@@ -134,6 +136,7 @@ __global__ __launch_bounds__(RE_THREADS) void compact_kernel(CompactArgs a) {
   __syncthreads();
   for (int j0 = s_first; j0 < keep; j0 += BATCH) {
     ru32x4_t kr[UN], vr[UN];
+    uint32_t sr[UN];                              // (the scales of K by the first lane of a row, of V by the second)
     int org[UN];
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
@@ -141,6 +144,7 @@ __global__ __launch_bounds__(RE_THREADS) void compact_kernel(CompactArgs a) {
       const int src = j < keep ? a.sel[off + j] : 0;
       kr[u] = kc[(off + src) * LPR + piece];
       vr[u] = vc[(off + src) * LPR + piece];
+      if constexpr (!std::is_void_v<ST>) if (piece < 2) sr[u] = reinterpret_cast<const ST*>((piece ? vc : kc) + a.cache_rows * LPR)[off + src];
       // original position: prompt rows and earlier generated rows carry theirs; rows appended since the
       // last (re-)eviction are generated tokens gen_base, gen_base + 1, ... after the prompt
       org[u] = src < len0 ? a.kept_idx[off + src] : a.L + a.gen_base + (src - len0);
@@ -152,6 +156,7 @@ __global__ __launch_bounds__(RE_THREADS) void compact_kernel(CompactArgs a) {
       if (j < keep) {
         kc[(off + j) * LPR + piece] = kr[u];
         vc[(off + j) * LPR + piece] = vr[u];
+        if constexpr (!std::is_void_v<ST>) if (piece < 2) reinterpret_cast<ST*>((piece ? vc : kc) + a.cache_rows * LPR)[off + j] = (ST)sr[u];
         if (piece == 0) a.kept_idx[off + j] = org[u];
       }
     }
@@ -172,12 +177,17 @@ hipError_t launch_restats(const Dims& dm, const madakv_config& c, const float* p
 }
 
 hipError_t launch_compact(const Dims& dm, const madakv_config& c, void* k_c, void* v_c, int32_t* kept_idx, const int32_t* sel,
-                          const int64_t* seg_off, int32_t* kv_len, const int32_t* budgets, int appended, int gen_base, hipStream_t st) {
+                          const int64_t* seg_off, int32_t* kv_len, const int32_t* budgets, long long cache_rows, int appended, int gen_base, hipStream_t st) {
   CompactArgs a;
+  a.cache_rows = cache_rows;
   a.k_c = k_c; a.v_c = v_c; a.kept_idx = kept_idx; a.sel = sel; a.seg_off = seg_off; a.kv_len = kv_len; a.budgets = budgets;
   a.W = dm.W; a.M = c.n_modalities; a.L = dm.L; a.appended = appended; a.gen_base = gen_base;
   const int lpr = cache_row_bytes(c) / 16;     // 16-byte pieces per cached row
-  if (lpr == 4) hipLaunchKernelGGL((compact_kernel<4>), dim3(dm.heads), dim3(RE_THREADS), 0, st, a);
+  if (c.cache_fp8 == CACHE_E2M1) {
+    if (lpr == 4) hipLaunchKernelGGL((compact_kernel<4, uint32_t>), dim3(dm.heads), dim3(RE_THREADS), 0, st, a);
+    else hipLaunchKernelGGL((compact_kernel<2, uint16_t>), dim3(dm.heads), dim3(RE_THREADS), 0, st, a);
+  }
+  else if (lpr == 4) hipLaunchKernelGGL((compact_kernel<4>), dim3(dm.heads), dim3(RE_THREADS), 0, st, a);
   else if (lpr == 8) hipLaunchKernelGGL((compact_kernel<8>), dim3(dm.heads), dim3(RE_THREADS), 0, st, a);
   else if (lpr == 16) hipLaunchKernelGGL((compact_kernel<16>), dim3(dm.heads), dim3(RE_THREADS), 0, st, a);
   else if (lpr == 32) hipLaunchKernelGGL((compact_kernel<32>), dim3(dm.heads), dim3(RE_THREADS), 0, st, a);
@@ -200,6 +210,7 @@ struct LinearArgs {
   const int64_t* seg_off; const int32_t* seg_len; const int32_t* page_tbl;
   int entries, shift, lpr;                                  // table entries per head, log2(page rows), 16-byte pieces per row
   int heads;
+  int sb; long long cache_rows;                             // 4-bit cache: bytes of a row's scales, behind the codes of so many rows, in the copy as in the cache
 };
 constexpr int LIN_ROWS = 64;                                // rows per workgroup
 
@@ -223,6 +234,15 @@ __global__ __launch_bounds__(1024) void linear_offsets_kernel(LinearArgs a) {
   for (int h = h0; h < h1; ++h) { a.lin_off[h] = run; run += max(a.seg_len[h], 0); }
 }
 
+// the scales of row `src` of one cache to row `dst` of another (two or four bytes, or none)
+__device__ __forceinline__ void copy_scales(const LinearArgs& a, long long dst, ru32x4_t* k_to, ru32x4_t* v_to, long long src, const ru32x4_t* k_from, const ru32x4_t* v_from) {
+  const long long codes = a.cache_rows * a.lpr;
+  for (int i = 0; i < a.sb; ++i) {
+    reinterpret_cast<uint8_t*>(k_to + codes)[dst * a.sb + i] = reinterpret_cast<const uint8_t*>(k_from + codes)[src * a.sb + i];
+    reinterpret_cast<uint8_t*>(v_to + codes)[dst * a.sb + i] = reinterpret_cast<const uint8_t*>(v_from + codes)[src * a.sb + i];
+  }
+}
+
 __global__ __launch_bounds__(RE_THREADS) void linear_copy_kernel(LinearArgs a) {
   const int head = blockIdx.y, tid = threadIdx.x;
   const int len = a.seg_len[head];
@@ -240,6 +260,7 @@ __global__ __launch_bounds__(RE_THREADS) void linear_copy_kernel(LinearArgs a) {
     a.k_lin[dst * a.lpr + piece] = __builtin_nontemporal_load(a.k_c + src * a.lpr + piece);
     a.v_lin[dst * a.lpr + piece] = __builtin_nontemporal_load(a.v_c + src * a.lpr + piece);
     if (piece == 0) a.kept_lin[dst] = r < init_rows ? a.kept_idx[src] : 0;   // (rows in later pages are generated tokens: their positions are computed)
+    if (piece == 0) copy_scales(a, dst, a.k_lin, a.v_lin, src, a.k_c, a.v_c);
   }
 }
 
@@ -256,6 +277,7 @@ __global__ __launch_bounds__(RE_THREADS) void write_back_kernel(LinearArgs a) {
     a.k_c[dst * a.lpr + piece] = a.k_lin[src * a.lpr + piece];
     a.v_c[dst * a.lpr + piece] = a.v_lin[src * a.lpr + piece];
     if (piece == 0) a.kept_idx[dst] = a.kept_lin[src];
+    if (piece == 0) copy_scales(a, dst, a.k_c, a.v_c, src, a.k_lin, a.v_lin);
   }
 }
 
@@ -275,7 +297,7 @@ hipError_t launch_linear_copy(const Dims& dm, const madakv_config& c, void* k_c,
   a.seg_off = seg_off; a.seg_len = seg_len; a.page_tbl = pg.table + head0 * pg.entries;
   a.entries = pg.entries; a.shift = 0;
   while ((1 << a.shift) < pg.page_rows) ++a.shift;
-  a.lpr = cache_row_bytes(c) / 16;
+  a.lpr = cache_row_bytes(c) / 16; a.sb = cache_scale_bytes(c); a.cache_rows = pg.region_tokens * dm.B;
   a.heads = dm.heads;
   const dim3 grid((unsigned)((std::max(longest, 1) + LIN_ROWS - 1) / LIN_ROWS), dm.heads);
   if (back) {

@@ -2198,7 +2198,7 @@ hipError_t launch_score_ragged(const Dims& dm, const madakv_config& c, const voi
   a.mpad = fused_mpad(dm); a.nsplit = 0; a.nmerge = 0; a.chunk = 0; a.head0 = 0;
   a.fsplit = ragged_split(dm, longest_rows);
   a.xgroups = 0; a.xstride = (long long)a.fsplit * fused_mpad(dm);
-  a.k_kind = c.cache_fp8 ? K_E4M3 : K_BF16;       // the reduced cache is what is scored here
+  a.k_kind = c.cache_fp8 == CACHE_E4M3 ? K_E4M3 : K_BF16;       // the reduced cache is what is scored here
   const char* spin = getenv("MADAKV_SCORE_SPIN_LIMIT");
   a.spin_limit = spin && atoi(spin) > 0 ? atoi(spin) : FUSED_SPIN_LIMIT;
   const float scale = c.softmax_scale > 0.f ? c.softmax_scale : 1.0f / sqrtf((float)dm.d);

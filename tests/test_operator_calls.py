@@ -134,11 +134,16 @@ print("ok")
 
 
 def test_four_bit_cache_on_the_host(runtime):  # noqa: F811
-    """Eviction and decode take a 4-bit cache, re-eviction says that it does not; other widths and fp32 are refused."""
+    """Eviction, decode and re-eviction take a 4-bit cache (the last one reads K back first); other widths and fp32 are refused."""
     out = scenario(runtime, ARGS + """
 h = create(sys.argv[3])
 log()
-assert lib.madakv_reevict(h, I(0), I(2), *[P(T().p) for _ in range(8)], P(T().p), Z(1 << 40), P(0)) == -7 and not log()
+assert lib.madakv_reevict(h, I(0), I(2), *[P(T().p) for _ in range(8)], P(T().p), Z(1 << 40), P(0)) == 0
+k = [x for x in kinds() if x != "query"]
+assert "cache_rows" in k[0] and "score" in k[1], k
+b = Z()
+assert lib.madakv_reevict_workspace_bytes(h, I(2), C.byref(b)) == 0
+assert lib.madakv_reevict(h, I(0), I(2), *[P(T().p) for _ in range(8)], P(T().p), Z(b.value - 1), P(0)) == -4 and "launch" not in str(log())
 assert lib.madakv_evict(h, I(0), I(2), *[P(T().p) for _ in range(14)], P(T().p), Z(1 << 40), P(T().p), Z(1 << 40), P(0)) == 0
 log()
 assert lib.madakv_decode_attn(h, I(0), I(1), *[P(T().p) for _ in range(8)], P(T().p), Z(1 << 40), P(0)) == 0
