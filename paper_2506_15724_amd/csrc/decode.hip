@@ -374,9 +374,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NB > 1 
     const float m_new = FIRST ? tmax : fmaxf(m_run, tmax);
     float psum = 0.f;
     dbf16x8_t pb[NB];                                        // P as bf16 hi + lo of the lane's 4 keys: the B fragment
+    dbf16x8_t pc[NB];                                        // WEIGHTS: what the two parts leave of it, a third one (outputs of a few hundred rows 1e-6 -> 2e-7 off)
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      uint32_t hi[2], lo[2];
+      uint32_t hi[2], lo[2], third[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const df32x2_t pv = {weight_of(p[nb][2 * e] - m_new), weight_of(p[nb][2 * e + 1] - m_new)};
@@ -384,7 +385,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NB > 1 
         hi[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pv, dbf16x2_t));          // round to nearest even
         const df32x2_t rest = {pv[0] - bf16_lo(hi[e]), pv[1] - bf16_hi(hi[e])};
         lo[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, dbf16x2_t));
+        if constexpr (WEIGHTS) {
+          const df32x2_t left = {rest[0] - bf16_lo(lo[e]), rest[1] - bf16_hi(lo[e])};
+          third[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(left, dbf16x2_t));
+        }
       }
+      if constexpr (WEIGHTS) pc[nb] = __builtin_bit_cast(dbf16x8_t, du32x4_t{third[0], third[1], 0u, 0u});
       pb[nb] = __builtin_bit_cast(dbf16x8_t, du32x4_t{hi[0], hi[1], lo[0], lo[1]});
     }
     if (FIRST) {
@@ -413,6 +419,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NB > 1 
         const ds16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr_t)(vf + nb * 16 * RS + db * 16));
         const dbf16x8_t va = __builtin_bit_cast(dbf16x8_t, __builtin_shufflevector(v, v, 0, 1, 2, 3, 4, 5, 6, 7));
         oacc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[nb], FIRST && nb == 0 ? df32x4_t{0.f, 0.f, 0.f, 0.f} : oacc[db], 0, 0, 0);
+        if constexpr (WEIGHTS) oacc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pc[nb], oacc[db], 0, 0, 0);
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
