@@ -317,11 +317,16 @@ __global__ __launch_bounds__(256) void prompt_normaliser_kernel(PromptArgs a, co
     } else {
       const int last = r / (a.per_chunk * cb_rows);          // the chunk with the row's own key
       float m = -__builtin_inff(), s = 0.f;
-      for (int c = 0; c <= last; ++c) {
-        const float2 x = a.stat[(qh * a.chunks + c) * a.rows + r];
-        const float t = fmaxf(m, x.x);
-        s = (m == -__builtin_inff() ? 0.f : s * __builtin_amdgcn_exp2f(m - t)) + (x.x == -__builtin_inff() ? 0.f : x.y * __builtin_amdgcn_exp2f(x.x - t));
-        m = t;
+      for (int c0 = 0; c0 <= last; c0 += 4) {
+        float2 x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = c0 + u <= last ? a.stat[(qh * a.chunks + c0 + u) * a.rows + r] : make_float2(-__builtin_inff(), 0.f);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float t = fmaxf(m, x[u].x);
+          s = (m == -__builtin_inff() ? 0.f : s * __builtin_amdgcn_exp2f(m - t)) + (x[u].x == -__builtin_inff() ? 0.f : x[u].y * __builtin_amdgcn_exp2f(x[u].x - t));
+          m = t;
+        }
       }
       out = m + log2f(s);
     }
@@ -339,11 +344,15 @@ __global__ __launch_bounds__(256) void prompt_sum_kernel(PromptArgs a, int cb_ro
   if (a.chunks == 1 && a.G == 1) {
     s = a.psi[i];
   } else {
-    const int first = c / (a.per_chunk * cb_rows);           // the chunk with the key's own query
-    for (int g = 0; g < a.G; ++g) {
-      float sg = 0.f;
-      for (int k = first; k < a.chunks; ++k) sg += a.part[((kvh * a.G + g) * a.chunks + k) * a.rows + c];
-      s += sg;
+    // eight loads at a time: one behind the other, 28 terms per key took 16 us of a launch
+    const int first = c / (a.per_chunk * cb_rows), terms = a.G * a.chunks;           // the chunk with the key's own query
+    const float* p = a.part + kvh * terms * a.rows + c;
+    for (int j0 = 0; j0 < terms; j0 += 8) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = j0 + u < terms && (j0 + u) % a.chunks >= first ? p[(long long)(j0 + u) * a.rows] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += x[u];
     }
     a.psi[i] = s;
   }
