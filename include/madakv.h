@@ -34,8 +34,8 @@
  *     misaligned pointer gives MADAKV_ERR_INVALID_ARG; nothing is enqueued then.
  *   - All work is ordered on the caller's stream (a hipStream_t passed as void*, NULL = the
  *     null stream): it starts after what the stream held before the call and is complete, as far
- *     as the stream is concerned, before anything enqueued after it.  madakv_allocate
- *     and madakv_decode_attn enqueue on that stream only.  madakv_score, madakv_score_lse,
+ *     as the stream is concerned, before anything enqueued after it.  madakv_allocate,
+ *     madakv_score_prompt, madakv_cache_rows and the decode calls enqueue on that stream only.  madakv_score, madakv_score_lse,
  *     madakv_select_gather and madakv_evict over four or more layers also use the handle's own
  *     stream for the per-head statistics / selection kernels of one layer group while another
  *     group is scored or gathered; that stream forks from and joins the caller's stream through
@@ -310,7 +310,8 @@ int32_t madakv_decode_attn(madakv_handle* h, int32_t layer0, int32_t n,
  *   acc_in, acc_out [capacity_tokens] float, indexed like the rows of k_c (the same array, or two): for every row r of the
  *            heads in the call acc_out[r] = decay * acc_in[r] + the sum over the G query heads of the weight they pay to r
  *            in this step; of a row that is new in this step the weights alone.  Entries of other rows are left as they are.
- *            What acc_in holds at first is the caller's choice: zeros, or psi of the kept positions.
+ *            What acc_in holds at first is the caller's choice: zeros, or psi of the kept positions.  The sums stay where
+ *            they are when a (re-)eviction moves rows.
  *   decay    0 .. 1; 1 = the plain sum
  *   slot_in  [n, B, H] or NULL.  NULL: k_new, v_new are appended as in madakv_decode_attn (or NULL too: attend only).  Else:
  *            they replace row slot_in of the head's segment (0 .. kv_len - 1); the segment keeps its length.  A head whose

@@ -54,7 +54,7 @@ struct PromptArgs {
 };
 
 // item -> (column block, chunk).  Sweep 1: block cb (queries) against chunks 0 .. cb / per_chunk of the keys; sweep 2: block cb
-// (keys) against chunks cb / per_chunk .. of the queries.  Blocks with many chunks come first.
+// (keys) against chunks cb / per_chunk .. of the queries.
 template <int PASS>
 __device__ __forceinline__ void item_of(const PromptArgs& a, int i, int& cb, int& chunk) {
   int g = 0;                                    // which stretch of per_chunk blocks, the one with the most chunks first
