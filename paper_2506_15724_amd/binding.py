@@ -366,7 +366,11 @@ class MadaKV:
     def cache_rows(self, l0, n, k_rows, v_rows):
         for name, t in (("k_rows", k_rows), ("v_rows", v_rows)):
             self._check_array(name, t, self.capacity * self.cfg.head_dim, self.tdtype)
-        madakv_cache_rows(self.h, l0, n, self.k_c, self.v_c, self._sl(self.kv_off, l0, n), self._sl(self.kv_len, l0, n), k_rows, v_rows)
+        heads0 = l0 * self._heads
+        rc = lib().madakv_cache_rows(self.h, l0, n, _ptr(self.k_c), _ptr(self.v_c), _ptr(self.kv_off) + 8 * heads0, _ptr(self.kv_len) + 4 * heads0,
+                                     _ptr(k_rows), _ptr(v_rows), _stream())
+        if rc != OK:
+            raise MadaKVError("madakv_cache_rows", rc)
 
     def score_prompt(self, l0, n, q, k, mask=None, row_lse=None):
         """q [n, B, Hq, L, d].  Without a mask psi alone, with one the pooled scores, statistics and counts as well (as `score`)."""
