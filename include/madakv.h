@@ -233,6 +233,7 @@ int32_t madakv_window_attn_score(madakv_handle* h, int32_t layer0, int32_t n,
  * madakv_select_gather to go on with; they are those of psi * 2^-s, s the least with W * 2^s >= L, so that they have the
  * range that W proxy tokens give (budgets, counts and rankings do not depend on it).
  *   ws       madakv_score_prompt_workspace_bytes(h, n) bytes (enough for calls over fewer layers as well)
+ * A row's normaliser is one float: a weight is off by 2^-24 of the magnitude of its row's log-sum-exp, relative to the weight (1e-5 at 200).
  * MADAKV_ERR_UNIMPLEMENTED unless dtype is bf16. */
 int32_t madakv_score_prompt_workspace_bytes(const madakv_handle* h, int32_t n_layers_per_call, size_t* bytes);
 int32_t madakv_score_prompt(madakv_handle* h, int32_t layer0, int32_t n,
@@ -325,7 +326,8 @@ int32_t madakv_decode_attn(madakv_handle* h, int32_t layer0, int32_t n,
  *   recent   >= 0: the newest tokens that slot_out spares, the one of this step among them
  *   ws       madakv_decode_attn_weights_workspace_bytes(h, n) bytes
  * Once rows have been replaced, a segment is no longer in order of position: madakv_reevict gives
- * MADAKV_ERR_INVALID_ARG for its layer until the next eviction.  Nothing depends on the host from step to step: a
+ * MADAKV_ERR_INVALID_ARG for its layer until the next eviction, and for good once a replacing step has been captured, whose
+ * replays the host does not see.  Nothing depends on the host from step to step: a
  * captured replacing step can be replayed any number of times (pos is the caller's to advance on the device). */
 int32_t madakv_decode_attn_weights_workspace_bytes(const madakv_handle* h, int32_t n_layers_per_call, size_t* bytes);
 int32_t madakv_decode_attn_weights(madakv_handle* h, int32_t layer0, int32_t n,

@@ -21,7 +21,9 @@ struct madakv_handle {
   int32_t* d_page_tbl;             // paged cache: [n_layers * B * H][entries] page table (null otherwise)
   void* d_split; size_t split_bytes;   // long contexts: buffer of the chunk-parallel statistics / selection (null otherwise)
   std::vector<int32_t> appended;   // decode rows appended since the last (re-)eviction, per layer
-  std::vector<uint8_t> replaced;   // per layer: rows have taken the places of others since the last eviction, so that they are not in order of position
+  // per layer: rows have taken the places of others since the last eviction (1), or do so whenever a captured step is replayed
+  // (2, for good: nobody tells the host of replays), so that they are not in order of position
+  std::vector<uint8_t> replaced;
   std::vector<int32_t> gen_base;   // tokens generated before that, per layer (their original positions are ctx_len + 0, 1, ...)
   // Longest head of each layer after eviction: stored by the layout kernel in pinned host memory (d_maxlen is its
   // device address); decode sizes its grid from it once it is known to have landed
@@ -304,7 +306,10 @@ int32_t decode_impl(madakv_handle* h, int32_t layer0, int32_t n,
                                region_tokens(h->cfg) * h->cfg.batch, longest, make_paging(h), layer0,
                                reinterpret_cast<hipStream_t>(stream), w);
   if (e == hipSuccess && appends) for (int l = layer0; l < layer0 + n; ++l) h->appended[l] += 1;
-  if (e == hipSuccess && k_new && !appends) for (int l = layer0; l < layer0 + n; ++l) h->replaced[l] = 1;
+  if (e == hipSuccess && k_new && !appends) {
+    const uint8_t how = replayed_later(reinterpret_cast<hipStream_t>(stream)) ? 2 : 1;
+    for (int l = layer0; l < layer0 + n; ++l) h->replaced[l] |= how;
+  }
   if (e == hipSuccess && w) e = launch_row_weights(dm, h->cfg, *w, kv_off, kv_len, h->meet, longest, make_paging(h), layer0, reinterpret_cast<hipStream_t>(stream));
   return hip_fail(h, e);
 }
@@ -592,7 +597,7 @@ int32_t madakv_select_gather(madakv_handle* h, int32_t layer0, int32_t n,
     if (e == hipSuccess) e = launch_gather(dg, c, 0, ng, kg, vg, kept_idx, kv_off + heads0, kv_len + heads0, k_c, v_c, ws_g, region, bpb, bpb, st, overlap);
   }
   if (overlap && e != hipSuccess) e = join_side(h, st, e);   // an enqueue failed: whatever did reach the side stream is still joined
-  for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] = 0; h->gen_base[l] = 0; h->replaced[l] = 0; }
+  for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] = 0; h->gen_base[l] = 0; h->replaced[l] &= ~1; }
   e = publish_maxlen(h, layer0, n, st, e);
   return hip_fail(h, e);
 }
@@ -671,7 +676,7 @@ int32_t madakv_evict(madakv_handle* h, int32_t layer0, int32_t n,
   }
   if (e == hipSuccess) gather_group(ngroups - 1);
   if (overlap && e != hipSuccess) e = join_side(h, st, e);   // an enqueue failed: whatever did reach the side stream is still joined
-  for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] = 0; h->gen_base[l] = 0; h->replaced[l] = 0; }
+  for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] = 0; h->gen_base[l] = 0; h->replaced[l] &= ~1; }
   e = publish_maxlen(h, layer0, n, st, e);
   return hip_fail(h, e);
 }

@@ -38,7 +38,6 @@ typedef __attribute__((ext_vector_type(4))) float pf32x4_t;
 typedef __attribute__((address_space(3))) void* plds_ptr_t;
 
 constexpr int PR_WAVES = 4, PR_TILE = 64, PR_RING = 3;
-constexpr float PR_UNSEEN = -1.0e30f;           // a masked logit, in accumulator units
 constexpr float PR_FAR = 0x1p60f;               // sums beyond it have left their references behind
 
 struct PromptArgs {
@@ -167,7 +166,7 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(N
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
       const int row = 8 * (j >> 2) + 4 * half + (j & 3);
-      x[j] = (PASS == 1 ? row <= col : row >= col) ? x[j] : PR_UNSEEN;
+      x[j] = (PASS == 1 ? row <= col : row >= col) ? x[j] : -__builtin_inff();
     }
     return x;
   };
@@ -185,7 +184,7 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(N
 #pragma unroll
     for (int j = 1; j < 16; ++j) top = fmaxf(top, x[j]);
     if (!(sum[b] + s < 0.25f * PR_FAR)) {       // (also: no number)
-      if (top > 0.5f * PR_UNSEEN) {
+      if (top > -__builtin_inff()) {
         const float r = fmaxf(sum[b] < 0x1p50f ? ref[b] : ref[b] + 50.f, top * a.scale_log2);
         sum[b] = ref[b] == -__builtin_inff() ? 0.f : sum[b] * __builtin_amdgcn_exp2f(ref[b] - r);
         ref[b] = r;

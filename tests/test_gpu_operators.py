@@ -531,6 +531,28 @@ def test_prompt_scores_far_from_the_first_keys(Hq, L, at, top):
     eng.close()
 
 
+@pytest.mark.parametrize("Hq,H,d,L", [(2, 2, 128, 300), (64, 64, 64, 1100)])
+def test_prompt_scores_of_tiny_and_huge_logits(Hq, H, d, L):
+    """A scale under which no logit is anything: a query pays 1 / (r + 1) to each key it sees and nothing to the others.  And q . k down to
+    -2e32 under a scale that makes -16 .. -176 of it (one element each, powers of two times 1 .. 11): 176 log2(e) * 2^-24 in
+    the weight, in the normaliser and in the scale itself make 3 * 1.1e-5; sums of 1100 terms 1100 * 2^-24 / 2 = 3.3e-5."""
+    say(f"prompt tiny and huge {Hq}/{H} d={d} L={L}")
+    eng, q, k = prompt_case(1, 1, Hq, H, d, L, softmax_scale=1e-33)
+    eng.score_prompt(0, 1, q, k)
+    want = (1.0 / torch.arange(1, L + 1, device=DEV, dtype=torch.float64)).flip(0).cumsum(0).flip(0)
+    assert float((eng.psi[0, 0].double() / want - 1).abs().max()) < 7e-5
+    eng.close()
+    eng, q, k = prompt_case(1, 1, Hq, H, d, L, softmax_scale=2.0 ** -100)
+    level = 1 + torch.arange(L - 1, -1, -1, device=DEV) // 100
+    q.zero_(), k.zero_()
+    q[..., 0], k[..., 0] = 2.0 ** 52, (-level * 2.0 ** 52).to(torch.bfloat16)
+    eng.score_prompt(0, 1, q, k)
+    s = (-16.0 * level.double()).expand(L, L).masked_fill(~torch.ones(L, L, dtype=torch.bool, device=DEV).tril_(), -math.inf)
+    want = torch.softmax(s, -1).sum(0)
+    assert float(((eng.psi[0, 0].double() - want).abs() / (want + 1e-8)).max()) < 7e-5
+    eng.close()
+
+
 def test_prompt_scores_with_statistics():
     """The pooled scores, masses, counts and candidates that go with them, and what allocation and selection make of those: the same
     as the statistics of the scores times the power of two, by the oracle."""

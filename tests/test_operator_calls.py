@@ -155,3 +155,21 @@ print("ok")
     for kw, status in ((dict(cache_fp8=3), -1), (dict(cache_fp8=5), -1), (dict(cache_fp8=-1), -1), (dict(cache_fp8=4, dtype=MB.FP32, head_dim=64, window=16), -5)):
         h = C.c_void_p()
         assert MB.lib().madakv_create(C.byref(good(**kw)), C.byref(h)) == status and not h.value
+
+
+def test_rows_replaced_by_replays_are_not_reevicted(runtime):  # noqa: F811
+    """A captured replacing step replaces rows whenever its graph is replayed, also behind a later eviction."""
+    out = scenario(runtime, ARGS + """
+h = create(sys.argv[3])
+st = 0x7000
+re = lambda l, n: lib.madakv_reevict(h, I(l), I(n), *[P(T().p) for _ in range(8)], P(T().p), Z(1 << 40), P(0))
+fake.fake_capture(P(st))
+assert weights(h, l0=0, st=st) == 0                     # (appends: the layer can be re-evicted)
+assert weights(h, l0=1, s0=1, st=st) == 0
+fake.fake_capture(P(0))
+assert re(0, 1) == 0 and re(1, 1) == -1
+assert lib.madakv_select_gather(h, I(0), I(2), *[P(T().p) for _ in range(10)], P(T().p), Z(1 << 40), P(0)) == 0
+assert re(0, 1) == 0 and re(1, 1) == -1 and re(0, 2) == -1
+print("ok")
+""", good())
+    assert out.strip() == "ok"
