@@ -28,15 +28,15 @@ template <int GT, bool PAGED>
 __global__ __launch_bounds__(RW_THREADS) void row_weights_kernel(RowWeightArgs a) {
   const int hidx = blockIdx.x, chunk = blockIdx.y, tid = threadIdx.x;
   const WeightArgs& w = a.w;
-  const int len = a.kv_len[hidx];
-  const int chunks = max(1, min((int)gridDim.y, (len + RW_ROWS - 1) / RW_ROWS));
-  if (chunk >= chunks) return;
   const long long off = a.kv_off[hidx], head = a.head0 + hidx;
-  const int fresh = w.fresh[hidx];
+  const int len = a.kv_len[hidx], fresh = w.fresh[hidx];
   const int pos = w.pos ? w.pos[(head / a.H) % a.B] : 0;
-  const long long newest = (long long)pos - w.recent;              // positions up to this one may go
   const int32_t* tbl = PAGED ? a.page_tbl + head * a.tbl_entries : nullptr;
   const int init_rows = PAGED ? tbl[0] << a.page_shift : 0x7fffffff;
+  asm volatile("" :: "s"(len), "s"((int)off), "s"(fresh), "s"(pos), "s"(init_rows));         // (all of them in one trip)
+  const int chunks = max(1, min((int)gridDim.y, (len + RW_ROWS - 1) / RW_ROWS));
+  if (chunk >= chunks) return;
+  const long long newest = (long long)pos - w.recent;              // positions up to this one may go
   float mx[GT], inv[GT];
 #pragma unroll
   for (int g = 0; g < GT; ++g) {
