@@ -153,8 +153,8 @@ def test_fp8_rows_out(d):
 @pytest.mark.parametrize("out_fp32", [1, 0])
 def test_fp4_decode(Hq, H, d, L, lens, out_fp32):
     """Attention over the rows as they are stored, appended ones among them.  Outputs are means of rows of N(0, 1) values in 4 bits;
-    products of codes and bf16 are exact, sums of <= 128 of them in fp32 leave 1e-5 on a logit (|logit| < 8), P as two bf16 parts
-    2^-17: 1e-4 covers both; a bf16 output is rounded to 8 significant bits, half a unit of the last being at most 2^-8 of the value."""
+    products of codes and bf16 are exact, sums of <= 128 of them in fp32 leave 1e-5 on a logit (|logit| < 8), P as three bf16
+    parts next to nothing: 1e-4 covers both; a bf16 output is rounded to 8 significant bits, half a unit of the last being at most 2^-8 of the value."""
     eng, args, *_ = make(lens, n_q_heads=Hq, n_kv_heads=H, head_dim=d, ctx_len=L, cache_fp8=4, out_fp32=out_fp32)
     g = torch.Generator().manual_seed(3)
     G, worst = Hq // H, 0.0
