@@ -14,7 +14,7 @@
 // instructions: sweep 1 looks for no maximum, but sums against the reference of the first tile and takes another
 // one when a sum passes 2^60 (a tile is then formed again); rows that no column of a wave sees are left out and the causal mask is
 // applied in diagonal tiles only; four blocks of columns share each operand read from LDS; a lane's offset in a tile is the same for all tiles.
-// 16K tokens, 28 / 4 heads of 128 dims, both sweeps: 1.79 ms, 240 ns per tile and SIMD, 1.08 PFLOP/s of logits (a library product of
+// 16K tokens, 28 / 4 heads of 128 dims, both sweeps: 1.76-1.81 ms, 240 ns per tile and SIMD, 1.08 PFLOP/s of logits (a library product of
 // 16K x 16K x 16K bf16 runs at 1.36 on this card); 8K tokens, 32 heads, one sweep 0.27 ms.  Kept steps: address arithmetic per load -> a
 // buffer with fixed offsets 1.85 -> 1.80; a block's contraction between the vector instructions of the one before it 1.89 -> 1.85.
 // No gain: blocks of two and three waves per SIMD (1.87), heads in plain order instead of one XCD's (1.84).  At 64 dims, half the
