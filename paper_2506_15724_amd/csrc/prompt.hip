@@ -303,6 +303,122 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(N
   }
 }
 
+// Prompts of up to PR_SHORT positions: one launch, a workgroup per query head, which has all keys in LDS and every wave a block of
+// 32 queries.  A wave keeps its logits (keys x queries, up to 8 tiles of 32 x 32) in registers, so that each is formed once: maximum
+// and sum of a query's column are the lane's own and the other half's, its weights follow, and a key's weights are added up over
+// the 32 lanes that have its row, 16 keys at a time: exchanges in which a lane sends half of what it has left and keeps the other.
+// Waves w and w + 4 share a SIMD and take blocks whose keys add up to the same.
+constexpr int PR_SHORT = 256, PR_SHORT_WAVES = PR_SHORT / 32;
+
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float x) { return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xF, 0xF, true)); }
+// N values of a lane and N of its partner -> N / 2 sums: the upper ones where `high`
+template <int CTRL, int N>
+__device__ __forceinline__ void halve(float (&v)[16], bool high) {
+#pragma unroll
+  for (int j = 0; j < N / 2; ++j) {
+    const float keep = high ? v[j + N / 2] : v[j], send = high ? v[j] : v[j + N / 2];
+    v[j] = keep + from_lane<CTRL>(send);
+  }
+}
+
+// What a wave's 32 queries (breg; a lane's is `col` of block `mine`) pay to each of the first 32 NT keys, to sums.  NT: mine + 1 or one
+// more.  GIVEN: `norm` is the log2 of the query's normaliser.
+template <int D, int NT, bool GIVEN>
+__device__ __forceinline__ void short_block(const unsigned char* keys, const pbf16x8_t (&breg)[D / 16], int mine, bool there, float norm, float scale_log2, float* sums) {
+  constexpr int KS = D / 16, PPR = D / 8, ROWB = D * 2;
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+  pf32x16_t x[NT];
+  float top = -__builtin_inff();
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    pbf16x8_t areg[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) areg[ks] = *reinterpret_cast<const pbf16x8_t*>(keys + (i * 32 + col) * ROWB + ((half * KS + ks) ^ (col % PPR)) * 16);
+    x[i] = pf32x16_t{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) x[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(areg[ks], breg[ks], x[i], 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      if (i >= NT - 2) x[i][j] = (i - mine) * 32 + 8 * (j >> 2) + 4 * half + (j & 3) <= col ? x[i][j] : -__builtin_inff();
+      if (!GIVEN) top = fmaxf(top, x[i][j]);
+    }
+    __builtin_amdgcn_sched_barrier(0);          // (operands of one tile at a time: all of them do not fit)
+  }
+  float share = 1.f;
+  if (GIVEN) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) x[i][j] = __builtin_amdgcn_exp2f(fmaf(x[i][j], scale_log2, -norm));
+  } else {
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        x[i][j] = __builtin_amdgcn_exp2f((x[i][j] - top) * scale_log2);
+        s[j & 3] += x[i][j];
+      }
+    const float sum = (s[0] + s[1]) + (s[2] + s[3]);
+    share = there ? 1.f / (sum + __shfl_xor(sum, 32, 64)) : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    float v[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = GIVEN ? x[i][j] : x[i][j] * share;
+    halve<0x128, 16>(v, lane & 8);              // row_ror 8: lane ^ 8
+    halve<0x141, 8>(v, lane & 4);               // row_half_mirror: lane ^ 7
+    halve<0x4E, 4>(v, lane & 2);                // quad_perm [2,3,0,1]: lane ^ 2
+    halve<0xB1, 2>(v, lane & 1);                // quad_perm [1,0,3,2]: lane ^ 1
+    const float s = v[0] + __shfl_xor(v[0], 16, 64);              // lane j has row j of its half
+    const int j = lane & 15;
+    if ((lane & 16) == 0) sums[i * 32 + 8 * (j >> 2) + 4 * half + (j & 3)] = s;
+  }
+}
+
+template <int D, bool GIVEN>
+__global__ __launch_bounds__(PR_SHORT_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_short_kernel(PromptArgs a, const float* row_lse, float* scaled, float factor) {
+  constexpr int KS = D / 16, PPR = D / 8, ROWB = D * 2;
+  __shared__ __attribute__((aligned(16))) unsigned char s_keys[PR_SHORT * ROWB];
+  __shared__ float s_sums[PR_SHORT_WAVES * PR_SHORT];        // what every block of queries pays to the keys
+  const int qh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, col = lane & 31;
+  const int nb = (a.L + 31) / 32, mine = wave < PR_SHORT_WAVES / 2 ? wave : PR_SHORT_WAVES * 3 / 2 - 1 - wave;
+  const unsigned char* qrows = reinterpret_cast<const unsigned char*>(a.q) + (long long)qh * a.L * ROWB;
+  const unsigned char* krows = reinterpret_cast<const unsigned char*>(a.k) + (long long)(qh / a.G) * a.L * ROWB;
+  // keys as the sweeps have them in LDS; rows past the prompt's end are zeros
+  const __amdgpu_buffer_rsrc_t keys_buf = buffer_of(krows, a.L * ROWB);
+  for (int i = wave; i < nb * (32 * ROWB / 1024); i += PR_SHORT_WAVES) {
+    const int piece = i * 64 + lane, row = piece / PPR;
+    to_lds16(keys_buf, (uint32_t)(uintptr_t)(plds_ptr_t)s_keys + (uint32_t)i * 1024u, row * ROWB + ((piece % PPR) ^ (row % PPR)) * 16, 0);
+  }
+  const int query = mine * 32 + col;
+  const bool there = query < a.L;
+  pbf16x8_t breg[KS];
+  const unsigned char* src = qrows + (long long)min(query, a.L - 1) * ROWB + half * D;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) breg[ks] = *reinterpret_cast<const pbf16x8_t*>(src + ks * 16);
+  const float norm = GIVEN && there ? row_lse[(long long)qh * a.L + query] * 1.4426950408889634f : __builtin_inff();
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  float* sums = s_sums + mine * PR_SHORT;
+  if (mine < nb) {                              // (a tile behind the wave's own is masked, whatever is there)
+    if (mine >= 6) short_block<D, 8, GIVEN>(s_keys, breg, mine, there, norm, a.scale_log2, sums);
+    else if (mine >= 4) short_block<D, 6, GIVEN>(s_keys, breg, mine, there, norm, a.scale_log2, sums);
+    else if (mine >= 2) short_block<D, 4, GIVEN>(s_keys, breg, mine, there, norm, a.scale_log2, sums);
+    else short_block<D, 2, GIVEN>(s_keys, breg, mine, there, norm, a.scale_log2, sums);
+  }
+  __syncthreads();
+  if (tid >= a.L) return;
+  float s = 0.f;
+  for (int b = tid / 32; b < nb; ++b) s += s_sums[b * PR_SHORT + tid];
+  if (a.G > 1) { a.part[(long long)qh * a.rows + tid] = s; return; }
+  a.psi[(long long)qh * a.L + tid] = s;
+  if (scaled) scaled[(long long)qh * a.L + tid] = s * factor;
+}
+
 // log2 of the rows' normalisers: from the chunks' (maximum, sum), or from the caller's natural logarithms
 __global__ __launch_bounds__(256) void prompt_normaliser_kernel(PromptArgs a, const float* row_lse, int cb_rows, long long n) {
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -399,6 +515,18 @@ size_t prompt_ws_bytes(const Dims& dm) {
   return up256(qheads * rows_of(dm) * 4) + up256(qheads * p.chunks * rows_of(dm) * 8) + up256((size_t)dm.heads * dm.L * 4);
 }
 
+template <int D>
+static hipError_t launch_short(const Dims& dm, const PromptArgs& a, const float* row_lse, float* scaled, float factor, hipStream_t st) {
+  const dim3 grid((unsigned)(dm.n * dm.B * dm.Hq)), block(PR_SHORT_WAVES * 64);
+  if (row_lse) hipLaunchKernelGGL((prompt_short_kernel<D, true>), grid, block, 0, st, a, row_lse, scaled, factor);
+  else hipLaunchKernelGGL((prompt_short_kernel<D, false>), grid, block, 0, st, a, row_lse, scaled, factor);
+  if (a.G == 1) return hipGetLastError();
+  if (hipError_t e = hipGetLastError()) return e;
+  const long long npsi = (long long)dm.heads * dm.L;
+  hipLaunchKernelGGL(prompt_sum_kernel, dim3((unsigned)((npsi + 255) / 256)), dim3(256), 0, st, a, PR_SHORT, scaled, factor, npsi);
+  return hipGetLastError();
+}
+
 template <int D, int NCB>
 static hipError_t launch_sweeps(const Dims& dm, const PromptPlan& p, PromptArgs& a, const float* row_lse, float* scaled, float factor, hipStream_t st) {
   constexpr int CB = PR_WAVES * NCB * 32;
@@ -441,6 +569,10 @@ hipError_t launch_prompt(const Dims& dm, const madakv_config& c, const void* q, 
   if (scaled) *scaled = s = reinterpret_cast<float*>(w);
   a.per_chunk = p.per_chunk; a.chunks = p.chunks; a.blocks = p.blocks;
   a.scale_log2 = (c.softmax_scale > 0.f ? c.softmax_scale : 1.0f / sqrtf((float)dm.d)) * 1.4426950408889634f;
+  if (dm.L <= PR_SHORT) {
+    a.per_chunk = a.chunks = 1;
+    return dm.d == 128 ? launch_short<128>(dm, a, row_lse, s, factor, st) : launch_short<64>(dm, a, row_lse, s, factor, st);
+  }
   if (dm.d == 128) return p.ncb == 4 ? launch_sweeps<128, 4>(dm, p, a, row_lse, s, factor, st) : launch_sweeps<128, 1>(dm, p, a, row_lse, s, factor, st);
   return p.ncb == 4 ? launch_sweeps<64, 4>(dm, p, a, row_lse, s, factor, st) : launch_sweeps<64, 1>(dm, p, a, row_lse, s, factor, st);
 }

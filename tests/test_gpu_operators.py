@@ -516,6 +516,17 @@ def test_prompt_scores_of_large_calls(NL, B, Hq, H, d, L, given):
     eng.close()
 
 
+@pytest.mark.parametrize("NL,B,Hq,H,d", [(2, 3, 4, 4, 128), (1, 2, 28, 4, 128), (3, 1, 6, 2, 64), (4, 16, 16, 8, 64)])
+@pytest.mark.parametrize("L", [17, 96, 160, 192, 203, 224, 256])
+@pytest.mark.parametrize("given", [False, True])
+def test_prompt_scores_of_short_prompts(NL, B, Hq, H, d, L, given):
+    """Prompts whose logits stay in registers: every number of blocks of 32 queries, full and ragged, layers and batch items."""
+    eng, q, k = prompt_case(NL, B, Hq, H, d, L)
+    say(f"prompt {NL} x {B} x {Hq}/{H} d={d} L={L} lse={given}")
+    check_prompt(eng, q, k, given)
+    eng.close()
+
+
 @pytest.mark.parametrize("top", [90.0, 400.0, -400.0])
 @pytest.mark.parametrize("Hq,L,at", [(2, 700, 300), (64, 1100, 520), (2, 130, 96)])
 def test_prompt_scores_far_from_the_first_keys(Hq, L, at, top):
