@@ -246,7 +246,7 @@ class MadaKV:
         with torch.cuda.device(self.device):
             self.h = madakv_create(self.cfg)
         self._out_dtype = torch.float32 if out_fp32 else self.tdtype
-        self._out_row, self._heads = batch * n_q_heads * head_dim, batch * n_kv_heads
+        self._out_row, self._heads, self._kv_row, self._ctx = batch * n_q_heads * head_dim, batch * n_kv_heads, batch * n_kv_heads * head_dim, ctx_len
         self.n_call = layers_per_call or n_layers
         s_ws, sel_ws, d_ws = madakv_workspace_bytes(self.h, self.n_call)
         d1 = madakv_workspace_bytes(self.h, 1)[2]
@@ -340,6 +340,13 @@ class MadaKV:
         if t is not None and (t.dtype != dtype or t.numel() < numel or t.device != self._device):
             raise ValueError(f"{name} must hold {numel} elements of {dtype} on {self._device}; got {t.numel()} of {t.dtype} on {t.device}")
 
+    def _own_stream(self):
+        """The current stream, where the current device is the handle's: kernels for another one would not find the buffers."""
+        d = torch.cuda.current_device()
+        if d != self._device.index:
+            raise ValueError(f"the handle is on {self._device}, the current device is cuda:{d}")
+        return _raw_stream(d)
+
     def decode_attn_weights(self, l0, n, q, k_new, v_new, out, acc_in, acc_out, decay=1.0, slot_in=None, slot_out=None, pos=None, recent=0):
         """kept_idx is the holder's own, kept up where the tokens' positions `pos` are given."""
         # (once per layer and token, like decode_attn: no views of the own buffers)
@@ -359,7 +366,7 @@ class MadaKV:
         rc = lib().madakv_decode_attn_weights(
             self.h, l0, n, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(self.k_c), _ptr(self.v_c), _ptr(self.kv_off) + 8 * heads0, _ptr(self.kv_len) + 4 * heads0,
             _ptr(out), _ptr(acc_in), _ptr(acc_out), decay, _ptr(slot_in), _ptr(slot_out), None if pos is None else _ptr(self.kept_idx), _ptr(pos), recent,
-            _ptr(ws), ws.numel() * ws.element_size(), _stream())
+            _ptr(ws), ws.numel(), self._own_stream())
         if rc != OK:
             raise MadaKVError("madakv_decode_attn_weights", rc)
 
@@ -368,21 +375,29 @@ class MadaKV:
             self._check_array(name, t, self.capacity * self.cfg.head_dim, self.tdtype)
         heads0 = l0 * self._heads
         rc = lib().madakv_cache_rows(self.h, l0, n, _ptr(self.k_c), _ptr(self.v_c), _ptr(self.kv_off) + 8 * heads0, _ptr(self.kv_len) + 4 * heads0,
-                                     _ptr(k_rows), _ptr(v_rows), _stream())
+                                     _ptr(k_rows), _ptr(v_rows), self._own_stream())
         if rc != OK:
             raise MadaKVError("madakv_cache_rows", rc)
 
     def score_prompt(self, l0, n, q, k, mask=None, row_lse=None):
         """q [n, B, Hq, L, d].  Without a mask psi alone, with one the pooled scores, statistics and counts as well (as `score`)."""
-        c = self.cfg
-        self._check_array("q", q, n * c.batch * c.n_q_heads * c.ctx_len * c.head_dim, self.tdtype)
-        self._check_array("k", k, n * self._heads * c.ctx_len * c.head_dim, self.tdtype)
-        self._check_array("mask", mask, c.batch * c.ctx_len, torch.uint8)
-        self._check_array("row_lse", row_lse, n * c.batch * c.n_q_heads * c.ctx_len, torch.float32)
+        # (a prompt of a few hundred tokens takes 7 us on the device: no views of the own buffers)
+        L = self._ctx
+        self._check_array("q", q, n * self._out_row * L, self.tdtype)
+        self._check_array("k", k, n * self._kv_row * L, self.tdtype)
+        if row_lse is not None:
+            self._check_array("row_lse", row_lse, n * self.cfg.batch * self.cfg.n_q_heads * L, torch.float32)
+        pool = stats = n_mod = None
+        if mask is not None:
+            self._check_array("mask", mask, self.cfg.batch * L, torch.uint8)
+            pool, stats, n_mod = _ptr(self._sl(self.psi_pool, l0, n)), _ptr(self._sl(self.stats, l0, n)), _ptr(self.n_mod)
         if getattr(self, "prompt_ws", None) is None:
             self.prompt_ws = torch.empty(max(16, madakv_score_prompt_workspace_bytes(self.h, self.n_call)), dtype=torch.uint8, device=self.device)
-        rest = (None,) * 3 if mask is None else (self._sl(self.psi_pool, l0, n), self._sl(self.stats, l0, n), self.n_mod)
-        madakv_score_prompt(self.h, l0, n, q, k, mask, row_lse, self._sl(self.psi, l0, n), *rest, self.prompt_ws)
+        ws = self.prompt_ws
+        rc = lib().madakv_score_prompt(self.h, l0, n, _ptr(q), _ptr(k), _ptr(mask), _ptr(row_lse), _ptr(self.psi) + 4 * l0 * self._heads * L, pool, stats, n_mod,
+                                       _ptr(ws), ws.numel(), self._own_stream())
+        if rc != OK:
+            raise MadaKVError("madakv_score_prompt", rc)
 
     def window_attn_score(self, l0, n, q_win, k, v, mask, out, row_lse=None):
         self._check_out(out, n * self.cfg.batch * self.cfg.n_q_heads * self.cfg.window * self.cfg.head_dim)

@@ -598,6 +598,56 @@ def test_prompt_scores_with_statistics():
     eng.close()
 
 
+def test_statistics_of_short_prompts():
+    """One query head per KV head (the kernel of short prompts writes the scaled scores itself) and four: psi with statistics is psi
+    without, the pooled scores are those of psi times the power of two."""
+    for NL, B, Hq, H, d, L, W, s in ((2, 3, 2, 2, 64, 200, 16, 4), (1, 2, 8, 2, 128, 256, 32, 3), (2, 1, 3, 3, 128, 40, 32, 1)):
+        eng, q, k = prompt_case(NL, B, Hq, H, d, L, W=W, pool_k=3)
+        mask = torch.randint(0, 2, (B, L), generator=torch.Generator().manual_seed(4)).to(DEV, torch.uint8)
+        eng.score_prompt(0, NL, q, k)
+        torch.cuda.synchronize()
+        psi = eng.psi.clone()
+        eng.psi.fill_(-1.0)
+        eng.score_prompt(0, NL, q, k, mask=mask)
+        torch.cuda.synchronize()
+        assert torch.equal(eng.psi, psi)
+        for l in range(NL):
+            for b in range(B):
+                want = O.pool_scores(psi[l, b].cpu().double().numpy() * 2.0 ** -s, W, 3)
+                np.testing.assert_array_equal(eng.psi_pool[l, b].cpu().double().numpy(), want)
+        eng.close()
+
+
+def test_arrays_and_devices_that_do_not_fit(monkeypatch):
+    """What the holder refuses before the library is called: arrays of another type, size or device, and a current device that is
+    not the handle's."""
+    eng, q, k = prompt_case(1, 2, 4, 2, 64, 64, W=8, cache_fp8=4)
+    cap, f32, i32 = eng.capacity, torch.float32, torch.int32
+    out = torch.empty(1, 2, 4, 64, device=DEV)
+    acc = torch.zeros(cap, device=DEV)
+    rows = torch.empty(cap, 64, dtype=torch.bfloat16, device=DEV)
+    short, host = acc[:-1], acc.cpu()
+    step = lambda **kw: eng.decode_attn_weights(0, 1, *[kw.pop(x, y) for x, y in (("q", out[..., :64].bfloat16()), ("kn", None), ("vn", None), ("out", out), ("a", acc), ("b", acc))], **kw)      # noqa: E731
+    bad = [lambda: step(a=short), lambda: step(b=short), lambda: step(a=host), lambda: step(b=acc.double()), lambda: step(out=out.bfloat16()), lambda: step(out=out[:, :1].contiguous()),
+           lambda: step(slot_in=torch.zeros(3, dtype=i32, device=DEV)), lambda: step(slot_out=torch.zeros(4, dtype=f32, device=DEV)), lambda: step(pos=torch.zeros(1, dtype=i32, device=DEV)),
+           lambda: eng.cache_rows(0, 1, rows[:-1], rows), lambda: eng.cache_rows(0, 1, rows, rows.float()),
+           lambda: eng.score_prompt(0, 1, q.float(), k), lambda: eng.score_prompt(0, 1, q, k[:, :1].contiguous()), lambda: eng.score_prompt(0, 1, q, k, row_lse=torch.zeros(4, device=DEV)),
+           lambda: eng.score_prompt(0, 1, q, k, mask=torch.zeros(2, 63, dtype=torch.uint8, device=DEV)), lambda: eng.score_prompt(0, 1, q.cpu(), k)]
+    for i, call in enumerate(bad):
+        say(f"refused {i}")
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(AssertionError):                     # not contiguous
+        eng.score_prompt(0, 1, q.transpose(2, 3), k)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in (lambda: step(), lambda: eng.cache_rows(0, 1, rows, rows), lambda: eng.score_prompt(0, 1, q, k)):
+        with pytest.raises(ValueError):
+            call()
+    monkeypatch.undo()
+    torch.cuda.synchronize()
+    eng.close()
+
+
 # ---- together ----------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("kind", ["fp4", "bf16"])
 def test_heavy_hitter_generation(kind):
