@@ -301,10 +301,14 @@ class MadaKV:
                         self._sl(self.budgets, l0, n) if budgets is None else budgets)
 
     def select_gather(self, l0, n, k, v, mask, psi_pool=None, budgets=None):
-        madakv_select_gather(self.h, l0, n, self._sl(self.psi_pool, l0, n) if psi_pool is None else psi_pool, mask,
-                             self._sl(self.budgets, l0, n) if budgets is None else budgets, k, v, self.kept_idx,
-                             self._sl(self.kv_off, l0, n), self._sl(self.kv_len, l0, n), self.k_c, self.v_c,
-                             self.select_ws)
+        # (one layer of few heads takes 15 us on the device: no views of the own buffers)
+        heads0, ws = l0 * self._heads, self.select_ws
+        rc = lib().madakv_select_gather(
+            self.h, l0, n, _ptr(self._sl(self.psi_pool, l0, n) if psi_pool is None else psi_pool), _ptr(mask),
+            _ptr(self._sl(self.budgets, l0, n) if budgets is None else budgets), _ptr(k), _ptr(v), _ptr(self.kept_idx),
+            _ptr(self.kv_off) + 8 * heads0, _ptr(self.kv_len) + 4 * heads0, _ptr(self.k_c), _ptr(self.v_c), _ptr(ws), ws.numel(), _stream())
+        if rc != OK:
+            raise MadaKVError("madakv_select_gather", rc)
 
     def evict(self, l0, n, q_win, k, v, mask):
         madakv_evict(self.h, l0, n, q_win, k, v, mask, self._sl(self.psi, l0, n), self._sl(self.psi_pool, l0, n),

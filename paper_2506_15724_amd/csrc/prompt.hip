@@ -307,7 +307,10 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(N
 // 32 queries.  A wave keeps its logits (keys x queries, up to 8 tiles of 32 x 32) in registers, so that each is formed once: maximum
 // and sum of a query's column are the lane's own and the other half's, its weights follow, and a key's weights are added up over
 // the 32 lanes that have its row, 16 keys at a time: exchanges in which a lane sends half of what it has left and keeps the other.
-// Waves w and w + 4 share a SIMD and take blocks whose keys add up to the same.
+// Waves w and w + 4 share a SIMD and take blocks whose keys add up to the same.  What bounds it: a launch's latency on few heads, the vector
+// unit on many.  us on the device, two sweeps / this: 8 heads of 40 x 64 6.9 / 3.6, of 203 x 64 11.8 / 7.2, 32 of 256 x 128 14.7 / 9.1 (normalisers
+// given 9.5 / 8.0), 28 / 4 of 256 x 128 17.0 / 11.3, 256 of 130 x 128 15.1 / 7.8, 2048 of 256 x 128 139 / 77, of 200 x 64 86 / 53: it is taken
+// wherever the logits of a block of queries fit a wave's registers.
 constexpr int PR_SHORT = 256, PR_SHORT_WAVES = PR_SHORT / 32;
 
 template <int CTRL>
@@ -480,8 +483,7 @@ struct PromptPlan { int ncb, per_chunk, chunks, blocks, items[2]; };      // ite
 // large ones, of which 512 run at a time; 500 of the small ones, of which 1024 do), but no shorter than 512 (256) rows: every
 // item starts with its columns and an empty ring.  us per call, 28 / 4 heads of 128 dims, at least 1200 / 2300 / 4100 large items: 16K 2112 /
 // 1788 / 1799, 32 heads of 8K with normalisers 293 / 274 / 279.  500 / 1000 small ones: 1K 36.5 / 44.7, 2K 67.4 / 66.8, 64 heads of 700
-// 33.2 / 37.4, 8 / 1 heads of 4K 74.9 / 82.9.  Chunks of at least 128 / 256 / 512 rows: 8 heads of 203 x 64 18.4 / 12.8 / 12.8 (one chunk: two launches
-// instead of four), of 1K 20.8 / 19.9 / 24.2.
+// 33.2 / 37.4, 8 / 1 heads of 4K 74.9 / 82.9.  Chunks of at least 128 / 256 / 512 rows: 8 heads of 1K x 64 20.8 / 19.9 / 24.2.
 constexpr int PR_MANY = 512, PR_ITEMS4 = 2300, PR_ITEMS1 = 500;
 static PromptPlan prompt_plan(const Dims& dm) {
   PromptPlan p;
