@@ -43,6 +43,7 @@ constexpr float PR_FAR = 0x1p60f;               // sums beyond it have left thei
 struct PromptArgs {
   const uint16_t* q; const uint16_t* k;         // [n, B, Hq, L, d], [n, B, H, L, d]
   float* lse2;                                  // [q heads][rows] log2 of the rows' normalisers; +inf past the prompt's end
+  const float* row_lse;                         // the caller's, or null
   float2* stat;                                 // [q heads][chunks][rows] (maximum, sum) per chunk, log2 units
   float* part;                                  // [q heads][chunks][rows] column sums per chunk
   float* psi;
@@ -79,7 +80,28 @@ __device__ __forceinline__ void to_lds4(__amdgpu_buffer_rsrc_t b, uint32_t dst, 
   __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (plds_ptr_t)(uintptr_t)dst, 4, at, base, 0, 0);
 }
 
-template <int D, int NCB, int PASS>             // a wave's column blocks of 32
+// log2 of the normaliser of row r: from the chunks' (maximum, sum), or from the caller's natural logarithm; +inf past the prompt's
+// end, where rows count for nothing
+__device__ __forceinline__ float normaliser_of(const PromptArgs& a, long long qh, int r, int cb_rows) {
+  if (r >= a.L) return __builtin_inff();
+  if (a.row_lse) return a.row_lse[qh * a.L + r] * 1.4426950408889634f;
+  const int last = r / (a.per_chunk * cb_rows);              // the chunk with the row's own key
+  float m = -__builtin_inff(), s = 0.f;
+  for (int c0 = 0; c0 <= last; c0 += 4) {
+    float2 x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[u] = c0 + u <= last ? a.stat[(qh * a.chunks + c0 + u) * a.rows + r] : make_float2(-__builtin_inff(), 0.f);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float t = fmaxf(m, x[u].x);
+      s = (m == -__builtin_inff() ? 0.f : s * __builtin_amdgcn_exp2f(m - t)) + (x[u].x == -__builtin_inff() ? 0.f : x[u].y * __builtin_amdgcn_exp2f(x[u].x - t));
+      m = t;
+    }
+  }
+  return m + log2f(s);
+}
+
+template <int D, int NCB, int PASS, bool OWN_NORM = false>             // a wave's column blocks of 32; OWN_NORM: sweep 2 makes the normalisers of its rows itself
 __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(NCB == 4 && D == 64 ? 3 : 2, NCB == 4 ? (D == 64 ? 3 : 2) : 4))) void prompt_sweep_kernel(PromptArgs a) {
   constexpr int KS = D / 16;                    // MFMA steps over the head dimension
   constexpr int PPR = D / 8;                    // 16-byte pieces per row
@@ -87,7 +109,9 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(N
   constexpr int TILEB = PR_TILE * ROWB;
   constexpr int LPT = PR_TILE * PPR / (PR_WAVES * 64);     // load instructions per wave and tile, 1 KB each
   constexpr int CB = PR_WAVES * NCB * 32;
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];     // [ring][64 rows][D], sweep 2: [ring][waves][64] normalisers
+  constexpr int LOADS = LPT + (PASS == 2 && !OWN_NORM ? 1 : 0);            // of a wave, per tile
+  // [ring][64 rows][D], sweep 2: [ring][waves][64] normalisers, or those of all rows of the item
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
 
   // workgroup -> item: XCD x (workgroups go to the XCDs in turn) takes the x-th eighth of all items, heads one after the other
   const int per_xcd = (a.total + 7) / 8;
@@ -127,11 +151,13 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(N
 #pragma unroll
     for (int j = 0; j < LPT; ++j)
       to_lds16(rows_buf, ring + slot * TILEB + (uint32_t)(wave * LPT + j) * 1024u, piece_off[j], r0 * ROWB);
-    if (PASS == 2)                              // the rows' normalisers, every wave its own copy
+    if (PASS == 2 && !OWN_NORM)                 // the rows' normalisers, every wave its own copy
       to_lds4(norm_buf, ring_n + (slot * PR_WAVES + wave) * (PR_TILE * 4u), lane * 4, r0 * 4);
   };
   issue(0);
   issue(min(1, ntiles - 1));
+  if constexpr (OWN_NORM)
+    for (int r = tid; r < row1 - row0; r += PR_WAVES * 64) reinterpret_cast<float*>(smem + PR_RING * TILEB)[r] = normaliser_of(a, qh, row0 + r, CB);
 
   // the wave's columns; a lane holds, for step ks, elements [half * D/2 + ks * 8, + 8) of column `col` of a block
   pbf16x8_t breg[NCB][KS];
@@ -199,14 +225,14 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(N
   for (int t = 0; t < ntiles; ++t) {
     // tile t has landed (the next one's loads may still be out); behind the barrier that holds for every wave, and nobody
     // reads tile t - 1 any more, whose slot the next loads take
-    if (LPT + (PASS == 2) == 5) asm volatile("s_waitcnt vmcnt(5) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    else if (LPT + (PASS == 2) == 4) asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    else if (LPT + (PASS == 2) == 3) asm volatile("s_waitcnt vmcnt(3) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (LOADS == 5) asm volatile("s_waitcnt vmcnt(5) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else if (LOADS == 4) asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else if (LOADS == 3) asm volatile("s_waitcnt vmcnt(3) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     else asm volatile("s_waitcnt vmcnt(2) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    static_assert(LPT + (PASS == 2) >= 2 && LPT + (PASS == 2) <= 5, "the waits above are written for these");
+    static_assert(LOADS >= 2 && LOADS <= 5, "the waits above are written for these");
     issue(min(t + 2, ntiles - 1));              // (past the end: the last tile once more, which keeps the count of loads in flight)
     const uint32_t tile = ring + (uint32_t)(t % PR_RING) * TILEB;
-    const uint32_t tile_n = ring_n + (uint32_t)((t % PR_RING) * PR_WAVES + wave) * (PR_TILE * 4u) + half * 16u;
+    const uint32_t tile_n = ring_n + (uint32_t)(OWN_NORM ? t : (t % PR_RING) * PR_WAVES + wave) * (PR_TILE * 4u) + half * 16u;
 #pragma unroll 1
     for (int sub = 0; sub < PR_TILE / 32; ++sub) {
       const int r = row0 + t * PR_TILE + sub * 32;
@@ -422,34 +448,13 @@ __global__ __launch_bounds__(PR_SHORT_WAVES * 64) __attribute__((amdgpu_waves_pe
   if (scaled) scaled[(long long)qh * a.L + tid] = s * factor;
 }
 
-// log2 of the rows' normalisers: from the chunks' (maximum, sum), or from the caller's natural logarithms
-__global__ __launch_bounds__(256) void prompt_normaliser_kernel(PromptArgs a, const float* row_lse, int cb_rows, long long n) {
+// log2 of the rows' normalisers, where the items do not make them themselves
+__global__ __launch_bounds__(256) void prompt_normaliser_kernel(PromptArgs a, int cb_rows, long long n) {
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
   if (i >= n) return;
   const long long qh = i / a.rows;
   const int r = (int)(i - qh * a.rows);
-  float out = __builtin_inff();                 // rows past the prompt's end count for nothing
-  if (r < a.L) {
-    if (row_lse) {
-      out = row_lse[qh * a.L + r] * 1.4426950408889634f;
-    } else {
-      const int last = r / (a.per_chunk * cb_rows);          // the chunk with the row's own key
-      float m = -__builtin_inff(), s = 0.f;
-      for (int c0 = 0; c0 <= last; c0 += 4) {
-        float2 x[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) x[u] = c0 + u <= last ? a.stat[(qh * a.chunks + c0 + u) * a.rows + r] : make_float2(-__builtin_inff(), 0.f);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const float t = fmaxf(m, x[u].x);
-          s = (m == -__builtin_inff() ? 0.f : s * __builtin_amdgcn_exp2f(m - t)) + (x[u].x == -__builtin_inff() ? 0.f : x[u].y * __builtin_amdgcn_exp2f(x[u].x - t));
-          m = t;
-        }
-      }
-      out = m + log2f(s);
-    }
-  }
-  a.lse2[i] = out;
+  a.lse2[i] = normaliser_of(a, qh, r, cb_rows);
 }
 
 // psi = the column sums of the query heads and chunks, in that order; scaled: psi * factor beside it
@@ -509,13 +514,26 @@ static PromptPlan prompt_plan(const Dims& dm) {
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 static size_t rows_of(const Dims& dm) { return (size_t)(dm.L + PR_TILE - 1) / PR_TILE * PR_TILE; }
 
-bool prompt_supported(const madakv_config& c) { return c.dtype == MADAKV_BF16; }
-// normalisers, then what the chunks leave (sweep 2's column sums take the place of sweep 1's statistics), then the scaled scores
-size_t prompt_ws_bytes(const Dims& dm) {
-  const PromptPlan p = prompt_plan(dm);
-  const size_t qheads = (size_t)dm.n * dm.B * dm.Hq;
-  return up256(qheads * rows_of(dm) * 4) + up256(qheads * p.chunks * rows_of(dm) * 8) + up256((size_t)dm.heads * dm.L * 4);
+// Items of few rows make the normalisers of their rows themselves, in sweep 2, which saves a launch.  us on the device, a launch of its own /
+// this: 8 heads of 512 x 64 16.4 / 14.7, of 1K x 64 17.3 / 15.3, 28 / 4 of 1K x 128 30.6 / 27.8, 20 of 1.5K x 128 34.0 / 32.6, 8 / 1 of 4K x 128
+// 66.2 / 65.9, normalisers given 36.3 / 34.3.  Up to 512, 1024 or 2048 rows: all the same; their normalisers take 4 KB of LDS at most.
+constexpr int PR_OWN_ROWS = 1024;
+static bool own_norm(const PromptPlan& p, bool given) { return p.ncb == 1 && p.per_chunk * PR_WAVES * 32 <= PR_OWN_ROWS && (given || p.chunks > 1); }
+// normalisers, then what the chunks leave (sweep 2's column sums take the place of sweep 1's statistics, but where sweep 2 still
+// reads those), then the scaled scores
+struct PromptWs { size_t stat, part, scaled, total; };
+static PromptWs prompt_ws(const Dims& dm, const PromptPlan& p) {
+  PromptWs w;
+  const size_t qheads = (size_t)dm.n * dm.B * dm.Hq, entries = qheads * p.chunks * rows_of(dm);
+  w.stat = up256(qheads * rows_of(dm) * 4);
+  const bool apart = own_norm(p, false);
+  w.part = apart ? w.stat + up256(entries * 8) : w.stat;
+  w.scaled = w.part + up256(entries * (apart ? 4 : 8));
+  w.total = w.scaled + up256((size_t)dm.heads * dm.L * 4);
+  return w;
 }
+bool prompt_supported(const madakv_config& c) { return c.dtype == MADAKV_BF16; }
+size_t prompt_ws_bytes(const Dims& dm) { return prompt_ws(dm, prompt_plan(dm)).total; }
 
 template <int D>
 static hipError_t launch_short(const Dims& dm, const PromptArgs& a, const float* row_lse, float* scaled, float factor, hipStream_t st) {
@@ -545,12 +563,17 @@ static hipError_t launch_sweeps(const Dims& dm, const PromptPlan& p, PromptArgs&
     hipLaunchKernelGGL((prompt_sweep_kernel<D, NCB, 1>), grid, block, lds1, st, a);
     if (hipError_t e = hipGetLastError()) return e;
   }
-  if (row_lse || a.chunks > 1) {
-    hipLaunchKernelGGL(prompt_normaliser_kernel, dim3((unsigned)((nrows + 255) / 256)), dim3(256), 0, st, a, row_lse, CB, nrows);
+  const bool own = own_norm(p, row_lse != nullptr);
+  if (!own && (row_lse || a.chunks > 1)) {
+    hipLaunchKernelGGL(prompt_normaliser_kernel, dim3((unsigned)((nrows + 255) / 256)), dim3(256), 0, st, a, CB, nrows);
     if (hipError_t e = hipGetLastError()) return e;
   }
   const dim3 grid = grid_of(2);
-  hipLaunchKernelGGL((prompt_sweep_kernel<D, NCB, 2>), grid, block, lds2, st, a);
+  if (own) {
+    if constexpr (NCB == 1) hipLaunchKernelGGL((prompt_sweep_kernel<D, 1, 2, true>), grid, block, lds1 + (size_t)a.per_chunk * CB * 4, st, a);
+  } else {
+    hipLaunchKernelGGL((prompt_sweep_kernel<D, NCB, 2>), grid, block, lds2, st, a);
+  }
   if (hipError_t e = hipGetLastError()) return e;
   if (a.chunks > 1 || a.G > 1 || scaled) hipLaunchKernelGGL(prompt_sum_kernel, dim3((unsigned)((npsi + 255) / 256)), dim3(256), 0, st, a, CB, scaled, factor, npsi);
   return hipGetLastError();
@@ -560,15 +583,15 @@ static hipError_t launch_sweeps(const Dims& dm, const PromptPlan& p, PromptArgs&
 hipError_t launch_prompt(const Dims& dm, const madakv_config& c, const void* q, const void* k, const float* row_lse, float* psi,
                          void* ws, float factor, float** scaled, hipStream_t st) {
   const PromptPlan p = prompt_plan(dm);
-  const size_t qheads = (size_t)dm.n * dm.B * dm.Hq;
   PromptArgs a;
   a.q = static_cast<const uint16_t*>(q); a.k = static_cast<const uint16_t*>(k);
-  a.psi = psi; a.G = dm.G; a.L = dm.L; a.rows = (int)rows_of(dm);
+  a.psi = psi; a.row_lse = row_lse; a.G = dm.G; a.L = dm.L; a.rows = (int)rows_of(dm);
   char* w = static_cast<char*>(ws);
-  a.lse2 = reinterpret_cast<float*>(w); w += up256(qheads * a.rows * 4);
-  a.stat = reinterpret_cast<float2*>(w); a.part = reinterpret_cast<float*>(w); w += up256(qheads * p.chunks * a.rows * 8);
+  const PromptWs at = prompt_ws(dm, p);
+  a.lse2 = reinterpret_cast<float*>(w);
+  a.stat = reinterpret_cast<float2*>(w + at.stat); a.part = reinterpret_cast<float*>(w + at.part);
   float* s = nullptr;
-  if (scaled) *scaled = s = reinterpret_cast<float*>(w);
+  if (scaled) *scaled = s = reinterpret_cast<float*>(w + at.scaled);
   a.per_chunk = p.per_chunk; a.chunks = p.chunks; a.blocks = p.blocks;
   a.scale_log2 = (c.softmax_scale > 0.f ? c.softmax_scale : 1.0f / sqrtf((float)dm.d)) * 1.4426950408889634f;
   if (dm.L <= PR_SHORT) {
