@@ -1,7 +1,8 @@
 // Scores of every key against all queries of the prompt (paper Sec. 3.3 Eq. 7 with every position as a proxy token; the
 // accumulated attention weight of heavy-hitter eviction): for KV head h with G query heads
 //   psi(i) = sum over g, r >= i of exp(scale * q_gr . k_i - lse_gr),   lse_gr = log sum over j <= r of exp(scale * q_gr . k_j)
-// L^2 / 2 logits per query head, which are never stored: sweep 1 forms them for the normalisers (left out where the caller's
+// L^2 / 2 logits per query head, which are never stored.  Prompts of up to PR_SHORT positions form them once (prompt_short_kernel).
+// Longer ones take two sweeps: sweep 1 forms them for the normalisers (left out where the caller's
 // prefill attention has them), sweep 2 once more for the column sums.
 //
 // Both sweeps are one kernel.  A workgroup holds a block of columns in registers as operand B (sweep 1: query rows, sweep 2: keys;
