@@ -249,11 +249,11 @@ class MadaKV:
         self._out_row, self._heads, self._kv_row, self._ctx = batch * n_q_heads * head_dim, batch * n_kv_heads, batch * n_kv_heads * head_dim, ctx_len
         self.n_call = layers_per_call or n_layers
         s_ws, sel_ws, d_ws = madakv_workspace_bytes(self.h, self.n_call)
-        d1 = madakv_workspace_bytes(self.h, 1)[2]
+        d_ws = max(madakv_workspace_bytes(self.h, m)[2] for m in range(1, self.n_call + 1))       # (longer pieces of more heads: not always the most layers')
         dev = self.device
         self.score_ws = torch.empty(max(s_ws, 16), dtype=torch.uint8, device=dev)
         self.select_ws = torch.empty(max(sel_ws, 16), dtype=torch.uint8, device=dev)
-        self.decode_ws = torch.empty(max(d_ws, d1, 16), dtype=torch.uint8, device=dev)
+        self.decode_ws = torch.empty(max(d_ws, 16), dtype=torch.uint8, device=dev)
         NL, B, H, L, W = n_layers, batch, n_kv_heads, ctx_len, window
         M = self.M = n_modalities
         self.psi = torch.empty(NL, B, H, L, dtype=torch.float32, device=dev)
@@ -364,7 +364,7 @@ class MadaKV:
             self._check_array("slot_out", slot_out, heads, torch.int32)
         self._check_array("pos", pos, self.cfg.batch, torch.int32)
         if getattr(self, "weights_ws", None) is None:
-            need = max(madakv_decode_attn_weights_workspace_bytes(self.h, m) for m in (1, self.n_call))
+            need = max(madakv_decode_attn_weights_workspace_bytes(self.h, m) for m in range(1, self.n_call + 1))
             self.weights_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         heads0, ws = l0 * self._heads, self.weights_ws
         rc = lib().madakv_decode_attn_weights(

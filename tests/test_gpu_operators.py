@@ -648,6 +648,27 @@ def test_arrays_and_devices_that_do_not_fit(monkeypatch):
     eng.close()
 
 
+@pytest.mark.parametrize("kind,L,NL,H", [("bf16", 2048, 32, 32), ("fp4", 4096, 6, 32)])
+def test_workspaces_of_the_holder_serve_every_number_of_layers(kind, L, NL, H):
+    """The pieces of a head get longer with the heads of a call, so that calls over fewer layers can need more workspace than one over all."""
+    eng = MB.MadaKV(n_layers=NL, batch=1, n_q_heads=H, n_kv_heads=H, head_dim=64, ctx_len=L, window=8, budget=L // 2, max_new_tokens=0, device=DEV, **KINDS[kind])
+    plain = [MB.madakv_workspace_bytes(eng.h, m)[2] for m in range(1, NL + 1)]
+    more = [MB.madakv_decode_attn_weights_workspace_bytes(eng.h, m) for m in range(1, NL + 1)]
+    n = 1 + int(np.argmax(plain))
+    say(f"{kind}: most workspace for {n} of {NL} layers")
+    assert 1 < n < NL and eng.decode_ws.numel() == plain[n - 1]
+    eng.kv_off.copy_(9 * torch.arange(NL * H).view(NL, 1, H)), eng.kv_len.fill_(9)
+    eng.k_c.zero_(), eng.v_c.zero_()
+    q = torch.randn(n, 1, H, 64, device=DEV).to(eng.tdtype)
+    out = torch.full((n, 1, H, 64), float("nan"), device=DEV)
+    eng.decode_attn(0, n, q, None, None, out)
+    acc = torch.zeros(eng.capacity, device=DEV)
+    eng.decode_attn_weights(0, n, q, None, None, out, acc, torch.zeros_like(acc))
+    torch.cuda.synchronize()
+    assert not out.any() and eng.weights_ws.numel() == max(more)
+    eng.close()
+
+
 # ---- together ----------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("kind", ["fp4", "bf16"])
 def test_heavy_hitter_generation(kind):
