@@ -18,7 +18,7 @@
 // 16K tokens, 28 / 4 heads of 128 dims, both sweeps: 1.76-1.81 ms, 240 ns per tile and SIMD, 1.08 PFLOP/s of logits (a library product of
 // 16K x 16K x 16K bf16 runs at 1.36 on this card); 8K tokens, 32 heads, one sweep 0.27 ms.  Kept steps: address arithmetic per load -> a
 // buffer with fixed offsets 1.85 -> 1.80; a block's contraction between the vector instructions of the one before it 1.89 -> 1.85.
-// No gain: blocks of two and three waves per SIMD (1.87), heads in plain order instead of one XCD's (1.84).  At 64 dims, half the
+// No gain at this size: blocks of two and three waves per SIMD (1.87; smaller calls take them, see prompt_plan), heads in plain order instead of one XCD's (1.84).  At 64 dims, half the
 // matrix instructions, the vector unit alone bounds it, and the registers leave room for three waves: 16K, 28 / 4 heads 1.22 ms,
 // 8K, 32 heads 0.376 (two waves 0.407, blocks of two and four waves 1.49 and 0.406, four waves with spills 1.38 and 0.437).
 // The rows come straight into LDS (16 bytes per lane, pieces of a row permuted so that operand reads do not collide), in a
@@ -484,19 +484,22 @@ __global__ __launch_bounds__(256) void prompt_sum_kernel(PromptArgs a, int cb_ro
 }
 
 struct PromptPlan { int ncb, per_chunk, chunks, blocks, items[2]; };      // items of a head in sweep 1 and 2 (item_of)
-// Column blocks of 512 (a wave has four blocks of 32) where those give the chip two workgroups per compute unit to work on, of 128
-// otherwise; chunks as long as leave enough items for the launch's last round of workgroups to be a small part of it (2300 of the
-// large ones, of which 512 run at a time; 500 of the small ones, of which 1024 do), but no shorter than 512 (256) rows: every
-// item starts with its columns and an empty ring.  us per call, 28 / 4 heads of 128 dims, at least 1200 / 2300 / 4100 large items: 16K 2112 /
-// 1788 / 1799, 32 heads of 8K with normalisers 293 / 274 / 279.  500 / 1000 small ones: 1K 36.5 / 44.7, 2K 67.4 / 66.8, 64 heads of 700
-// 33.2 / 37.4, 8 / 1 heads of 4K 74.9 / 82.9.  Chunks of at least 128 / 256 / 512 rows: 8 heads of 1K x 64 20.8 / 19.9 / 24.2.
-constexpr int PR_MANY = 512, PR_ITEMS4 = 2300, PR_ITEMS1 = 500;
+// Column blocks of 512 (a wave has four blocks of 32) where those are enough items to fill the chip several times over, of 256 where
+// it is those, of 128 otherwise, and none so large that more than 15% (20%) of the columns are past the prompt's end; chunks as long as
+// leave 2300 (1300, 640) items, of which 512 (768, 1024) run at a time, so that the launch's last round of workgroups is a small
+// part of it, but no shorter than 512 (256, 256) rows: every item starts with its columns and an empty ring.  The numbers are those
+// with the least time over 122 calls of 8 to 128 heads and 300 to 9000 positions, 1.9% above the best choice for each (2.4% with
+// 1800, 600, 600 items; 6.1% without blocks of 256).  us on the device, blocks of 512 / 256 / 128: 32 / 8 heads of 2K x 128 79 / 62 / 66, 80 of 1.7K x 64
+// 87 / 69 / 76, 28 / 4 of 4K x 128 154 / 158 / 178, 20 of 6K x 128 236 / 227 / 251, 32 of 1K x 128 52 / 33 / 27.  28 / 4 heads of 16K x 128, at least 1200 / 2300 / 4100
+// items: 2112 / 1788 / 1799, 32 heads of 8K with normalisers 293 / 274 / 279.
 static PromptPlan prompt_plan(const Dims& dm) {
+  struct Choice { int ncb, shortest, want, least, fill; };   // blocks, least blocks per chunk, items to aim for, least items, least % of columns in the prompt
+  constexpr Choice choices[] = {{4, 1, 2300, 2000, 85}, {2, 1, 1300, 700, 80}, {1, 2, 640, 0, 0}};
   PromptPlan p;
   const long long qheads = (long long)dm.n * dm.B * dm.Hq;
-  for (int ncb : {4, 1}) {
-    const int cb = PR_WAVES * ncb * 32, shortest = ncb == 4 ? 1 : 2;
-    p.ncb = ncb;
+  for (const Choice& c : choices) {
+    const int cb = PR_WAVES * c.ncb * 32;
+    p.ncb = c.ncb;
     p.blocks = (dm.L + cb - 1) / cb;
     for (p.per_chunk = p.blocks;; p.per_chunk = (p.per_chunk + 1) / 2) {
       p.chunks = (p.blocks + p.per_chunk - 1) / p.per_chunk;
@@ -506,9 +509,9 @@ static PromptPlan prompt_plan(const Dims& dm) {
         p.items[0] += nb * (g + 1);
         p.items[1] += nb * (p.chunks - g);
       }
-      if (qheads * p.items[0] >= (ncb == 4 ? PR_ITEMS4 : PR_ITEMS1) || p.per_chunk <= shortest) break;
+      if (qheads * p.items[0] >= c.want || p.per_chunk <= c.shortest) break;
     }
-    if (qheads * p.items[0] >= PR_MANY) break;
+    if (qheads * p.items[0] >= c.least && 100ll * dm.L >= (long long)c.fill * p.blocks * cb) break;
   }
   return p;
 }
@@ -516,10 +519,10 @@ static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 static size_t rows_of(const Dims& dm) { return (size_t)(dm.L + PR_TILE - 1) / PR_TILE * PR_TILE; }
 
 // Items of few rows make the normalisers of their rows themselves, in sweep 2, which saves a launch.  us on the device, a launch of its own /
-// this: 8 heads of 512 x 64 16.4 / 14.7, of 1K x 64 17.3 / 15.3, 28 / 4 of 1K x 128 30.6 / 27.8, 20 of 1.5K x 128 34.0 / 32.6, 8 / 1 of 4K x 128
-// 66.2 / 65.9, normalisers given 36.3 / 34.3.  Up to 512, 1024 or 2048 rows: all the same; their normalisers take 4 KB of LDS at most.
+// this: 8 heads of 512 x 64 16.4 / 14.7, of 1K x 64 17.3 / 15.3, 28 / 4 of 1K x 128 30.6 / 27.8, 8 of 1K x 128 with normalisers
+// given 12.0 / 10.2.  Up to 512, 1024 or 2048 rows: all the same; their normalisers take 4 KB of LDS at most.
 constexpr int PR_OWN_ROWS = 1024;
-static bool own_norm(const PromptPlan& p, bool given) { return p.ncb == 1 && p.per_chunk * PR_WAVES * 32 <= PR_OWN_ROWS && (given || p.chunks > 1); }
+static bool own_norm(const PromptPlan& p, bool given) { return p.ncb <= 2 && p.per_chunk * PR_WAVES * p.ncb * 32 <= PR_OWN_ROWS && (given || p.chunks > 1); }
 // normalisers, then what the chunks leave (sweep 2's column sums take the place of sweep 1's statistics, but where sweep 2 still
 // reads those), then the scaled scores
 struct PromptWs { size_t stat, part, scaled, total; };
@@ -571,7 +574,7 @@ static hipError_t launch_sweeps(const Dims& dm, const PromptPlan& p, PromptArgs&
   }
   const dim3 grid = grid_of(2);
   if (own) {
-    if constexpr (NCB == 1) hipLaunchKernelGGL((prompt_sweep_kernel<D, 1, 2, true>), grid, block, lds1 + (size_t)a.per_chunk * CB * 4, st, a);
+    if constexpr (NCB <= 2) hipLaunchKernelGGL((prompt_sweep_kernel<D, NCB, 2, true>), grid, block, lds1 + (size_t)a.per_chunk * CB * 4, st, a);
   } else {
     hipLaunchKernelGGL((prompt_sweep_kernel<D, NCB, 2>), grid, block, lds2, st, a);
   }
@@ -599,8 +602,8 @@ hipError_t launch_prompt(const Dims& dm, const madakv_config& c, const void* q, 
     a.per_chunk = a.chunks = 1;
     return dm.d == 128 ? launch_short<128>(dm, a, row_lse, s, factor, st) : launch_short<64>(dm, a, row_lse, s, factor, st);
   }
-  if (dm.d == 128) return p.ncb == 4 ? launch_sweeps<128, 4>(dm, p, a, row_lse, s, factor, st) : launch_sweeps<128, 1>(dm, p, a, row_lse, s, factor, st);
-  return p.ncb == 4 ? launch_sweeps<64, 4>(dm, p, a, row_lse, s, factor, st) : launch_sweeps<64, 1>(dm, p, a, row_lse, s, factor, st);
+  if (dm.d == 128) return p.ncb == 4 ? launch_sweeps<128, 4>(dm, p, a, row_lse, s, factor, st) : p.ncb == 2 ? launch_sweeps<128, 2>(dm, p, a, row_lse, s, factor, st) : launch_sweeps<128, 1>(dm, p, a, row_lse, s, factor, st);
+  return p.ncb == 4 ? launch_sweeps<64, 4>(dm, p, a, row_lse, s, factor, st) : p.ncb == 2 ? launch_sweeps<64, 2>(dm, p, a, row_lse, s, factor, st) : launch_sweeps<64, 1>(dm, p, a, row_lse, s, factor, st);
 }
 
 }  // namespace madakv

@@ -506,10 +506,11 @@ def test_prompt_scores_at_edges(L, Hq, H, d, given):
     eng.close()
 
 
-@pytest.mark.parametrize("NL,B,Hq,H,d,L", [(1, 1, 28, 4, 128, 4100), (1, 2, 32, 32, 128, 1025), (2, 2, 16, 8, 64, 1500), (1, 1, 8, 8, 64, 5000), (1, 4, 32, 32, 64, 2047), (3, 1, 32, 32, 128, 640)])
+@pytest.mark.parametrize("NL,B,Hq,H,d,L", [(1, 1, 28, 4, 128, 4100), (1, 2, 32, 32, 128, 1025), (2, 2, 16, 8, 64, 1500), (1, 1, 8, 8, 64, 5000), (1, 4, 32, 32, 64, 2047), (3, 1, 32, 32, 128, 640),
+                                            (1, 1, 32, 8, 128, 2048), (1, 1, 12, 2, 64, 3500), (2, 1, 16, 4, 64, 1790), (4, 2, 32, 32, 64, 513), (1, 1, 20, 20, 128, 1537), (1, 2, 28, 4, 128, 1025)])
 @pytest.mark.parametrize("given", [False, True])
 def test_prompt_scores_of_large_calls(NL, B, Hq, H, d, L, given):
-    """Calls that take blocks of 512 columns, several chunks per head, several layers and batch items."""
+    """Calls that take blocks of 256 and 512 columns, several chunks per head, several layers and batch items."""
     eng, q, k = prompt_case(NL, B, Hq, H, d, L)
     say(f"prompt {NL} x {B} x {Hq}/{H} d={d} L={L} lse={given}")
     check_prompt(eng, q, k, given)
