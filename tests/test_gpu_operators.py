@@ -619,6 +619,37 @@ def test_statistics_of_short_prompts():
         eng.close()
 
 
+@pytest.mark.parametrize("Hq,H,d,L", [(4, 4, 64, 200), (7, 1, 128, 256), (8, 2, 64, 700), (32, 8, 128, 2048)])
+@pytest.mark.parametrize("given", [False, True])
+def test_prompt_scores_in_a_replayed_graph(Hq, H, d, L, given):
+    """Scores with statistics, captured once and replayed on other inputs, with eager calls of the same holder between the replays."""
+    eng, q, k = prompt_case(1, 1, Hq, H, d, L, W=8)
+    lse = torch.zeros(1, 1, Hq, L, device=DEV) if given else None
+    mask = torch.randint(0, 2, (1, L), generator=torch.Generator().manual_seed(2)).to(DEV, torch.uint8)
+    call = lambda: eng.score_prompt(0, 1, q, k, mask=mask, row_lse=lse)      # noqa: E731
+    outs = lambda: [t.clone() for t in (eng.psi, eng.psi_pool, eng.stats, eng.n_mod)]      # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        call()
+    g = torch.Generator(device=DEV).manual_seed(8)
+    for step in range(4):
+        say(f"prompt graph {Hq}/{H} d={d} L={L} lse={given} replay {step}")
+        q.copy_(torch.randn(q.shape, generator=g, device=DEV)), k.copy_(torch.randn(k.shape, generator=g, device=DEV))
+        if given:
+            lse.copy_(5.0 + torch.rand(lse.shape, generator=g, device=DEV))
+        call()
+        torch.cuda.synchronize()
+        want = outs()
+        for t in (eng.psi, eng.psi_pool):
+            t.fill_(-1.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs(), want))
+    eng.close()
+
+
 def test_arrays_and_devices_that_do_not_fit(monkeypatch):
     """What the holder refuses before the library is called: arrays of another type, size or device, and a current device that is
     not the handle's."""
