@@ -21,6 +21,7 @@ struct madakv_handle {
   int32_t* d_page_tbl;             // paged cache: [n_layers * B * H][entries] page table (null otherwise)
   void* d_split; size_t split_bytes;   // long contexts: buffer of the chunk-parallel statistics / selection (null otherwise)
   std::vector<int32_t> appended;   // decode rows appended since the last (re-)eviction, per layer
+  std::vector<uint8_t> replays;    // per layer: an appending step has been captured, so that rows come without the host's knowing (for good: its graph may live on)
   // per layer: rows have taken the places of others since the last eviction (1), or do so whenever a captured step is replayed
   // (2, for good: nobody tells the host of replays), so that they are not in order of position
   std::vector<uint8_t> replaced;
@@ -220,7 +221,8 @@ hipError_t publish_maxlen(madakv_handle* h, int layer0, int n, hipStream_t st, h
 // worst case otherwise.
 // replayed: the launch may run again later without coming through here (a stream under graph capture): the bound
 // then covers every row the segments have room for, not only the rows of this step.
-int longest_rows(madakv_handle* h, int layer0, int n, bool replayed = false) {
+// whatever_replayed: so it does for layers that a captured step appends to: for calls that may come behind its replays.
+int longest_rows(madakv_handle* h, int layer0, int n, bool replayed = false, bool whatever_replayed = false) {
   const madakv_config& c = h->cfg;
   const int worst = c.ctx_len + c.max_new_tokens;
   bool pending = false;
@@ -230,7 +232,7 @@ int longest_rows(madakv_handle* h, int layer0, int n, bool replayed = false) {
   int mx = 0;
   for (int l = layer0; l < layer0 + n; ++l) {
     if (h->maxlen_state[l] != 2) return worst;
-    const int grown = replayed ? c.max_new_tokens : h->appended[l] + 1;
+    const int grown = replayed || (whatever_replayed && h->replays[l]) ? c.max_new_tokens : h->appended[l] + 1;
     for (int b = 0; b < c.batch; ++b) mx = std::max(mx, h->h_maxlen[(size_t)l * c.batch + b] + grown);
   }
   return std::min(worst, mx);
@@ -287,7 +289,8 @@ int32_t decode_impl(madakv_handle* h, int32_t layer0, int32_t n,
   Dims dm = make_dims(h->cfg, n);
   // Under graph capture the launch is sized once and replayed while the heads grow: the grid (and the share of the
   // workspace) then covers all the rows the segments have room for.
-  const int longest = longest_rows(h, layer0, n, replayed_later(reinterpret_cast<hipStream_t>(stream)));
+  const bool later = replayed_later(reinterpret_cast<hipStream_t>(stream));
+  const int longest = longest_rows(h, layer0, n, later);
   // a caller's workspace is sized for the worst case; the handle's scratch must hold what this launch uses
   if (ws_bytes != NO_WORKSPACE) {
     if (ws_bytes < (w ? weights_ws_bytes(dm, h->cfg) : decode_ws_bytes(dm, h->cfg))) return MADAKV_ERR_WORKSPACE_TOO_SMALL;
@@ -305,9 +308,9 @@ int32_t decode_impl(madakv_handle* h, int32_t layer0, int32_t n,
   hipError_t e = launch_decode(dm, h->cfg, q, k_new, v_new, k_c, v_c, kv_off, kv_len, out, h->meet, ws,
                                region_tokens(h->cfg) * h->cfg.batch, longest, make_paging(h), layer0,
                                reinterpret_cast<hipStream_t>(stream), w);
-  if (e == hipSuccess && appends) for (int l = layer0; l < layer0 + n; ++l) h->appended[l] += 1;
+  if (e == hipSuccess && appends) for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] += 1; h->replays[l] |= later; }
   if (e == hipSuccess && k_new && !appends) {
-    const uint8_t how = replayed_later(reinterpret_cast<hipStream_t>(stream)) ? 2 : 1;
+    const uint8_t how = later ? 2 : 1;
     for (int l = layer0; l < layer0 + n; ++l) h->replaced[l] |= how;
   }
   if (e == hipSuccess && w) e = launch_row_weights(dm, h->cfg, *w, kv_off, kv_len, h->meet, longest, make_paging(h), layer0, reinterpret_cast<hipStream_t>(stream));
@@ -334,6 +337,7 @@ int32_t madakv_create(const madakv_config* cfg, madakv_handle** out) {
   h->appended.assign(cfg->n_layers, 0);
   h->gen_base.assign(cfg->n_layers, 0);
   h->replaced.assign(cfg->n_layers, 0);
+  h->replays.assign(cfg->n_layers, 0);
   h->xchg = nullptr; h->xchg_words = 0; h->xchg_left = false;
   h->meet = Meet{}; h->scratch = nullptr; h->scratch_bytes = 0; h->d_page_tbl = nullptr;
   h->d_split = nullptr; h->split_bytes = 0;
@@ -730,7 +734,7 @@ int32_t madakv_cache_rows(madakv_handle* h, int32_t layer0, int32_t n, const voi
   if (!c.cache_fp8) return MADAKV_ERR_UNIMPLEMENTED;                        // the cache holds the rows as they are
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   return hip_fail(h, launch_cache_rows(make_dims(c, n), c, k_c, v_c, kv_off, kv_len, k_rows, v_rows, region_tokens(c) * c.batch,
-                                       longest_rows(h, layer0, n, replayed_later(st)), make_paging(h), layer0, st));
+                                       longest_rows(h, layer0, n, replayed_later(st), true), make_paging(h), layer0, st));
 }
 
 namespace {

@@ -17,6 +17,7 @@ std::map<const void*, std::string> names;
 Launch pushed;
 std::string failing;                 // launches of kernels whose name contains one of these parts, separated by |, fail
 void* capturing = nullptr;           // the stream under capture
+bool done = false;                   // what events say when they are asked
 int last_error = 0;
 long made = 0;                       // streams and events
 
@@ -43,6 +44,7 @@ const char* fake_log() { return text.c_str(); }
 void fake_clear() { text.clear(); }
 void fake_fail(const char* part) { failing = part; }
 void fake_capture(void* stream) { capturing = stream; }
+void fake_events_done(int yes) { done = yes != 0; }
 
 // ---- the runtime
 int hipGetDevice(int* d) { *d = 0; return 0; }
@@ -62,7 +64,7 @@ int hipStreamIsCapturing(void* st, int* status) { *status = st && st == capturin
 int hipEventCreateWithFlags(void** ev, unsigned) { *ev = next_object(); return 0; }
 int hipEventDestroy(void*) { return 0; }
 int hipEventRecord(void* ev, void* st) { note("record %p %p", ev, st); return 0; }
-int hipEventQuery(void* ev) { note("query %p", ev); return 600; }             // not ready
+int hipEventQuery(void* ev) { note("query %p", ev); return done ? 0 : 600; }             // 600: not ready
 int hipEventSynchronize(void*) { return 0; }
 int hipFuncSetAttribute(const void*, int, int) { return 0; }
 int hipLaunchKernel(const void* f, Dim3 grid, Dim3 block, void** args, size_t lds, void* st) {

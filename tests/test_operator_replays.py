@@ -1,0 +1,37 @@
+"""What the host knows of rows that a captured step appends whenever its graph is replayed, on the runtime that only keeps a log:
+calls that look at all rows of a head cover every row that replays can have left.  No GPU."""
+import pytest
+
+from tests.test_abi import good
+from tests.test_host_calls import runtime, scenario  # noqa: F401  (a fixture)
+from tests.test_operator_calls import ARGS
+
+CALLS = ARGS + """
+st = 0x7000
+evict = lambda h, n=2: lib.madakv_evict(h, I(0), I(n), *[P(T().p) for _ in range(14)], P(T().p), Z(1 << 40), P(T().p), Z(1 << 40), P(0))
+plain = lambda h, l0=0, n=1, st=0: lib.madakv_decode_attn(h, I(l0), I(n), *[P(T().p) for _ in range(8)], P(T().p), Z(1 << 40), P(st))
+def grids(part): return [[int(g) for g in x.rest[1].split(",")] for x in log() if x.kind == "launch" and part in x.rest[3]]
+"""
+
+
+@pytest.mark.parametrize("step", ["plain(h, 0, 1, st)", "weights(h, st=st)"])
+@pytest.mark.parametrize("kw", [dict(cache_fp8=4), dict(cache_fp8=1, page_rows=16)])
+def test_rows_read_back_cover_replayed_appends(runtime, step, kw):  # noqa: F811
+    """madakv_cache_rows after a captured append: as many blocks of 64 rows as a head with every free row taken has, also behind a
+    later eviction; the other layer's as before."""
+    out = scenario(runtime, CALLS + f"""
+h = create(sys.argv[3])
+fake.fake_events_done(1)
+assert evict(h) == 0
+assert plain(h, 0, 2) == 0 and rows(h) == 0 and rows(h, l0=1) == 0
+assert [g[0] for g in grids("cache_rows")] == [1, 1]             # (the runtime's eviction leaves heads of no rows)
+fake.fake_capture(P(st))
+assert {step} == 0
+fake.fake_capture(P(0))
+for _ in range(2):
+    assert rows(h) == 0 and rows(h, l0=1) == 0 and rows(h, n=2) == 0
+    assert [g[0] for g in grids("cache_rows")] == [4, 1, 4]
+    assert evict(h) == 0
+print("ok")
+""", good(max_new_tokens=200, **kw))
+    assert out.strip() == "ok"
