@@ -400,11 +400,12 @@ int32_t madakv_page_table(const madakv_handle* h, const int32_t** table, int32_t
  *     taken from what the eviction produced once that has reached the host, from ctx_len +
  *     max_new_tokens before.  One layer of 128 heads of up to 16K rows fits.  Nothing is
  *     enqueued in that case.
- *   - On a stream under graph capture (this call or madakv_decode_attn) the launch is sized for every
+ *   - On a stream under graph capture (this call, madakv_decode_attn or madakv_decode_attn_weights) the launch is sized for every
  *     row the segments have room for, so that the captured step can be replayed while the heads
  *     grow; each replay appends a row like a call would, but the library's count of appended rows
  *     only sees the capture itself: the caller must not replay beyond max_new_tokens rows per
- *     head, and takes up eager calls again only after a new eviction or re-eviction. */
+ *     head, and takes up eager decode calls again only after a new eviction or re-eviction.  (madakv_cache_rows and
+ *     madakv_reevict go by the lengths on the device and take whatever rows the replays have left.) */
 #define MADAKV_STATIC_SCRATCH_BYTES ((size_t)8 << 20)
 int32_t madakv_decode_attn_static(madakv_handle* h, int32_t layer0, int32_t n,
                                   const void* q, const void* k_new, const void* v_new,

@@ -106,10 +106,10 @@ size_t window_attn_ws_bytes(const Dims& dm, const madakv_config& c);
 hipError_t launch_window_attn(const Dims& dm, const madakv_config& c, const void* q_win, const void* k, const void* v,
                               void* out, float* row_lse, float* psi, void* ws, Exchange& x, hipStream_t st);
 hipError_t launch_restats(const Dims& dm, const madakv_config& c, const float* psi_c, const int32_t* kept_idx, const uint8_t* mask,
-                          const int64_t* seg_off, const int32_t* seg_len, int appended, float* pool_c, uint8_t* rowmod,
+                          const int64_t* seg_off, const int32_t* seg_len, const int32_t* len1, int appended, float* pool_c, uint8_t* rowmod,
                           void* stats, int32_t* budgets, hipStream_t st);
 hipError_t launch_compact(const Dims& dm, const madakv_config& c, void* k_c, void* v_c, int32_t* kept_idx, const int32_t* sel,
-                          const int64_t* seg_off, int32_t* kv_len, const int32_t* budgets, long long cache_rows, int appended, int gen_base, hipStream_t st);
+                          const int64_t* seg_off, int32_t* kv_len, const int32_t* budgets, long long cache_rows, const int32_t* len1, int appended, hipStream_t st);
 hipError_t launch_linear_copy(const Dims& dm, const madakv_config& c, void* k_c, void* v_c, int32_t* kept_idx, const int64_t* seg_off,
                               const int32_t* seg_len, const Paging& pg, long long head0, int longest, void* k_lin, void* v_lin,
                               int32_t* kept_lin, int64_t* lin_off, bool back, hipStream_t st);

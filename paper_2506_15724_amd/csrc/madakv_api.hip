@@ -25,7 +25,6 @@ struct madakv_handle {
   // per layer: rows have taken the places of others since the last eviction (1), or do so whenever a captured step is replayed
   // (2, for good: nobody tells the host of replays), so that they are not in order of position
   std::vector<uint8_t> replaced;
-  std::vector<int32_t> gen_base;   // tokens generated before that, per layer (their original positions are ctx_len + 0, 1, ...)
   // Longest head of each layer after eviction: stored by the layout kernel in pinned host memory (d_maxlen is its
   // device address); decode sizes its grid from it once it is known to have landed
   // (event query, never a wait) and from the budget before that.
@@ -335,7 +334,6 @@ int32_t madakv_create(const madakv_config* cfg, madakv_handle** out) {
   h->side = nullptr; h->ev_fork = nullptr; h->ev_join = nullptr;
   for (int g = 0; g < MAX_GROUPS; ++g) { h->ev_grp[g] = nullptr; h->ev_sel[g] = nullptr; }
   h->appended.assign(cfg->n_layers, 0);
-  h->gen_base.assign(cfg->n_layers, 0);
   h->replaced.assign(cfg->n_layers, 0);
   h->replays.assign(cfg->n_layers, 0);
   h->xchg = nullptr; h->xchg_words = 0; h->xchg_left = false;
@@ -601,7 +599,7 @@ int32_t madakv_select_gather(madakv_handle* h, int32_t layer0, int32_t n,
     if (e == hipSuccess) e = launch_gather(dg, c, 0, ng, kg, vg, kept_idx, kv_off + heads0, kv_len + heads0, k_c, v_c, ws_g, region, bpb, bpb, st, overlap);
   }
   if (overlap && e != hipSuccess) e = join_side(h, st, e);   // an enqueue failed: whatever did reach the side stream is still joined
-  for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] = 0; h->gen_base[l] = 0; h->replaced[l] &= ~1; }
+  for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] = 0; h->replaced[l] &= ~1; }
   e = publish_maxlen(h, layer0, n, st, e);
   return hip_fail(h, e);
 }
@@ -680,7 +678,7 @@ int32_t madakv_evict(madakv_handle* h, int32_t layer0, int32_t n,
   }
   if (e == hipSuccess) gather_group(ngroups - 1);
   if (overlap && e != hipSuccess) e = join_side(h, st, e);   // an enqueue failed: whatever did reach the side stream is still joined
-  for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] = 0; h->gen_base[l] = 0; h->replaced[l] &= ~1; }
+  for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] = 0; h->replaced[l] &= ~1; }
   e = publish_maxlen(h, layer0, n, st, e);
   return hip_fail(h, e);
 }
@@ -783,13 +781,13 @@ int32_t madakv_reevict(madakv_handle* h, int32_t layer0, int32_t n,
     if (h->replaced[l]) return MADAKV_ERR_INVALID_ARG;                     // the last rows of a segment are no longer the newest
   // a paged cache hands the pages taken since the eviction back to the pools, which all layers share
   if (c.page_rows && (layer0 != 0 || n != c.n_layers)) return MADAKV_ERR_INVALID_ARG;
-  int longest = longest_rows(h, layer0, n);
+  int longest = longest_rows(h, layer0, n, false, true);
   if (!score_ragged_supported(make_dims(c, n), c, longest)) {
     // the bound may be the worst case only because the lengths of the eviction have not reached the host
     // yet: this call is rare enough to wait for them once
     bool pending = false;
     for (int l = layer0; l < layer0 + n; ++l) pending = pending || h->maxlen_state[l] == 1;
-    if (pending && hipEventSynchronize(h->maxlen_event) == hipSuccess) longest = longest_rows(h, layer0, n);
+    if (pending && hipEventSynchronize(h->maxlen_event) == hipSuccess) longest = longest_rows(h, layer0, n, false, true);
     if (!score_ragged_supported(make_dims(c, n), c, longest)) return MADAKV_ERR_UNIMPLEMENTED;
   }
   const ReevictWs w = reevict_layout(h, n);
@@ -814,7 +812,7 @@ int32_t madakv_reevict(madakv_handle* h, int32_t layer0, int32_t n,
   // layers that have appended the same number of rows since their last (re-)eviction go in one set of launches
   for (int l0 = layer0; l0 < layer0 + n && e == hipSuccess;) {
     int l1 = l0 + 1;
-    while (l1 < layer0 + n && h->appended[l1] == h->appended[l0] && h->gen_base[l1] == h->gen_base[l0]) ++l1;
+    while (l1 < layer0 + n && h->appended[l1] == h->appended[l0]) ++l1;
     const Dims dr = make_dims(c, l1 - l0);
     const size_t heads0 = (size_t)(l0 - layer0) * c.batch * c.n_kv_heads;
     const char* qr = static_cast<const char*>(q_recent) + (size_t)(l0 - layer0) * c.batch * c.n_q_heads * c.window * c.head_dim * es;
@@ -828,12 +826,12 @@ int32_t madakv_reevict(madakv_handle* h, int32_t layer0, int32_t n,
       k_score = wsb + w.dec_k;
     }
     if (e == hipSuccess) e = launch_score_ragged(dr, c, qr, k_score, off_work + heads0, kv_len + heads0, longest, cache_rows, psi_c, wsb + w.score, st);
-    if (e == hipSuccess) e = launch_restats(dr, c, psi_c, idx_work, mask, off_work + heads0, kv_len + heads0, h->appended[l0], pool_c, rowmod,
+    if (e == hipSuccess) e = launch_restats(dr, c, psi_c, idx_work, mask, off_work + heads0, kv_len + heads0, len1_of(h, l0), h->appended[l0], pool_c, rowmod,
                                             stats_r, bud_r, st);
     if (e == hipSuccess) e = launch_select(dr, c, pool_c, mask, bud_r, off_work + heads0, kv_len + heads0, sel, st, kv_len + heads0, rowmod);
-    if (e == hipSuccess) e = launch_compact(dr, c, k_work, v_work, idx_work, sel, off_work + heads0, kv_len + heads0, bud_r, cache_rows, h->appended[l0],
-                                            h->gen_base[l0], st);
-    if (e == hipSuccess) for (int l = l0; l < l1; ++l) { h->gen_base[l] += h->appended[l]; h->appended[l] = 0; }
+    if (e == hipSuccess) e = launch_compact(dr, c, k_work, v_work, idx_work, sel, off_work + heads0, kv_len + heads0, bud_r, cache_rows,
+                                            len1_of(h, l0), h->appended[l0], st);
+    if (e == hipSuccess) for (int l = l0; l < l1; ++l) h->appended[l] = 0;
     l0 = l1;
   }
   if (c.page_rows && e == hipSuccess) {

@@ -8,6 +8,10 @@
 // best-scored candidates per modality survive (ties: lower row).  Everything is per head: nothing
 // couples heads or layers here.
 //
+// How many of a head's rows are appended ones is what the eviction left it (Meet::len1) and its length now say, and which tokens they
+// are follows from the position of the row in front of them, the newest before them: a captured step appends rows whenever its
+// graph is replayed, and the host sees none of that.
+//
 //   restats_kernel   per head: modality of every row (from the row's original position: a prompt
 //                    position looks up the modality mask, a generated token is text), masses and counts
 //                    over the candidates, pooled scores, then the Eq. 8 split of the unchanged total
@@ -31,8 +35,13 @@ constexpr float RE_PSI_MAX = 256.0f;
 struct RestatsArgs {
   const float* psi; const int32_t* kept_idx; const uint8_t* mask; const int64_t* seg_off; const int32_t* seg_len;
   float* psi_pool; uint8_t* rowmod; void* stats; int32_t* budgets;
+  const int32_t* len1;
   int B, H, L, W, M, appended, pool_r, pool_mode, share_mode, mpa_mode;
 };
+
+// Rows of a head before the appended ones.  len1: 1 + the rows the eviction left it, 0 where this handle has not seen one: the
+// host's count then.
+__device__ __forceinline__ int rows_before(int len, int len1, int appended) { return len1 > 0 ? min(len, len1 - 1) : len - appended; }
 
 __device__ __forceinline__ unsigned long long re_to_fx(float v) {
   v = fminf(fmaxf(v, 0.f), RE_PSI_MAX);
@@ -48,7 +57,7 @@ __global__ __launch_bounds__(RE_THREADS) void restats_kernel(RestatsArgs a) {
   const int len = a.seg_len[head];
   if (len <= 0) return;                                     // an empty segment stays empty
   const long long off = a.seg_off[head];
-  const int len0 = len - a.appended;                        // rows before the appended ones: they have original positions
+  const int len0 = rows_before(len, a.len1[head], a.appended);      // rows before the appended ones: they have original positions
   const int nc = len - a.W;                                 // candidates: everything before the new window
   if (tid < 4) { s_w[tid] = 0ULL; s_n[tid] = 0u; }
   __syncthreads();
@@ -104,7 +113,8 @@ typedef __attribute__((ext_vector_type(4))) unsigned int ru32x4_t;
 struct CompactArgs {
   void* k_c; void* v_c; int32_t* kept_idx; const int32_t* sel; const int64_t* seg_off; int32_t* kv_len; const int32_t* budgets;
   long long cache_rows;      // 4-bit cache: the scales are behind the codes of so many rows
-  int W, M, L, appended, gen_base;
+  const int32_t* len1;
+  int W, M, L, appended;
 };
 
 template <int LPR, typename ST = void>   // 16-byte pieces per row; ST: the scales of a row of the 4-bit cache, as one word
@@ -117,7 +127,8 @@ __global__ __launch_bounds__(RE_THREADS) void compact_kernel(CompactArgs a) {
   const int len = a.kv_len[head];
   if (len <= 0) return;
   const long long off = a.seg_off[head];
-  const int len0 = len - a.appended;
+  const int len0 = rows_before(len, a.len1[head], a.appended);
+  const int newest = len0 > 0 ? a.kept_idx[off + len0 - 1] : a.L - 1;     // the position before those of the appended rows
   int keep = a.W;
   for (int m = 0; m < a.M; ++m) keep += a.budgets[(long long)head * a.M + m];
   const int sub = tid / LPR, piece = tid % LPR;
@@ -145,9 +156,8 @@ __global__ __launch_bounds__(RE_THREADS) void compact_kernel(CompactArgs a) {
       kr[u] = kc[(off + src) * LPR + piece];
       vr[u] = vc[(off + src) * LPR + piece];
       if constexpr (!std::is_void_v<ST>) if (piece < 2) sr[u] = reinterpret_cast<const ST*>((piece ? vc : kc) + a.cache_rows * LPR)[off + src];
-      // original position: prompt rows and earlier generated rows carry theirs; rows appended since the
-      // last (re-)eviction are generated tokens gen_base, gen_base + 1, ... after the prompt
-      org[u] = src < len0 ? a.kept_idx[off + src] : a.L + a.gen_base + (src - len0);
+      // original position: prompt rows and earlier generated rows carry theirs, rows appended since the last (re-)eviction follow on
+      org[u] = src < len0 ? a.kept_idx[off + src] : newest + 1 + (src - len0);
     }
     __syncthreads();                              // every row of the batch is in registers before any is overwritten
 #pragma unroll
@@ -165,23 +175,24 @@ __global__ __launch_bounds__(RE_THREADS) void compact_kernel(CompactArgs a) {
 }
 
 hipError_t launch_restats(const Dims& dm, const madakv_config& c, const float* psi_c, const int32_t* kept_idx, const uint8_t* mask,
-                          const int64_t* seg_off, const int32_t* seg_len, int appended, float* pool_c, uint8_t* rowmod,
+                          const int64_t* seg_off, const int32_t* seg_len, const int32_t* len1, int appended, float* pool_c, uint8_t* rowmod,
                           void* stats, int32_t* budgets, hipStream_t st) {
   RestatsArgs a;
   a.psi = psi_c; a.kept_idx = kept_idx; a.mask = mask; a.seg_off = seg_off; a.seg_len = seg_len; a.psi_pool = pool_c;
   a.rowmod = rowmod; a.stats = stats; a.budgets = budgets;
   a.B = dm.B; a.H = dm.H; a.L = dm.L; a.W = dm.W; a.M = c.n_modalities; a.appended = appended;
   a.pool_r = (c.pool_k - 1) / 2; a.pool_mode = c.pool_mode; a.share_mode = c.share_mode; a.mpa_mode = c.mpa_mode;
+  a.len1 = len1;
   hipLaunchKernelGGL(restats_kernel, dim3(dm.heads), dim3(RE_THREADS), 0, st, a);
   return hipGetLastError();
 }
 
 hipError_t launch_compact(const Dims& dm, const madakv_config& c, void* k_c, void* v_c, int32_t* kept_idx, const int32_t* sel,
-                          const int64_t* seg_off, int32_t* kv_len, const int32_t* budgets, long long cache_rows, int appended, int gen_base, hipStream_t st) {
+                          const int64_t* seg_off, int32_t* kv_len, const int32_t* budgets, long long cache_rows, const int32_t* len1, int appended, hipStream_t st) {
   CompactArgs a;
   a.cache_rows = cache_rows;
   a.k_c = k_c; a.v_c = v_c; a.kept_idx = kept_idx; a.sel = sel; a.seg_off = seg_off; a.kv_len = kv_len; a.budgets = budgets;
-  a.W = dm.W; a.M = c.n_modalities; a.L = dm.L; a.appended = appended; a.gen_base = gen_base;
+  a.W = dm.W; a.M = c.n_modalities; a.L = dm.L; a.appended = appended; a.len1 = len1;
   const int lpr = cache_row_bytes(c) / 16;     // 16-byte pieces per cached row
   if (c.cache_fp8 == CACHE_E2M1) {
     if (lpr == 4) hipLaunchKernelGGL((compact_kernel<4, uint32_t>), dim3(dm.heads), dim3(RE_THREADS), 0, st, a);

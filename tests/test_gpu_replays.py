@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2506_15724_amd import binding as MB
 from tests.test_gpu_operators import DEV, make, row_numbers, say, values
 
 pytestmark = pytest.mark.gpu
@@ -53,3 +54,53 @@ def test_rows_read_back_after_replayed_appends(kind, P, weights):
         assert (rows.cpu()[rest] == 77.0).all()
     del graph
     eng.close()
+
+
+@pytest.mark.parametrize("kw,weights", [(dict(), False), (dict(cache_fp8=4), True), (dict(cache_fp8=1, page_rows=16), False), (dict(cache_fp8=4, page_rows=16), False),
+                                        (dict(page_rows=64), True)])
+def test_reeviction_after_replayed_appends(kw, weights):
+    """Twice, 30 and 17 replays of a captured step in front of it: lengths, budgets, positions and rows as after the same steps taken
+    by calls, and the eager steps behind it give the same outputs."""
+    NL, B, Hq, H, d, L, W, T = 2, 2, 4, 2, 64, 500, 8, 40
+    args = dict(n_layers=NL, batch=B, n_q_heads=Hq, n_kv_heads=H, head_dim=d, page_rows=kw.get("page_rows", 0), cache_fp8=kw.get("cache_fp8", 0))
+    g = torch.Generator(device=DEV).manual_seed(L)
+    randn = lambda *s: torch.randn(*s, generator=g, device=DEV).to(torch.bfloat16)        # noqa: E731
+    q, k, v = randn(NL, B, Hq, W, d), randn(NL, B, H, L, d), randn(NL, B, H, L, d)
+    mask = torch.randint(0, 2, (B, L), generator=g, device=DEV).to(torch.uint8)
+    eager, graphed = (MB.MadaKV(n_layers=NL, batch=B, n_q_heads=Hq, n_kv_heads=H, head_dim=d, ctx_len=L, window=W, budget=100, max_new_tokens=T, device=DEV, **kw) for _ in range(2))
+    for e in (eager, graphed):
+        e.kept_idx.zero_()                              # (a position nobody has written reads as one)
+        e.evict(0, NL, q, k, v, mask)
+    len0 = eager.kv_len.clone()
+    graph, x, out, replay = captured_append(graphed, args, weights)
+    out_e = torch.zeros_like(out)
+    for round_, times in enumerate((30, 17)):
+        for i in range(times):
+            replay(1, torch.Generator().manual_seed(100 * round_ + i))
+            eager.decode_attn(0, NL, *x, out_e)
+        torch.cuda.synchronize()
+        recent = randn(NL, B, Hq, W, d)
+        say(f"re-eviction after {times} replays {kw} weights={weights}")
+        assert torch.equal(graphed.kv_len, len0 + times)
+        for e in (eager, graphed):
+            e.reevict(0, NL, recent, mask)
+        torch.cuda.synchronize()
+        for e in (eager, graphed):
+            assert torch.equal(e.kv_len, len0)
+        assert torch.equal(eager.budgets, graphed.budgets)
+        for i in range(NL * B * H):
+            a, b = row_numbers(eager, args, i), row_numbers(graphed, args, i)
+            pos = eager.kept_idx.cpu()[a]
+            assert torch.equal(pos, graphed.kept_idx.cpu()[b])
+            assert (pos[1:] > pos[:-1]).all() and int(pos[-1]) == L + (30, 47)[round_] - 1         # (the newest token is always kept)
+            for name in ("k_c", "v_c"):
+                assert torch.equal(values(eager, args, name)[a], values(graphed, args, name)[b])
+        for step in range(2):
+            y = randn(NL, B, Hq, d), randn(NL, B, H, d), randn(NL, B, H, d)
+            outs = [torch.zeros(NL, B, Hq, d, device=DEV) for _ in range(2)]
+            for e, o in zip((eager, graphed), outs):
+                e.decode_attn(0, NL, y[0], None, None, o)
+            torch.cuda.synchronize()
+            assert torch.isfinite(outs[0]).all() and torch.equal(*outs)
+    del graph
+    eager.close(), graphed.close()

@@ -35,3 +35,36 @@ for _ in range(2):
 print("ok")
 """, good(max_new_tokens=200, **kw))
     assert out.strip() == "ok"
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(page_rows=16), dict(cache_fp8=4)])
+def test_reeviction_covers_replayed_appends(runtime, kw):  # noqa: F811
+    """madakv_reevict after a captured append: its kernels over rows of a head cover every row that replays can have left."""
+    out = scenario(runtime, CALLS + """
+h = create(sys.argv[3])
+fake.fake_events_done(1)
+re = lambda: lib.madakv_reevict(h, I(0), I(2), *[P(T().p) for _ in range(8)], P(T().p), Z(1 << 40), P(0))
+def widest():
+    found = {}
+    for x in log():
+        if x.kind == "launch":
+            for part in ("cache_rows", "linear_copy", "write_back", "score_fused"):
+                if part in x.rest[3]: found.setdefault(part, int(x.rest[1].split(",")[0]))
+    return found
+assert evict(h) == 0 and plain(h) == 0
+widest()
+assert re() == 0
+before = widest()
+fake.fake_capture(P(st))
+assert plain(h, 0, 1, st) == 0
+fake.fake_capture(P(0))
+widest()
+for _ in range(2):
+    assert re() == 0
+    after = widest()
+    assert before.keys() == after.keys() and "score_fused" in after
+    assert all(v == 1 for v in before.values()), before
+    assert all(v == (-(-5000 // 64) if x != "score_fused" else -(-5000 // 1024)) for x, v in after.items()), after
+print("ok")
+""", good(max_new_tokens=5000, **kw))
+    assert out.strip() == "ok"
