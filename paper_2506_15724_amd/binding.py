@@ -356,6 +356,15 @@ class MadaKV:
         # (once per layer and token, like decode_attn: no views of the own buffers)
         heads = n * self._heads
         self._check_out(out, n * self._out_row)
+        # (the step's own arrays in one expression: a call of _check_array for each of them is 1 us of the 12 that a step takes on the host)
+        dt, at, nq, nkv = self.tdtype, self._device.index, n * self._out_row, n * self._kv_row
+        if (out.get_device() != at or q.dtype is not dt or q.numel() < nq or q.get_device() != at
+                or (k_new is not None and (k_new.dtype is not dt or k_new.numel() < nkv or k_new.get_device() != at))
+                or (v_new is not None and (v_new.dtype is not dt or v_new.numel() < nkv or v_new.get_device() != at))):
+            self._check_array("out", out, nq, self._out_dtype)
+            self._check_array("q", q, nq, dt)
+            self._check_array("k_new", k_new, nkv, dt)
+            self._check_array("v_new", v_new, nkv, dt)
         self._check_array("acc_in", acc_in, self.capacity, torch.float32)
         if acc_out is not acc_in:
             self._check_array("acc_out", acc_out, self.capacity, torch.float32)
