@@ -137,8 +137,10 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(N
   const uint32_t ring = (uint32_t)(uintptr_t)smem;
   const uint32_t ring_n = ring + PR_RING * TILEB;
   // tile T -> ring slot T mod 3: load j of wave w fills bytes [(w LPT + j) 1024, + 1024) of the slot, lane i slot P mod PPR of row P / PPR,
-  // P = (w LPT + j) 64 + i, with that row's piece (P mod PPR) ^ (row mod PPR).  Through a buffer that ends with the prompt: rows
-  // past its end are zeros, and a lane's offset in a tile is the same for all tiles.
+  // P = (w LPT + j) 64 + i, with that row's piece (P mod PPR) ^ (row mod PPR).  Through a buffer that ends with the prompt: keys
+  // past its end are zeros, and a lane's offset in a tile is the same for all tiles but a last one that is not whole, whose queries past
+  // the end are the last one again: their normalisers make nothing of a logit of any size, but zeros times an infinite key would be
+  // no number.
   const __amdgpu_buffer_rsrc_t rows_buf = buffer_of(rows, a.L * ROWB), norm_buf = buffer_of(a.lse2 + (long long)qh * a.rows, a.rows * 4);
   int piece_off[LPT];
 #pragma unroll
@@ -149,9 +151,18 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(N
   const auto issue = [&](int t) {
     const int r0 = row0 + t * PR_TILE;
     const uint32_t slot = (uint32_t)(t % PR_RING);
+    const auto load = [&](int j, int at) { to_lds16(rows_buf, ring + slot * TILEB + (uint32_t)(wave * LPT + j) * 1024u, at, r0 * ROWB); };
+    if (PASS == 2 && __builtin_expect(r0 + PR_TILE > a.L, 0)) {
 #pragma unroll
-    for (int j = 0; j < LPT; ++j)
-      to_lds16(rows_buf, ring + slot * TILEB + (uint32_t)(wave * LPT + j) * 1024u, piece_off[j], r0 * ROWB);
+      for (int j = 0; j < LPT; ++j) {
+        int at = piece_off[j];
+        asm volatile("" : "+v"(at));            // (made here: kept over the loop, its parts would take registers)
+        load(j, min(at & -ROWB, (a.L - 1 - r0) * ROWB) + (at & (ROWB - 1)));
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < LPT; ++j) load(j, piece_off[j]);
+    }
     if (PASS == 2 && !OWN_NORM)                 // the rows' normalisers, every wave its own copy
       to_lds4(norm_buf, ring_n + (slot * PR_WAVES + wave) * (PR_TILE * 4u), lane * 4, r0 * 4);
   };
