@@ -151,8 +151,9 @@ int32_t madakv_destroy(madakv_handle* h);
 /* hipError_t of the last failing HIP call made through this handle (0 if none). */
 int32_t madakv_last_hip_error(const madakv_handle* h);
 
-/* Bytes of caller-provided scratch each call needs when it covers n layers (the
- * worst case over layer ranges of that size).  Any out pointer may be NULL. */
+/* Bytes of caller-provided scratch that serve calls over up to n layers (the worst case over all
+ * such layer ranges: a call over fewer layers can need more than one over n).  So do the other calls named
+ * madakv_*_workspace_bytes.  Any out pointer may be NULL. */
 int32_t madakv_workspace_bytes(const madakv_handle* h, int32_t n_layers_per_call,
                                size_t* score_ws, size_t* select_ws, size_t* decode_ws);
 
@@ -232,7 +233,7 @@ int32_t madakv_window_attn_score(madakv_handle* h, int32_t layer0, int32_t n,
  * mask, psi_pool, stats, n_mod: all NULL (the scores alone), or as in madakv_score, for madakv_allocate and
  * madakv_select_gather to go on with; they are those of psi * 2^-s, s the least with W * 2^s >= L, so that they have the
  * range that W proxy tokens give (budgets, counts and rankings do not depend on it).
- *   ws       madakv_score_prompt_workspace_bytes(h, n) bytes (enough for calls over fewer layers as well)
+ *   ws       madakv_score_prompt_workspace_bytes(h, n) bytes
  * A row's normaliser is one float: a weight is off by 2^-24 of the magnitude of its row's log-sum-exp, relative to the weight (1e-5 at 200).
  * MADAKV_ERR_UNIMPLEMENTED unless dtype is bf16. */
 int32_t madakv_score_prompt_workspace_bytes(const madakv_handle* h, int32_t n_layers_per_call, size_t* bytes);

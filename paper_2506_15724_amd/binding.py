@@ -249,7 +249,6 @@ class MadaKV:
         self._out_row, self._heads, self._kv_row, self._ctx = batch * n_q_heads * head_dim, batch * n_kv_heads, batch * n_kv_heads * head_dim, ctx_len
         self.n_call = layers_per_call or n_layers
         s_ws, sel_ws, d_ws = madakv_workspace_bytes(self.h, self.n_call)
-        d_ws = max(madakv_workspace_bytes(self.h, m)[2] for m in range(1, self.n_call + 1))       # (longer pieces of more heads: not always the most layers')
         dev = self.device
         self.score_ws = torch.empty(max(s_ws, 16), dtype=torch.uint8, device=dev)
         self.select_ws = torch.empty(max(sel_ws, 16), dtype=torch.uint8, device=dev)
@@ -373,8 +372,7 @@ class MadaKV:
             self._check_array("slot_out", slot_out, heads, torch.int32)
         self._check_array("pos", pos, self.cfg.batch, torch.int32)
         if getattr(self, "weights_ws", None) is None:
-            need = max(madakv_decode_attn_weights_workspace_bytes(self.h, m) for m in range(1, self.n_call + 1))
-            self.weights_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+            self.weights_ws = torch.empty(madakv_decode_attn_weights_workspace_bytes(self.h, self.n_call), dtype=torch.uint8, device=self.device)
         heads0, ws = l0 * self._heads, self.weights_ws
         rc = lib().madakv_decode_attn_weights(
             self.h, l0, n, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(self.k_c), _ptr(self.v_c), _ptr(self.kv_off) + 8 * heads0, _ptr(self.kv_len) + 4 * heads0,

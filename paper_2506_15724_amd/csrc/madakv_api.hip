@@ -182,6 +182,15 @@ int largest_group(const madakv_config& c, int n) {
   return m;
 }
 
+// What a workspace for up to n layers per call has to hold.  Layer groups, the pieces of a head and the plans of the scoring kernels
+// follow the heads of a call: what calls over fewer layers need is not always less.
+template <typename F>
+size_t most_over_calls(int n, F need) {
+  size_t most = 0;
+  for (int m = 1; m <= n; ++m) most = std::max(most, need(m));
+  return most;
+}
+
 size_t window_ws_for_call(const madakv_config& c, int n) {
   int b[MAX_GROUPS + 1];
   const int ng = layer_groups(c, n, b);
@@ -393,15 +402,17 @@ int32_t madakv_last_hip_error(const madakv_handle* h) { return h ? h->last_hip_e
 int32_t madakv_workspace_bytes(const madakv_handle* h, int32_t n_layers_per_call,
                                size_t* score_ws, size_t* select_ws, size_t* decode_ws) {
   if (!h || n_layers_per_call < 1 || n_layers_per_call > h->cfg.n_layers) return MADAKV_ERR_INVALID_ARG;
-  Dims dm = make_dims(h->cfg, n_layers_per_call);
-  if (score_ws) *score_ws = score_ws_for_call(h->cfg, n_layers_per_call);
+  const madakv_config& c = h->cfg;
+  const int n = n_layers_per_call;
+  if (score_ws) *score_ws = most_over_calls(n, [&](int m) { return score_ws_for_call(c, m); });
   if (select_ws) {
     // enough for madakv_select_gather over n layers and for madakv_evict (one slice per layer group)
-    const int gl = largest_group(h->cfg, n_layers_per_call);
-    const size_t slices = ((select_ws_bytes(make_dims(h->cfg, gl), h->cfg) + 255) / 256 * 256) * MAX_GROUPS;
-    *select_ws = std::max(select_ws_bytes(dm, h->cfg), slices);
+    *select_ws = most_over_calls(n, [&](int m) {
+      const size_t slices = ((select_ws_bytes(make_dims(c, largest_group(c, m)), c) + 255) / 256 * 256) * MAX_GROUPS;
+      return std::max(select_ws_bytes(make_dims(c, m), c), slices);
+    });
   }
-  if (decode_ws) *decode_ws = decode_ws_bytes(dm, h->cfg);
+  if (decode_ws) *decode_ws = most_over_calls(n, [&](int m) { return decode_ws_bytes(make_dims(c, m), c); });
   return MADAKV_OK;
 }
 
@@ -487,7 +498,7 @@ int32_t madakv_score_lse(madakv_handle* h, int32_t layer0, int32_t n,
 
 int32_t madakv_window_attn_workspace_bytes(const madakv_handle* h, int32_t n_layers_per_call, size_t* bytes) {
   if (!h || !bytes || n_layers_per_call < 1 || n_layers_per_call > h->cfg.n_layers) return MADAKV_ERR_INVALID_ARG;
-  *bytes = window_ws_for_call(h->cfg, n_layers_per_call);
+  *bytes = most_over_calls(n_layers_per_call, [&](int m) { return window_ws_for_call(h->cfg, m); });
   return MADAKV_OK;
 }
 
@@ -500,16 +511,9 @@ int32_t madakv_window_attn_score(madakv_handle* h, int32_t layer0, int32_t n,
   return score_impl(h, layer0, n, q_win, k, mask, nullptr, psi, psi_pool, stats, n_mod, ws, ws_bytes, stream, v, out, row_lse);
 }
 
-// The plan of a launch follows the heads in it: what calls over fewer layers need is not always less.
-static size_t prompt_ws_for(const madakv_config& c, int n) {
-  size_t need = 0;
-  for (int m = 1; m <= n; ++m) need = std::max(need, prompt_ws_bytes(make_dims(c, m)));
-  return need;
-}
-
 int32_t madakv_score_prompt_workspace_bytes(const madakv_handle* h, int32_t n_layers_per_call, size_t* bytes) {
   if (!h || !bytes || n_layers_per_call < 1 || n_layers_per_call > h->cfg.n_layers) return MADAKV_ERR_INVALID_ARG;
-  *bytes = prompt_ws_for(h->cfg, n_layers_per_call);
+  *bytes = most_over_calls(n_layers_per_call, [&](int m) { return prompt_ws_bytes(make_dims(h->cfg, m)); });
   return MADAKV_OK;
 }
 
@@ -700,7 +704,7 @@ int32_t madakv_decode_attn_static(madakv_handle* h, int32_t layer0, int32_t n,
 
 int32_t madakv_decode_attn_weights_workspace_bytes(const madakv_handle* h, int32_t n_layers_per_call, size_t* bytes) {
   if (!h || !bytes || n_layers_per_call < 1 || n_layers_per_call > h->cfg.n_layers) return MADAKV_ERR_INVALID_ARG;
-  *bytes = weights_ws_bytes(make_dims(h->cfg, n_layers_per_call), h->cfg);
+  *bytes = most_over_calls(n_layers_per_call, [&](int m) { return weights_ws_bytes(make_dims(h->cfg, m), h->cfg); });
   return MADAKV_OK;
 }
 
@@ -763,7 +767,7 @@ ReevictWs reevict_layout(const madakv_handle* h, int n) {
 
 int32_t madakv_reevict_workspace_bytes(const madakv_handle* h, int32_t n_layers_per_call, size_t* bytes) {
   if (!h || !bytes || n_layers_per_call < 1 || n_layers_per_call > h->cfg.n_layers) return MADAKV_ERR_INVALID_ARG;
-  *bytes = reevict_layout(h, n_layers_per_call).total;
+  *bytes = most_over_calls(n_layers_per_call, [&](int m) { return reevict_layout(h, m).total; });
   return MADAKV_OK;
 }
 
