@@ -105,7 +105,8 @@ bool window_attn_supported(const Dims& dm, const madakv_config& c);
 size_t window_attn_ws_bytes(const Dims& dm, const madakv_config& c);
 hipError_t launch_window_attn(const Dims& dm, const madakv_config& c, const void* q_win, const void* k, const void* v,
                               void* out, float* row_lse, float* psi, void* ws, Exchange& x, hipStream_t st);
-hipError_t launch_restats(const Dims& dm, const madakv_config& c, const float* psi_c, const int32_t* kept_idx, const uint8_t* mask,
+// psi_off: where the scores of every head are
+hipError_t launch_restats(const Dims& dm, const madakv_config& c, const float* psi_c, const int64_t* psi_off, const int32_t* kept_idx, const uint8_t* mask,
                           const int64_t* seg_off, const int32_t* seg_len, const int32_t* len1, int appended, float* pool_c, uint8_t* rowmod,
                           void* stats, int32_t* budgets, hipStream_t st);
 hipError_t launch_compact(const Dims& dm, const madakv_config& c, void* k_c, void* v_c, int32_t* kept_idx, const int32_t* sel,
@@ -123,9 +124,12 @@ bool prompt_supported(const madakv_config& c);
 size_t prompt_ws_bytes(const Dims& dm);
 hipError_t launch_prompt(const Dims& dm, const madakv_config& c, const void* q, const void* k, const float* row_lse, float* psi,
                          void* ws, float factor, float** scaled, hipStream_t st);
-// v_rows null: K alone
+// v_rows null: K alone.  to_off null: rows go to the places they have in the cache; else (contiguous segments) into the first
+// cache_rows_front rows, whatever layers the call is over, and to_off gets the first row of every head
+long long cache_rows_front(const Dims& dm, const madakv_config& c);
 hipError_t launch_cache_rows(const Dims& dm, const madakv_config& c, const void* k_c, const void* v_c, const int64_t* kv_off, const int32_t* kv_len,
-                             void* k_rows, void* v_rows, long long capacity_tokens, int longest_rows, const Paging& pg, int layer0, hipStream_t st);
+                             void* k_rows, void* v_rows, long long capacity_tokens, int longest_rows, const Paging& pg, int layer0, hipStream_t st,
+                             int64_t* to_off = nullptr);
 // A decode step that adds up the weights it pays (weights.hip).  The first seven are the caller's, the others point into the workspace.
 struct WeightArgs {
   const float* acc_in; float* acc_out; const int32_t* slot_in; int32_t* slot_out; int32_t* kept_idx; const int32_t* pos;

@@ -191,6 +191,10 @@ struct RowsArgs {
   const void* k_c; const void* v_c; const int64_t* kv_off; const int32_t* kv_len; u32x4_t* k_rows; u32x4_t* v_rows;
   long long capacity;
   const int32_t* page_tbl; int entries, shift;      // of the call's first head; null without paging
+  // null: rows go to the places they have in the cache.  Else: those of a batch item's heads (contiguous segments) to the front of its item_rows
+  // rows, and where those of every head begin is left here
+  int64_t* to_off;
+  long long item_rows; int B, H, head0;             // head0: the launch's first head of the call
 };
 constexpr int ROWS_PER_BLOCK = 64;
 
@@ -199,8 +203,15 @@ __global__ __launch_bounds__(256) void cache_rows_kernel(RowsArgs a) {
   constexpr int RPI = 256 / LPR, ITERS = ROWS_PER_BLOCK / RPI;
   const int head = blockIdx.y, len = a.kv_len[head];
   const int r0 = blockIdx.x * ROWS_PER_BLOCK;
-  if (r0 >= len) return;
   const long long off = a.kv_off[head];
+  long long to = 0;
+  if (a.to_off) {
+    const int item = (a.head0 + head) / a.H % a.B;
+    // (a batch item's segments follow each other: from the first of the call's on they fit its rows)
+    to = min(max(off - a.kv_off[item * a.H - a.head0], 0ll), a.item_rows - max(len, 0)) + item * a.item_rows;
+    if (r0 == 0 && threadIdx.x == 0) a.to_off[head] = to;
+  }
+  if (r0 >= len) return;
   const int32_t* tbl = a.page_tbl ? a.page_tbl + (long long)head * a.entries : nullptr;
   const int init_rows = tbl ? tbl[0] << a.shift : 0x7fffffff;
   const int sub = threadIdx.x / LPR, piece = threadIdx.x % LPR;
@@ -233,6 +244,10 @@ __global__ __launch_bounds__(256) void cache_rows_kernel(RowsArgs a) {
       vv[it] = u32x4_t{pair(v8[0], false), pair(v8[0], true), pair(v8[1], false), pair(v8[1], true)};
     }
   }
+  if (a.to_off) {
+#pragma unroll
+    for (int it = 0; it < ITERS; ++it) at[it] = to + r0 + it * RPI + sub;
+  }
 #pragma unroll
   for (int it = 0; it < ITERS; ++it) {
     if (r0 + it * RPI + sub < len) {
@@ -242,9 +257,14 @@ __global__ __launch_bounds__(256) void cache_rows_kernel(RowsArgs a) {
   }
 }
 
+// most rows of a batch item that the call's heads hold, free ones included
+static long long front_rows(const Dims& dm, const madakv_config& c) { return std::min(region_tokens_of(c), (long long)dm.n * dm.H * (c.ctx_len + c.max_new_tokens)); }
+long long cache_rows_front(const Dims& dm, const madakv_config& c) { return dm.B * front_rows(dm, c); }
 hipError_t launch_cache_rows(const Dims& dm, const madakv_config& c, const void* k_c, const void* v_c, const int64_t* kv_off, const int32_t* kv_len,
-                             void* k_rows, void* v_rows, long long capacity_tokens, int longest_rows, const Paging& pg, int layer0, hipStream_t st) {
+                             void* k_rows, void* v_rows, long long capacity_tokens, int longest_rows, const Paging& pg, int layer0, hipStream_t st,
+                             int64_t* to_off) {
   RowsArgs a;
+  a.to_off = to_off; a.B = dm.B; a.H = dm.H; a.item_rows = front_rows(dm, c);
   a.k_c = k_c; a.v_c = v_c; a.kv_off = kv_off; a.kv_len = kv_len; a.capacity = capacity_tokens;
   a.k_rows = static_cast<u32x4_t*>(k_rows); a.v_rows = static_cast<u32x4_t*>(v_rows);
   a.entries = pg.entries; a.shift = 0;
@@ -254,6 +274,8 @@ hipError_t launch_cache_rows(const Dims& dm, const madakv_config& c, const void*
   for (int h0 = 0; h0 < dm.heads; h0 += 32768) {
     RowsArgs b = a;
     b.kv_off += h0; b.kv_len += h0;
+    if (b.to_off) b.to_off += h0;
+    b.head0 = h0;
     if (b.page_tbl) b.page_tbl += (long long)h0 * a.entries;
     const dim3 grid((unsigned)((std::max(longest_rows, 1) + ROWS_PER_BLOCK - 1) / ROWS_PER_BLOCK), std::min(32768, dm.heads - h0));
     const bool four = c.cache_fp8 == CACHE_E2M1;

@@ -744,8 +744,9 @@ namespace {
 // the per-head records of the call, the exchange array of the scoring kernel
 // (paged cache: the per-row arrays cover the linear copy of the heads' rows, which follows them: K, V, the
 // original positions, the heads' offsets in the copy; it has as many rows as the cache)
-// (4-bit cache: the rows of K as bf16, for the scoring kernel, at the places they have in the cache or its copy)
-struct ReevictWs { size_t psi, pool, sel, rowmod, stats, score, lin_k, lin_v, lin_idx, lin_off, dec_k, total; };
+// (4-bit cache: the rows of K as bf16, for the scoring kernel: those of the call's heads, with their offsets; of a paged cache at the
+// places they have in its copy)
+struct ReevictWs { size_t psi, pool, sel, rowmod, stats, score, lin_k, lin_v, lin_idx, lin_off, dec_k, dec_off, total; long long score_rows; };
 ReevictWs reevict_layout(const madakv_handle* h, int n) {
   const madakv_config& c = h->cfg;
   const Dims dm = make_dims(c, n);
@@ -755,12 +756,15 @@ ReevictWs reevict_layout(const madakv_handle* h, int n) {
   w.psi = 0; w.pool = up(cap * 4); w.sel = w.pool + up(cap * 4); w.rowmod = w.sel + up(cap * 4);
   w.stats = w.rowmod + up(cap);
   w.score = w.stats + up((size_t)dm.heads * 8 * c.n_modalities);
-  w.lin_k = w.score + up(score_ragged_ws_bytes(dm, c, c.ctx_len + c.max_new_tokens, (long long)cap));
+  const bool four = c.cache_fp8 == CACHE_E2M1, apart = four && !c.page_rows;
+  w.score_rows = apart ? cache_rows_front(dm, c) : (long long)cap;
+  w.lin_k = w.score + up(score_ragged_ws_bytes(dm, c, c.ctx_len + c.max_new_tokens, w.score_rows));
   const size_t row_bytes = (size_t)(cache_row_bytes(c) + cache_scale_bytes(c));
   const size_t lin = c.page_rows ? up(cap * row_bytes) : 0;
   w.lin_v = w.lin_k + lin; w.lin_idx = w.lin_v + lin; w.lin_off = w.lin_idx + (c.page_rows ? up(cap * 4) : 0);
   w.dec_k = w.lin_off + (c.page_rows ? up((size_t)dm.heads * 8) : 0);
-  w.total = w.dec_k + (c.cache_fp8 == CACHE_E2M1 ? up(cap * c.head_dim * 2) : 0);
+  w.dec_off = w.dec_k + (four ? up((size_t)w.score_rows * c.head_dim * 2) : 0);
+  w.total = w.dec_off + (apart ? up((size_t)dm.heads * 8) : 0);
   return w;
 }
 }  // namespace
@@ -823,14 +827,17 @@ int32_t madakv_reevict(madakv_handle* h, int32_t layer0, int32_t n,
     char* stats_r = wsb + w.stats + heads0 * 8 * c.n_modalities;
     int32_t* bud_r = budgets + heads0 * c.n_modalities;
     const void* k_score = k_work;
+    const int64_t* score_off = off_work + heads0;
     if (c.cache_fp8 == CACHE_E2M1) {
       Paging flat = make_paging(h);
       flat.page_rows = 0;
-      e = launch_cache_rows(dr, c, k_work, v_work, off_work + heads0, kv_len + heads0, wsb + w.dec_k, nullptr, cache_rows, longest, flat, 0, st);
+      int64_t* dec_off = c.page_rows ? nullptr : reinterpret_cast<int64_t*>(wsb + w.dec_off);
+      e = launch_cache_rows(dr, c, k_work, v_work, off_work + heads0, kv_len + heads0, wsb + w.dec_k, nullptr, cache_rows, longest, flat, 0, st, dec_off);
       k_score = wsb + w.dec_k;
+      if (dec_off) score_off = dec_off;
     }
-    if (e == hipSuccess) e = launch_score_ragged(dr, c, qr, k_score, off_work + heads0, kv_len + heads0, longest, cache_rows, psi_c, wsb + w.score, st);
-    if (e == hipSuccess) e = launch_restats(dr, c, psi_c, idx_work, mask, off_work + heads0, kv_len + heads0, len1_of(h, l0), h->appended[l0], pool_c, rowmod,
+    if (e == hipSuccess) e = launch_score_ragged(dr, c, qr, k_score, score_off, kv_len + heads0, longest, w.score_rows, psi_c, wsb + w.score, st);
+    if (e == hipSuccess) e = launch_restats(dr, c, psi_c, score_off, idx_work, mask, off_work + heads0, kv_len + heads0, len1_of(h, l0), h->appended[l0], pool_c, rowmod,
                                             stats_r, bud_r, st);
     if (e == hipSuccess) e = launch_select(dr, c, pool_c, mask, bud_r, off_work + heads0, kv_len + heads0, sel, st, kv_len + heads0, rowmod);
     if (e == hipSuccess) e = launch_compact(dr, c, k_work, v_work, idx_work, sel, off_work + heads0, kv_len + heads0, bud_r, cache_rows,

@@ -33,7 +33,7 @@ constexpr float RE_FX_SCALE = 17592186044416.0f;    // 2^44, the fixed-point uni
 constexpr float RE_PSI_MAX = 256.0f;
 
 struct RestatsArgs {
-  const float* psi; const int32_t* kept_idx; const uint8_t* mask; const int64_t* seg_off; const int32_t* seg_len;
+  const float* psi; const int64_t* psi_off; const int32_t* kept_idx; const uint8_t* mask; const int64_t* seg_off; const int32_t* seg_len;
   float* psi_pool; uint8_t* rowmod; void* stats; int32_t* budgets;
   const int32_t* len1;
   int B, H, L, W, M, appended, pool_r, pool_mode, share_mode, mpa_mode;
@@ -58,6 +58,7 @@ __global__ __launch_bounds__(RE_THREADS) void restats_kernel(RestatsArgs a) {
   if (len <= 0) return;                                     // an empty segment stays empty
   const long long off = a.seg_off[head];
   const int len0 = rows_before(len, a.len1[head], a.appended);      // rows before the appended ones: they have original positions
+  const float* psi = a.psi + a.psi_off[head];
   const int nc = len - a.W;                                 // candidates: everything before the new window
   if (tid < 4) { s_w[tid] = 0ULL; s_n[tid] = 0u; }
   __syncthreads();
@@ -70,7 +71,7 @@ __global__ __launch_bounds__(RE_THREADS) void restats_kernel(RestatsArgs a) {
       if (origin < a.L) m = min((int)a.mask[(long long)b * a.L + origin], a.M - 1);
     }
     a.rowmod[off + i] = (uint8_t)m;
-    const float v = a.psi[off + i];
+    const float v = psi[i];
     if (i < nc || a.share_mode) {
       const unsigned long long fx = re_to_fx(v);
 #pragma unroll
@@ -82,7 +83,7 @@ __global__ __launch_bounds__(RE_THREADS) void restats_kernel(RestatsArgs a) {
       // pooled score over the neighbouring rows of the cache, clipped at the candidate range
       const int lo = max(i - a.pool_r, 0), hi = min(i + a.pool_r, nc - 1);
       float acc = a.pool_mode ? 0.f : v;
-      for (int j = lo; j <= hi; ++j) acc = a.pool_mode ? acc + a.psi[off + j] : fmaxf(acc, a.psi[off + j]);
+      for (int j = lo; j <= hi; ++j) acc = a.pool_mode ? acc + psi[j] : fmaxf(acc, psi[j]);
       a.psi_pool[off + i] = a.pool_mode ? acc / (float)(hi - lo + 1) : acc;
     }
   }
@@ -174,11 +175,11 @@ __global__ __launch_bounds__(RE_THREADS) void compact_kernel(CompactArgs a) {
   if (tid == 0) a.kv_len[head] = keep;
 }
 
-hipError_t launch_restats(const Dims& dm, const madakv_config& c, const float* psi_c, const int32_t* kept_idx, const uint8_t* mask,
+hipError_t launch_restats(const Dims& dm, const madakv_config& c, const float* psi_c, const int64_t* psi_off, const int32_t* kept_idx, const uint8_t* mask,
                           const int64_t* seg_off, const int32_t* seg_len, const int32_t* len1, int appended, float* pool_c, uint8_t* rowmod,
                           void* stats, int32_t* budgets, hipStream_t st) {
   RestatsArgs a;
-  a.psi = psi_c; a.kept_idx = kept_idx; a.mask = mask; a.seg_off = seg_off; a.seg_len = seg_len; a.psi_pool = pool_c;
+  a.psi = psi_c; a.psi_off = psi_off; a.kept_idx = kept_idx; a.mask = mask; a.seg_off = seg_off; a.seg_len = seg_len; a.psi_pool = pool_c;
   a.rowmod = rowmod; a.stats = stats; a.budgets = budgets;
   a.B = dm.B; a.H = dm.H; a.L = dm.L; a.W = dm.W; a.M = c.n_modalities; a.appended = appended;
   a.pool_r = (c.pool_k - 1) / 2; a.pool_mode = c.pool_mode; a.share_mode = c.share_mode; a.mpa_mode = c.mpa_mode;

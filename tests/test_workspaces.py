@@ -53,3 +53,25 @@ for name in calls:
 print("ok")
 """ % (cfg.get("dtype") == 0, bool(cfg.get("page_rows"))), good(**cfg))
     assert out.strip() == "ok"
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(n_q_heads=28, n_kv_heads=4, window=16)])
+def test_reeviction_of_one_layer_in_4_bits_holds_one_layer_of_k(runtime, kw):  # noqa: F811
+    """The workspace has K as bf16 for the rows that the call's layers can hold, not for all layers of the model."""
+    cfg = dict(n_layers=32, n_q_heads=128, n_kv_heads=64, batch=2, ctx_len=16384, budget=4096, max_new_tokens=100, cache_fp8=4)
+    cfg.update(kw)
+    capacity = cfg["n_layers"] * cfg["batch"] * cfg["n_kv_heads"] * (cfg["budget"] + 100)
+    layer = cfg["batch"] * cfg["n_kv_heads"] * (cfg["ctx_len"] + 100)
+    out = scenario(runtime, f"""
+h = create(sys.argv[3])
+z, cap = Z(), C.c_int64()
+assert lib.madakv_compact_capacity_tokens(h, C.byref(cap)) == 0 and cap.value == {capacity}
+def size(n): assert lib.madakv_reevict_workspace_bytes(h, I(n), C.byref(z)) == 0; return z.value
+for n in (1, 2, 32):
+    held = min({capacity}, n * {layer})
+    # per row of the cache 13 bytes of scores, choices and modalities; per row of the call K, and a score for every 64 proxy rows
+    least = 13 * {capacity} + 2 * 128 * held
+    assert least <= size(n) <= least + (4 * 4 * held) + n * (64 << 20), (n, size(n), least)
+print("ok")
+""", good(**cfg))
+    assert out.strip() == "ok"
