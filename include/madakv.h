@@ -228,7 +228,8 @@ int32_t madakv_window_attn_score(madakv_handle* h, int32_t layer0, int32_t n,
  *   q        [n, B, Hq, L, d]  queries of the whole prompt
  *   k        [n, B, H, L, d]
  *   row_lse  [n, B, Hq, L] float or NULL  natural log of sum_i exp(scale * q_r . k_i) over the keys i <= r, which the prefill
- *                              attention has; without it the call forms the logits twice
+ *                              attention has; without it the call forms the logits of prompts
+ *                              of more than 256 positions twice
  *   psi      [n, B, H, L]      out: sum over the G * L query rows of the causal softmax weight they pay to key i
  * mask, psi_pool, stats, n_mod: all NULL (the scores alone), or as in madakv_score, for madakv_allocate and
  * madakv_select_gather to go on with; they are those of psi * 2^-s, s the least with W * 2^s >= L, so that they have the
@@ -368,7 +369,8 @@ int32_t madakv_cache_rows(madakv_handle* h, int32_t layer0, int32_t n, const voi
  *   budgets  [n, B, H, M]       out: the new split
  *   ws                          madakv_reevict_workspace_bytes(h, n) bytes
  * The decode-step counters of the layers are reset: max_new_tokens rows can be appended again.
- * An 8-bit or 4-bit cache is scored by the values it holds and moved as it is stored (4 bits: the workspace holds K as bf16).  A paged cache is re-evicted as a whole
+ * An 8-bit or 4-bit cache is scored by the values it holds and moved as it is stored (4 bits: the workspace holds K as bf16, of the
+ * rows that n layers can have).  A paged cache is re-evicted as a whole
  * (layer0 = 0, n = n_layers, else MADAKV_ERR_INVALID_ARG): the survivors end up in the heads' initial pages
  * and every page taken since the eviction goes back to the pools, which all layers share; the work is done
  * on a linear copy of the rows in the workspace (as many rows as the cache holds).

@@ -19,8 +19,8 @@
 // A load instruction of a wave takes 1 KB of consecutive codes (16 rows of 128 dims, 32 of 64) and one of 64 scale bytes.  Rows of
 // 64 dims: lanes 0-31 have the blocks of rows 0-15, lanes 32-63 those of rows 16-31; columns 0-7 have the query in the half of the
 // contraction that belongs to the former and zeros in the other, columns 8-15 the other way round.
-// What bounds it: HBM for long caches, 128 heads of 16K rows of 128 dims (285 MB) 50-52 us, 5.5 TB/s, with four waves per SIMD issuing
-// most of the time; a launch's own latency for short ones, 8 heads of 256 rows of 64 dims 6.2 us, 28 / 4 heads of 2K rows of 128 dims 7.1.
+// What bounds it: HBM for long caches, 128 heads of 16K rows of 128 dims (285 MB) 50-54 us by the card, 5.3-5.7 TB/s, with four waves per SIMD issuing
+// most of the time; a launch's own latency for short ones, 8 heads of 256 rows of 64 dims 6.0-6.6 us, 28 / 4 heads of 2K rows of 128 dims 6.3-7.1.
 // Measured against it at 285 MB: eight waves a workgroup 55.7, no loads ahead of a tile 53.7, loads of codes through the caches 58.6,
 // 8 logits per lane with half of the columns idle 54.5 (now 52.9 on that card); scales
 // as one load per 32 rows 0.4 us less at the most.

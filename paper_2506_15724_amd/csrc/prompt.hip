@@ -15,11 +15,11 @@
 // instructions: sweep 1 looks for no maximum, but sums against the reference of the first tile and takes another
 // one when a sum passes 2^60 (a tile is then formed again); rows that no column of a wave sees are left out and the causal mask is
 // applied in diagonal tiles only; four blocks of columns share each operand read from LDS; a lane's offset in a tile is the same for all tiles.
-// 16K tokens, 28 / 4 heads of 128 dims, both sweeps: 1.76-1.81 ms, 240 ns per tile and SIMD, 1.08 PFLOP/s of logits (a library product of
-// 16K x 16K x 16K bf16 runs at 1.36 on this card); 8K tokens, 32 heads, one sweep 0.27 ms.  Kept steps: address arithmetic per load -> a
+// 16K tokens, 28 / 4 heads of 128 dims, both sweeps: 1.75-1.86 ms by the card, 240-255 ns per tile and SIMD, 1.03-1.10 PFLOP/s of logits (a library product of
+// 16K x 16K x 16K bf16 runs at 1.36 on this card); 8K tokens, 32 heads, one sweep 0.27-0.29 ms.  Kept steps: address arithmetic per load -> a
 // buffer with fixed offsets 1.85 -> 1.80; a block's contraction between the vector instructions of the one before it 1.89 -> 1.85.
 // No gain at this size: blocks of two and three waves per SIMD (1.87; smaller calls take them, see prompt_plan), heads in plain order instead of one XCD's (1.84).  At 64 dims, half the
-// matrix instructions, the vector unit alone bounds it, and the registers leave room for three waves: 16K, 28 / 4 heads 1.22 ms,
+// matrix instructions, the vector unit alone bounds it, and the registers leave room for three waves: 16K, 28 / 4 heads 1.17-1.22 ms,
 // 8K, 32 heads 0.376 (two waves 0.407, blocks of two and four waves 1.49 and 0.406, four waves with spills 1.38 and 0.437).
 // The rows come straight into LDS (16 bytes per lane, pieces of a row permuted so that operand reads do not collide), in a
 // ring of three tiles of 64 rows; LDS accesses and waits of the loop are written out, as in score.hip and for its reason.

@@ -1,12 +1,12 @@
 // What a decode step paid to every row of the reduced cache, added up over the steps: acc[r] = decay * acc[r] + sum over the G
 // query heads of softmax(scale * q K_c^T)[r], and the row of each head that has had the least of it.
 //
-// The attention kernels leave the logits of the step (4 bytes per row and query head beside the row's K and V of 136 to 1024)
+// The attention kernels leave the logits of the step (4 bytes per row and query head beside the row's K and V of 68 to 1024)
 // and, when a head's pieces have met, their maximum and the sum of 2^(logit - maximum); a second launch makes weights of them:
 // a row's weight needs the whole head's sum, and a launch behind the first one knows it without anybody waiting for anybody.
 // Per row: G logits, 4 bytes of acc read and written, 4 of its position.  What bounds it is a launch's latency: 4.5 us behind an
 // attention of 17 (128 heads of 2K 8-bit rows) or 8 (4 heads of 2K rows, 7 queries each), 6.5 behind one of 91 (64 heads of
-// 16K bf16 rows).  One launch instead of two would leave a head's rows to the one workgroup that finishes its attention.
+// 16K bf16 rows).  One launch instead of two would leave a head's rows to the one workgroup that finishes its attention (not measured).
 // Workgroups of 1024 rows (256 to 4096: the same); the smallest sums of a
 // head's workgroups meet like the pieces of its attention: as (sum, row) in one 64-bit word each, whose minimum does not depend
 // on an order, counted at the head's counter, and the last one to arrive takes the least.
