@@ -15,11 +15,11 @@
 // instructions: sweep 1 looks for no maximum, but sums against the reference of the first tile and takes another
 // one when a sum passes 2^60 (a tile is then formed again); rows that no column of a wave sees are left out and the causal mask is
 // applied in diagonal tiles only; four blocks of columns share each operand read from LDS; a lane's offset in a tile is the same for all tiles.
-// 16K tokens, 28 / 4 heads of 128 dims, both sweeps: 1.75-1.86 ms by the card, 240-255 ns per tile and SIMD, 1.03-1.10 PFLOP/s of logits (a library product of
+// 16K tokens, 28 / 4 heads of 128 dims, both sweeps: 1.72-1.86 ms by the card, 235-255 ns per tile and SIMD, 1.03-1.12 PFLOP/s of logits (a library product of
 // 16K x 16K x 16K bf16 runs at 1.36 on this card); 8K tokens, 32 heads, one sweep 0.27-0.29 ms.  Kept steps: address arithmetic per load -> a
 // buffer with fixed offsets 1.85 -> 1.80; a block's contraction between the vector instructions of the one before it 1.89 -> 1.85.
 // No gain at this size: blocks of two and three waves per SIMD (1.87; smaller calls take them, see prompt_plan), heads in plain order instead of one XCD's (1.84).  At 64 dims, half the
-// matrix instructions, the vector unit alone bounds it, and the registers leave room for three waves: 16K, 28 / 4 heads 1.17-1.22 ms,
+// matrix instructions, the vector unit alone bounds it, and the registers leave room for three waves: 16K, 28 / 4 heads 1.15-1.22 ms,
 // 8K, 32 heads 0.376 (two waves 0.407, blocks of two and four waves 1.49 and 0.406, four waves with spills 1.38 and 0.437).
 // The rows come straight into LDS (16 bytes per lane, pieces of a row permuted so that operand reads do not collide), in a
 // ring of three tiles of 64 rows; LDS accesses and waits of the loop are written out, as in score.hip and for its reason.
@@ -209,11 +209,24 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(N
     return x;
   };
   // the sum of a column's 16 terms: against the rows' normalisers, or its own reference
+  const auto sum16 = [](const float (&p)[16]) {
+    return (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]))) + (((p[8] + p[9]) + (p[10] + p[11])) + ((p[12] + p[13]) + (p[14] + p[15])));
+  };
+  const auto term = [&](int b, const pf32x16_t& x, int j) { return __builtin_amdgcn_exp2f(fmaf(x[j], a.scale_log2, PASS == 2 ? -nreg[j % (PASS == 2 ? 16 : 1)] : -ref[b])); };
   const auto terms = [&](int b, const pf32x16_t& x) {
     float p[16];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(x[j], a.scale_log2, PASS == 2 ? -nreg[j % (PASS == 2 ? 16 : 1)] : -ref[b]));
-    return (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]))) + (((p[8] + p[9]) + (p[10] + p[11])) + ((p[12] + p[13]) + (p[14] + p[15])));
+    for (int j = 0; j < 16; ++j) p[j] = term(b, x, j);
+    return sum16(p);
+  };
+  // the same of sweep 2's diagonal tile where a normaliser is no number, or minus infinity: nothing from the rows that do not see the key
+  const auto seen_terms = [&](int b, const pf32x16_t& x) {
+    int first = col - 4 * half;
+    asm volatile("" : "+v"(first));             // (made here: the comparisons, kept over the loop, would take registers)
+    float p[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) p[j] = 8 * (j >> 2) + (j & 3) >= first ? term(b, x, j) : 0.f;
+    return sum16(p);
   };
   // sweep 1, a tile for which some column has no reference yet or has left it far behind: there the largest logit becomes the
   // reference
@@ -308,8 +321,10 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(N
           const int mine = my0 + b * 32;
           if (PASS == 1 ? r > mine : r < mine) continue;
           const pf32x16_t x = r == mine ? masked(logits(b)) : logits(b);
-          if (PASS == 1) look(b, x);
-          else sum[b] += terms(b, x);
+          if (PASS == 1) { look(b, x); continue; }
+          float s = terms(b, x);
+          if (r == mine && __builtin_expect(__builtin_amdgcn_ballot_w64(s != s) != 0, 0)) s = seen_terms(b, x);
+          sum[b] += s;
         }
       }
     }
@@ -386,12 +401,23 @@ __device__ __forceinline__ void short_block(const unsigned char* keys, const pbf
     }
     __builtin_amdgcn_sched_barrier(0);          // (operands of one tile at a time: all of them do not fit)
   }
+  // a lane whose normaliser is no number, or minus infinity: nothing to the keys that its query does not see, no number to the others
+  const auto unseen = [&](bool lost, bool all) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const bool sees = (i - mine) * 32 + 8 * (j >> 2) + 4 * half + (j & 3) <= col;
+        if (lost) x[i][j] = !sees ? 0.f : all ? __builtin_nanf("") : x[i][j];
+      }
+  };
   float share = 1.f;
   if (GIVEN) {
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
       for (int j = 0; j < 16; ++j) x[i][j] = __builtin_amdgcn_exp2f(fmaf(x[i][j], scale_log2, -norm));
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(norm > -__builtin_inff())) != 0, 0)) unseen(!(norm > -__builtin_inff()), false);
   } else {
     top = fmaxf(top, __shfl_xor(top, 32, 64));
     float s[4] = {0.f, 0.f, 0.f, 0.f};
@@ -404,6 +430,10 @@ __device__ __forceinline__ void short_block(const unsigned char* keys, const pbf
       }
     const float sum = (s[0] + s[1]) + (s[2] + s[3]);
     share = there ? 1.f / (sum + __shfl_xor(sum, 32, 64)) : 0.f;
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(share != share) != 0, 0)) {
+      unseen(share != share, true);
+      share = share != share ? 1.f : share;
+    }
   }
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
