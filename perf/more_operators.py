@@ -6,7 +6,8 @@ A case names one of three operators and a shape (layers, batch, heads, head_dim,
                 (madakv_prompt_attn).  The L positions of a batch item hold one prompt, one padded prompt, or several that
                 follow each other and do not see each other; positions of none are left as they are
   op "tree"     attention of a tree of drafted tokens: every node attends over the rows of the reduced cache and over the nodes
-                that its mask names, its ancestors and itself (madakv_tree_attn)
+                that its mask names, its ancestors and itself, whose rows count with the values the cache would give them
+                (madakv_tree_attn)
   op "commit"   the nodes of the accepted path become rows of the cache, each batch item its own number of them
                 (madakv_tree_commit)
 
@@ -282,7 +283,9 @@ def _tree_attn(state):
     NL, B, Hq, H, d, L, W, keep = _sizes(case)
     T, rows, there = case["nodes"], state["rows"], state["there"]
     k, v = (_decode4(*c) if case["cache"] == "fp4" else c.float() for c in (state["k"], state["v"]))
-    k, v = (torch.cat([c[rows], x[n].float().view(NL * B * H, T, d)], 1) for c, n in ((k, "k_new"), (v, "v_new")))
+    new = [x[n].view(NL * B * H, T, d) for n in ("k_new", "v_new")]
+    new = [_decode4(*_encode4(c)) if case["cache"] == "fp4" else c.clamp(-448, 448).to(torch.float8_e4m3fn).float() if case["cache"] == "fp8" else c.float() for c in new]
+    k, v = (torch.cat([c[rows], n], 1) for c, n in zip((k, v), new))
     sees = (x["tree"].unsqueeze(-1) >> torch.arange(T, device=DEV)) & 1
     sees = sees.bool().view(1, B, 1, 1, T, T).expand(NL, B, H, Hq // H, T, T).reshape(NL * B * H, -1, T)
     may = torch.cat([there.unsqueeze(1).expand(-1, sees.shape[1], -1), sees], -1)
@@ -448,12 +451,12 @@ def exact(case, seed):
                 if keep < L:
                     c = np.lexsort((np.arange(L - W), -score[l, b, h]))[:budgets[l, b, h, 0]]
                     p = np.concatenate([np.sort(c), np.arange(L - W, L)])
-                k, v = (x[n][l, b, h][torch.from_numpy(p).to(DEV)] for n in ("k", "v"))
+                k, v = (torch.cat([x[n][l, b, h][torch.from_numpy(p).to(DEV)], x[n + "_new"][l, b, h]]) for n in ("k", "v"))
                 if case["cache"] == "fp4":
                     k, v = _value4(k), _value4(v)
                 elif case["cache"] == "fp8":
                     k, v = (t.clamp(-448, 448).to(torch.float8_e4m3fn) for t in (k, v))
-                k, v = torch.cat([k.double(), x["k_new"][l, b, h].double()]), torch.cat([v.double(), x["v_new"][l, b, h].double()])
+                k, v = k.double(), v.double()
                 may = torch.cat([torch.ones(T, len(p), dtype=torch.float64, device=DEV), sees], 1)
                 for j in range(h * G, (h + 1) * G):
                     s = x["q"][l, b, j].double() @ k.t().contiguous() / math.sqrt(d)
