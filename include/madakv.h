@@ -21,6 +21,9 @@
  *                         accumulated over the whole prompt
  *   madakv_decode_attn_weights  a decode step that goes on accumulating it, and the eviction of one row per step by it
  *   madakv_cache_rows     the rows of an 8-bit or 4-bit reduced cache in the type of the model
+ *   madakv_prompt_attn    that prefill attention for every position (Sec. 3.1 Eq. 5), whose normalisers madakv_score_prompt takes
+ *   madakv_tree_attn      Eq. 5 for several drafted tokens per step over the reduced cache
+ *   madakv_tree_commit    Eq. 4 for those of them that are accepted
  *   madakv_window_attn_score  that prefill attention for the proxy rows (Sec. 3.1 Eq. 5) with Eq. 7, 6, 9 as
  *                         by-products of the same pass
  *
@@ -35,7 +38,7 @@
  *   - All work is ordered on the caller's stream (a hipStream_t passed as void*, NULL = the
  *     null stream): it starts after what the stream held before the call and is complete, as far
  *     as the stream is concerned, before anything enqueued after it.  madakv_allocate,
- *     madakv_score_prompt, madakv_cache_rows and the decode calls enqueue on that stream only.  madakv_score, madakv_score_lse,
+ *     madakv_score_prompt, madakv_prompt_attn, madakv_cache_rows, the tree and the decode calls enqueue on that stream only.  madakv_score, madakv_score_lse,
  *     madakv_select_gather and madakv_evict over four or more layers also use the handle's own
  *     stream for the per-head statistics / selection kernels of one layer group while another
  *     group is scored or gathered; that stream forks from and joins the caller's stream through
@@ -243,6 +246,20 @@ int32_t madakv_score_prompt(madakv_handle* h, int32_t layer0, int32_t n,
                             float* psi, float* psi_pool, void* stats, int32_t* n_mod,
                             void* ws, size_t ws_bytes, void* stream);
 
+/* The prefill attention of the whole prompt (Sec. 3.1 Eq. 5 at every position), causal, with grouped heads.
+ *   q        [n, B, Hq, L, d]
+ *   k, v     [n, B, H, L, d]
+ *   seq_off  [B, n_seq + 1] int32 on the device, ascending within 0 .. L, or NULL with n_seq = 0.  Sequence s of batch item b has the
+ *            positions seq_off[b][s] .. seq_off[b][s + 1] - 1 (possibly none); a position sees those of its own sequence up to itself.
+ *            One sequence of each item is a padded batch, several are packed prompts.  NULL: all L positions are one sequence
+ *   out      [n, B, Hq, L, d]  softmax(scale * q k^T) v (float if out_fp32 else dtype)
+ *   row_lse  [n, B, Hq, L]     optional (may be NULL): natural log-sum-exp of each row, as madakv_score_prompt takes it
+ * Rows of out and row_lse at positions of no sequence are left as they are, and what k and v hold where a position does not look
+ * has no influence on it, whatever it is.  (A caller that has filled row_lse with +infinity has madakv_score_prompt count nothing from the queries of
+ * positions of no sequence.)  No workspace. */
+int32_t madakv_prompt_attn(madakv_handle* h, int32_t layer0, int32_t n, const void* q, const void* k, const void* v,
+                           const int32_t* seq_off, int32_t n_seq, void* out, float* row_lse, void* stream);
+
 /* Eq. 8, Eq. 10-11 for layers [layer0, layer0 + n) in order.
  *   stats    [n, B, H]        from madakv_score
  *   n_mod    [B, M]
@@ -339,6 +356,39 @@ int32_t madakv_decode_attn_weights(madakv_handle* h, int32_t layer0, int32_t n,
                                    const int32_t* slot_in, int32_t* slot_out,
                                    int32_t* kept_idx, const int32_t* pos, int32_t recent,
                                    void* ws, size_t ws_bytes, void* stream);
+
+/* Attention of several drafted tokens at once (Eq. 5 for the nodes of a tree, each following its parent): every node attends over the rows of the
+ * reduced cache and over the nodes that its mask names.  Nothing is stored: madakv_tree_commit does that for the nodes that are accepted.
+ *   n_nodes  T, 1 .. 64 (else MADAKV_ERR_BAD_SHAPE)
+ *   q        [n, B, Hq, T, d]
+ *   k_new, v_new [n, B, H, T, d]  the nodes' rows; they count with the values that the cache would hold of them (cache_fp8), so that a
+ *            node's output is what madakv_decode_attn gives for its token behind its ancestors
+ *   tree     [B, T] uint64     bit i of entry t: node t sees node i (its ancestors, and as a rule itself); bits from T on mean nothing.  A node may
+ *                              see none
+ *   k_c, v_c, kv_off, kv_len   as in madakv_decode_attn; none of them is written
+ *   out      [n, B, Hq, T, d]  float if out_fp32 else dtype; not finite for a head with an empty segment
+ *   ws       madakv_tree_attn_workspace_bytes(h, n, T) bytes; what it reports serves calls over up to n layers and T nodes */
+int32_t madakv_tree_attn_workspace_bytes(const madakv_handle* h, int32_t n_layers_per_call, int32_t n_nodes, size_t* bytes);
+int32_t madakv_tree_attn(madakv_handle* h, int32_t layer0, int32_t n, int32_t n_nodes, const void* q, const void* k_new, const void* v_new,
+                         const uint64_t* tree, const void* k_c, const void* v_c, const int64_t* kv_off, const int32_t* kv_len,
+                         void* out, void* ws, size_t ws_bytes, void* stream);
+
+/* The accepted nodes' rows into the cache (Eq. 4 for several tokens, of every batch item as many as it has accepted).
+ *   k_new, v_new [n, B, H, T, d]  as in madakv_tree_attn
+ *   path     [B, max_path] int32 on the device: the accepted nodes, in order; an entry that is no node ends the path.  max_path 1 .. 64
+ *   n_path   [B] int32 on the device: how many there are (0 .. max_path)
+ *   start    [B] int32 on the device: the rows that the heads of the item have behind those that the last (re-)eviction left them, in front of the
+ *            accepted ones.  Fewer than a head has: its later rows are taken back.  More, or less than 0: there is a mistake, and the
+ *            heads of the item are left as they are.  In a paged cache rows are not taken back: heads that have more rows are left as they are, too
+ *   most     the most rows that any head of these layers has behind those of the eviction after the call (0 .. max_new_tokens, else
+ *            MADAKV_ERR_INVALID_ARG): accepted rows beyond it are not stored, and contiguous segments with more rows are cut to it.  The host counts `most` rows as
+ *            appended (madakv_decode_attn refuses a layer from max_new_tokens on); a caller that does not know the lengths gives an upper bound
+ *   kv_len   in/out: the rows that the (re-)eviction left + start + the rows stored
+ * A call repeated with the same arguments does the same again.  kept_idx has no entries for these rows until a re-eviction.  Segments that are empty, or
+ * that this handle has not evicted, are left as they are. */
+int32_t madakv_tree_commit(madakv_handle* h, int32_t layer0, int32_t n, int32_t n_nodes, const void* k_new, const void* v_new,
+                           const int32_t* path, const int32_t* n_path, int32_t max_path, const int32_t* start, int32_t most,
+                           void* k_c, void* v_c, const int64_t* kv_off, int32_t* kv_len, void* stream);
 
 /* The rows that the heads of layers [layer0, layer0 + n) hold in an 8-bit or 4-bit reduced cache, as values of dtype:
  *   k_rows, v_rows [capacity_tokens, d]  out: row i holds what row i of k_c / v_c stands for (every value is exact in

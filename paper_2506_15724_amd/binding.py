@@ -70,6 +70,10 @@ def lib() -> C.CDLL:
         L.madakv_cache_rows.argtypes = [vp, i32, i32] + [vp] * 7
         L.madakv_score_prompt_workspace_bytes.argtypes = [vp, i32, C.POINTER(sz)]
         L.madakv_score_prompt.argtypes = [vp, i32, i32] + [vp] * 8 + [vp, sz, vp]
+        L.madakv_prompt_attn.argtypes = [vp, i32, i32, vp, vp, vp, vp, i32, vp, vp, vp]
+        L.madakv_tree_attn_workspace_bytes.argtypes = [vp, i32, i32, C.POINTER(sz)]
+        L.madakv_tree_attn.argtypes = [vp, i32, i32, i32] + [vp] * 10 + [sz, vp]
+        L.madakv_tree_commit.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp]
         for name in EXPORTS:
             getattr(L, name).restype = i32
         _lib = L
@@ -81,6 +85,7 @@ EXPORTS = ["madakv_create", "madakv_destroy", "madakv_last_hip_error", "madakv_w
            "madakv_decode_attn", "madakv_decode_attn_static", "madakv_page_table",
            "madakv_decode_attn_weights_workspace_bytes", "madakv_decode_attn_weights", "madakv_cache_rows",
            "madakv_score_prompt_workspace_bytes", "madakv_score_prompt",
+           "madakv_prompt_attn", "madakv_tree_attn_workspace_bytes", "madakv_tree_attn", "madakv_tree_commit",
            "madakv_reevict_workspace_bytes", "madakv_reevict", "madakv_window_attn_workspace_bytes", "madakv_window_attn_score"]
 
 
@@ -196,6 +201,26 @@ def madakv_score_prompt_workspace_bytes(h, n_layers_per_call: int) -> int:
 def madakv_score_prompt(h, layer0, n, q, k, mask, row_lse, psi, psi_pool, stats, n_mod, ws):
     _check("madakv_score_prompt", lib().madakv_score_prompt(h, layer0, n, _ptr(q), _ptr(k), _ptr(mask), _ptr(row_lse), _ptr(psi), _ptr(psi_pool),
                                                             _ptr(stats), _ptr(n_mod), _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+
+
+def madakv_prompt_attn(h, layer0, n, q, k, v, seq_off, n_seq, out, row_lse):
+    _check("madakv_prompt_attn", lib().madakv_prompt_attn(h, layer0, n, _ptr(q), _ptr(k), _ptr(v), _ptr(seq_off), n_seq, _ptr(out), _ptr(row_lse), _stream()))
+
+
+def madakv_tree_attn_workspace_bytes(h, n_layers_per_call: int, n_nodes: int) -> int:
+    b = C.c_size_t()
+    _check("madakv_tree_attn_workspace_bytes", lib().madakv_tree_attn_workspace_bytes(h, n_layers_per_call, n_nodes, C.byref(b)))
+    return b.value
+
+
+def madakv_tree_attn(h, layer0, n, n_nodes, q, k_new, v_new, tree, k_c, v_c, kv_off, kv_len, out, ws):
+    _check("madakv_tree_attn", lib().madakv_tree_attn(h, layer0, n, n_nodes, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(tree), _ptr(k_c), _ptr(v_c), _ptr(kv_off),
+                                                      _ptr(kv_len), _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+
+
+def madakv_tree_commit(h, layer0, n, n_nodes, k_new, v_new, path, n_path, max_path, start, most, k_c, v_c, kv_off, kv_len):
+    _check("madakv_tree_commit", lib().madakv_tree_commit(h, layer0, n, n_nodes, _ptr(k_new), _ptr(v_new), _ptr(path), _ptr(n_path), max_path, _ptr(start), most,
+                                                          _ptr(k_c), _ptr(v_c), _ptr(kv_off), _ptr(kv_len), _stream()))
 
 
 def madakv_window_attn_workspace_bytes(h, n_layers_per_call: int) -> int:
@@ -409,6 +434,69 @@ class MadaKV:
                                        _ptr(ws), ws.numel(), self._own_stream())
         if rc != OK:
             raise MadaKVError("madakv_score_prompt", rc)
+
+    def prompt_attn(self, l0, n, q, k, v, out, row_lse=None, seq_off=None):
+        """q, out [n, B, Hq, L, d], row_lse [n, B, Hq, L].  seq_off [B, S + 1]: sequence s of a batch item has the positions seq_off[s] up to
+        seq_off[s + 1]; without it all L positions are one."""
+        # (a prompt of a few hundred tokens takes a few us on the device: no views of the own buffers)
+        L = self._ctx
+        self._check_out(out, n * self._out_row * L)
+        self._check_array("out", out, n * self._out_row * L, self._out_dtype)
+        self._check_array("q", q, n * self._out_row * L, self.tdtype)
+        self._check_array("k", k, n * self._kv_row * L, self.tdtype)
+        self._check_array("v", v, n * self._kv_row * L, self.tdtype)
+        n_seq = 0
+        if row_lse is not None:
+            self._check_array("row_lse", row_lse, n * self.cfg.batch * self.cfg.n_q_heads * L, torch.float32)
+        if seq_off is not None:
+            if seq_off.dim() != 2 or seq_off.shape[0] != self.cfg.batch or seq_off.shape[1] < 2:
+                raise ValueError(f"seq_off must be [{self.cfg.batch}, sequences + 1], got {list(seq_off.shape)}")
+            self._check_array("seq_off", seq_off, seq_off.numel(), torch.int32)
+            n_seq = seq_off.shape[1] - 1
+        rc = lib().madakv_prompt_attn(self.h, l0, n, _ptr(q), _ptr(k), _ptr(v), _ptr(seq_off), n_seq, _ptr(out), _ptr(row_lse), self._own_stream())
+        if rc != OK:
+            raise MadaKVError("madakv_prompt_attn", rc)
+
+    def _nodes(self, t):
+        """Nodes of a tree, from a tensor [n, B, heads, T, d]."""
+        if t.dim() != 5:
+            raise ValueError(f"nodes come as [layers, batch, heads, nodes, head_dim], got {list(t.shape)}")
+        return t.shape[3]
+
+    def tree_attn(self, l0, n, q, k_new, v_new, tree, out):
+        """q, out [n, B, Hq, T, d], k_new, v_new [n, B, H, T, d]; tree [B, T] int64: bit i of entry t: node t sees node i."""
+        T = self._nodes(q)
+        self._check_out(out, n * self._out_row * T)
+        self._check_array("out", out, n * self._out_row * T, self._out_dtype)
+        self._check_array("q", q, n * self._out_row * T, self.tdtype)
+        self._check_array("k_new", k_new, n * self._kv_row * T, self.tdtype)
+        self._check_array("v_new", v_new, n * self._kv_row * T, self.tdtype)
+        self._check_array("tree", tree, self.cfg.batch * T, torch.int64)
+        ws = getattr(self, "tree_ws", None)
+        if ws is None or self._tree_nodes < T:
+            ws = self.tree_ws = torch.empty(madakv_tree_attn_workspace_bytes(self.h, self.n_call, T), dtype=torch.uint8, device=self.device)
+            self._tree_nodes = T
+        heads0 = l0 * self._heads
+        rc = lib().madakv_tree_attn(self.h, l0, n, T, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(tree), _ptr(self.k_c), _ptr(self.v_c), _ptr(self.kv_off) + 8 * heads0,
+                                    _ptr(self.kv_len) + 4 * heads0, _ptr(out), _ptr(ws), ws.numel(), self._own_stream())
+        if rc != OK:
+            raise MadaKVError("madakv_tree_attn", rc)
+
+    def tree_commit(self, l0, n, k_new, v_new, path, n_path, start, most):
+        """path [B, P], n_path, start [B] int32 on the device; most: the rows that any head may have behind those of the eviction afterwards."""
+        T = self._nodes(k_new)
+        self._check_array("k_new", k_new, n * self._kv_row * T, self.tdtype)
+        self._check_array("v_new", v_new, n * self._kv_row * T, self.tdtype)
+        if path.dim() != 2 or path.shape[0] != self.cfg.batch:
+            raise ValueError(f"path must be [{self.cfg.batch}, steps], got {list(path.shape)}")
+        self._check_array("path", path, path.numel(), torch.int32)
+        self._check_array("n_path", n_path, self.cfg.batch, torch.int32)
+        self._check_array("start", start, self.cfg.batch, torch.int32)
+        heads0 = l0 * self._heads
+        rc = lib().madakv_tree_commit(self.h, l0, n, T, _ptr(k_new), _ptr(v_new), _ptr(path), _ptr(n_path), path.shape[1], _ptr(start), most, _ptr(self.k_c), _ptr(self.v_c),
+                                      _ptr(self.kv_off) + 8 * heads0, _ptr(self.kv_len) + 4 * heads0, self._own_stream())
+        if rc != OK:
+            raise MadaKVError("madakv_tree_commit", rc)
 
     def window_attn_score(self, l0, n, q_win, k, v, mask, out, row_lse=None):
         self._check_out(out, n * self.cfg.batch * self.cfg.n_q_heads * self.cfg.window * self.cfg.head_dim)

@@ -854,6 +854,63 @@ int32_t madakv_reevict(madakv_handle* h, int32_t layer0, int32_t n,
   return hip_fail(h, e);
 }
 
+int32_t madakv_prompt_attn(madakv_handle* h, int32_t layer0, int32_t n, const void* q, const void* k, const void* v,
+                           const int32_t* seq_off, int32_t n_seq, void* out, float* row_lse, void* stream) {
+  int32_t r = check_range(h, layer0, n);
+  if (r != MADAKV_OK) return r;
+  if (bad_ptr(q) || bad_ptr(k) || bad_ptr(v) || bad_ptr(out) || (row_lse && bad_ptr(row_lse, 4))) return MADAKV_ERR_INVALID_ARG;
+  if (seq_off ? bad_ptr(seq_off, 4) || n_seq < 1 : n_seq != 0) return MADAKV_ERR_INVALID_ARG;
+  return hip_fail(h, launch_prompt_attn(make_dims(h->cfg, n), h->cfg, q, k, v, seq_off, n_seq, out, row_lse, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int32_t madakv_tree_attn_workspace_bytes(const madakv_handle* h, int32_t n_layers_per_call, int32_t n_nodes, size_t* bytes) {
+  if (!h || !bytes || n_layers_per_call < 1 || n_layers_per_call > h->cfg.n_layers || n_nodes < 1 || n_nodes > TREE_NODES) return MADAKV_ERR_INVALID_ARG;
+  const madakv_config& c = h->cfg;
+  *bytes = most_over_calls(n_layers_per_call, [&](int m) {
+    size_t most = 0;
+    for (int t = 1; t <= n_nodes; ++t) most = std::max(most, tree_ws_bytes(make_dims(c, m), c, t, c.ctx_len + c.max_new_tokens));
+    return most;
+  });
+  return MADAKV_OK;
+}
+
+int32_t madakv_tree_attn(madakv_handle* h, int32_t layer0, int32_t n, int32_t n_nodes, const void* q, const void* k_new, const void* v_new,
+                         const uint64_t* tree, const void* k_c, const void* v_c, const int64_t* kv_off, const int32_t* kv_len,
+                         void* out, void* ws, size_t ws_bytes, void* stream) {
+  int32_t r = check_range(h, layer0, n);
+  if (r != MADAKV_OK) return r;
+  if (bad_ptr(q) || bad_ptr(k_new) || bad_ptr(v_new) || bad_ptr(tree, 8) || bad_ptr(k_c) || bad_ptr(v_c) || bad_ptr(kv_off, 8) || bad_ptr(kv_len, 4) ||
+      bad_ptr(out) || bad_ptr(ws)) return MADAKV_ERR_INVALID_ARG;
+  if (n_nodes < 1 || n_nodes > TREE_NODES) return MADAKV_ERR_BAD_SHAPE;
+  const madakv_config& c = h->cfg;
+  const Dims dm = make_dims(c, n);
+  if (ws_bytes < tree_ws_bytes(dm, c, n_nodes, c.ctx_len + c.max_new_tokens)) return MADAKV_ERR_WORKSPACE_TOO_SMALL;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  // (a layer that a captured step appends to may be longer than the host knows)
+  const int longest = longest_rows(h, layer0, n, replayed_later(st), true);
+  return hip_fail(h, launch_tree_attn(dm, c, n_nodes, q, k_new, v_new, tree, k_c, v_c, kv_off, kv_len, out, h->meet, ws, region_tokens(c) * c.batch, longest,
+                                      make_paging(h), layer0, st));
+}
+
+int32_t madakv_tree_commit(madakv_handle* h, int32_t layer0, int32_t n, int32_t n_nodes, const void* k_new, const void* v_new,
+                           const int32_t* path, const int32_t* n_path, int32_t max_path, const int32_t* start, int32_t most,
+                           void* k_c, void* v_c, const int64_t* kv_off, int32_t* kv_len, void* stream) {
+  int32_t r = check_range(h, layer0, n);
+  if (r != MADAKV_OK) return r;
+  if (bad_ptr(k_new) || bad_ptr(v_new) || bad_ptr(path, 4) || bad_ptr(n_path, 4) || bad_ptr(start, 4) || bad_ptr(k_c) || bad_ptr(v_c) || bad_ptr(kv_off, 8) ||
+      bad_ptr(kv_len, 4)) return MADAKV_ERR_INVALID_ARG;
+  if (n_nodes < 1 || n_nodes > TREE_NODES || max_path < 1 || max_path > TREE_NODES) return MADAKV_ERR_BAD_SHAPE;
+  const madakv_config& c = h->cfg;
+  if (most < 0 || most > c.max_new_tokens) return MADAKV_ERR_INVALID_ARG;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  const bool later = replayed_later(st);
+  const hipError_t e = launch_tree_commit(make_dims(c, n), c, n_nodes, k_new, v_new, path, n_path, max_path, start, most, k_c, v_c, kv_off, kv_len, h->meet,
+                                          region_tokens(c) * c.batch, make_paging(h), layer0, st);
+  // (rows of a paged cache are not taken back)
+  if (e == hipSuccess) for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] = c.page_rows ? std::max(h->appended[l], most) : most; h->replays[l] |= later; }
+  return hip_fail(h, e);
+}
+
 int32_t madakv_page_table(const madakv_handle* h, const int32_t** table, int32_t* entries_per_head) {
   if (!h || !table || !entries_per_head) return MADAKV_ERR_INVALID_ARG;
   *table = h->d_page_tbl;

@@ -1,0 +1,502 @@
+// Several drafted tokens per step over the reduced, ragged cache (paper Sec. 3.1 Eq. 3-5 for a tree of tokens): the attention of all nodes of the
+// tree, and the accepted nodes' rows into the cache.
+//
+// Attention: the G * T query rows of a KV head (T nodes) are the columns of attn_tile.h, its keys the rows of the head's segment and behind
+// them the T nodes, of which a column sees those that its node's mask names.  A workgroup has 32 WC columns; its 2 WC waves are WC blocks of
+// columns times the two halves of a tile of 64 keys.  A head is cut into pieces as in decode_pieces.h: every piece leaves its partial (reference, sum,
+// output) in the workspace and counts itself, and whoever comes last merges them in piece order.  Rows of the type of the model come straight into LDS, 8-bit
+// and 4-bit rows through registers, which turn them into bf16 (exactly); nodes' rows count with the values that the cache would give them.
+// Masked keys count for nothing whatever they hold, as in prompt_attn.hip.
+#include "attn_tile.h"
+#include "decode_pieces.h"
+
+#include <algorithm>
+
+namespace madakv {
+
+struct TreeArgs {
+  const void* q; const void* k_new; const void* v_new; const unsigned char* k_c; const unsigned char* v_c;
+  const unsigned long long* tree;      // [B][T]
+  const int64_t* kv_off; const int32_t* kv_len; void* out;
+  int B, H, G, T, R;                   // R = G * T columns
+  int groups;                          // column groups of a head
+  int chunk_rows, max_chunks, slots;
+  float* part; float* part_ml;         // [heads][groups][slots][columns of a group][D], [2]
+  uint32_t* count;                     // Meet::count of the call's first head
+  long long capacity;
+  int page_rows, page_shift, tbl_entries;
+  const int32_t* page_tbl;             // of the call's first head
+  float scale_log2;
+};
+
+// 32 elements of a node's row as the 4-bit cache would have them: in place
+__device__ __forceinline__ void as_mx4(uint4 (&x)[4]) {
+  uint32_t top = 0;
+  uint32_t y[16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { y[4 * i] = x[i].x; y[4 * i + 1] = x[i].y; y[4 * i + 2] = x[i].z; y[4 * i + 3] = x[i].w; }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t lo = min(y[i] & 0x7fffu, 0x7f7fu), hi = min(y[i] >> 16 & 0x7fffu, 0x7f7fu);
+    top = max(top, max(lo, hi));
+    y[i] = (y[i] & 0x80008000u) | lo | hi << 16;
+  }
+  const uint32_t byte = mx_scale_byte(top);
+  const float s = mx_scale_value(byte);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t code = 0;
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(mx_bf16x2_t, y[4 * i]), s, 0);
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(mx_bf16x2_t, y[4 * i + 1]), s, 1);
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(mx_bf16x2_t, y[4 * i + 2]), s, 2);
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(mx_bf16x2_t, y[4 * i + 3]), s, 3);
+    x[i] = mx_decode8(code, byte);
+  }
+}
+// four E4M3 bytes -> four bf16 (exact)
+__device__ __forceinline__ uint2 from_e4m3(uint32_t w) {
+  const df32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  return make_uint2((__float_as_uint(a[0]) >> 16) | (__float_as_uint(a[1]) & 0xffff0000u), (__float_as_uint(b[0]) >> 16) | (__float_as_uint(b[1]) & 0xffff0000u));
+}
+__device__ __forceinline__ uint32_t e4m3_of(uint32_t a, uint32_t b) {          // two bf16 pairs
+  return f32_to_e4m3(bf16_lo(a)) | f32_to_e4m3(bf16_hi(a)) << 8 | f32_to_e4m3(bf16_lo(b)) << 16 | f32_to_e4m3(bf16_hi(b)) << 24;
+}
+
+// T: Q, nodes' rows; CACHE: 0 rows of T, CACHE_E4M3, CACHE_E2M1; WC blocks of 32 columns
+template <typename T, typename OT, int CACHE, int D, int WC>
+__global__ __launch_bounds__(WC * 128) void tree_attn_kernel(TreeArgs a) {
+  using Tile = AttnTile<T, D>;
+  constexpr int PARTS = sizeof(T) == 2 && sizeof(OT) == 4 ? 3 : 1;
+  constexpr int NT = WC * 128, COLS = WC * 32, ROWB = Tile::ROWB, PPR = Tile::PPR;
+  constexpr int EPL = CACHE == CACHE_E2M1 ? 32 : CACHE == CACHE_E4M3 ? 16 : 16 / (int)sizeof(T);      // elements of a 16-byte load
+  constexpr int LPR = D / EPL;                                                                          // loads of a row
+  constexpr int LPT = (ATT_TILE * LPR + NT - 1) / NT;                                                   // of a thread, per tile and tensor
+  constexpr int CROWB = CACHE ? LPR * 16 : ROWB;                                                        // bytes of a cache row
+  constexpr int RES = COLS * (D + 4) * 4;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * Tile::BYTES > RES ? 4 * Tile::BYTES : RES];      // two tiles of K, two of V; later the second halves' results
+  __shared__ float s_ml[COLS][2];
+  __shared__ int s_last;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wc = wave >> 1, wk = wave & 1, half = lane >> 5, col = lane & 31;
+  const uint32_t xy = blockIdx.x + blockIdx.y;                 // the pieces of a head on different XCDs
+  const int x = (int)(xy % gridDim.x), chunk = blockIdx.y;
+  const long long hidx = x / a.groups;
+  const int group = x % a.groups;
+  const int len = a.kv_len[hidx];
+  const long long off = a.kv_off[hidx];
+  const int total = len > 0 ? len + a.T : 0;                   // (an empty segment: its budgets did not fit the cache)
+  int rows = a.chunk_rows;
+  if (total > rows * a.max_chunks) rows = ((total + a.max_chunks - 1) / a.max_chunks + ATT_TILE - 1) / ATT_TILE * ATT_TILE;
+  const int pieces = max(1, (total + rows - 1) / rows);
+  if (chunk >= pieces) return;
+  const int r_begin = chunk * rows, r_end = min(total, r_begin + rows);
+  const int ntiles = (r_end - r_begin + ATT_TILE - 1) / ATT_TILE;
+  RowMap at;
+  at.off = off; at.init_rows = 0x7fffffff; at.tbl = nullptr; at.shift = 0; at.fresh_slot = -1; at.fresh_page = 0;
+  if (a.page_rows) { at.tbl = a.page_tbl + hidx * a.tbl_entries; at.shift = a.page_shift; at.init_rows = at.tbl[0] << a.page_shift; }
+
+  const int c_own = group * COLS + wc * 32 + col, c = min(c_own, a.R - 1);       // (a column without a query: the last one's once more, not stored)
+  typename Tile::Query q[1];
+  Tile::load(q[0], reinterpret_cast<const T*>(a.q) + (hidx * a.R + c) * D, half);
+  const unsigned long long mask = a.tree[(hidx / a.H % a.B) * a.T + c % a.T];
+
+  const unsigned char* kn = reinterpret_cast<const unsigned char*>(a.k_new) + hidx * a.T * ROWB;
+  const unsigned char* vn = reinterpret_cast<const unsigned char*>(a.v_new) + hidx * a.T * ROWB;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
+  // ---- rows of T: straight into LDS, tile t into slot t & 1 (rows past the end of the piece: its last one once more, masked where they are used)
+  const auto load_direct = [&](int t) {
+#pragma unroll
+    for (int j = 0; j < LPT; ++j) {
+      const int p = (wave * LPT + j) * 64 + lane, lr = p / PPR, s = p % PPR;
+      const int r = min(r_begin + t * ATT_TILE + lr, r_end - 1);
+      const bool node = r >= len;
+      const long long row = node ? r - len : at(r);
+      const unsigned char* kp = (node ? kn : a.k_c) + row * ROWB + Tile::k_slot(lr, s) * 16;
+      const unsigned char* vp = (node ? vn : a.v_c) + row * ROWB + Tile::v_slot(lr, s) * 16;
+      const uint32_t to = lds0 + (uint32_t)((t & 1) * Tile::BYTES + (wave * LPT + j) * 1024);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(kp));
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + 2 * Tile::BYTES), "v"(vp));
+    }
+  };
+  // ---- 8-bit and 4-bit rows: through registers
+  struct Raw { uint4 k[CACHE ? LPT : 1], v[CACHE ? LPT : 1]; uint32_t ks[CACHE ? LPT : 1], vs[CACHE ? LPT : 1]; } raw;
+  const auto fetch = [&](int t) {
+#pragma unroll
+    for (int j = 0; j < LPT; ++j) {
+      const int p = j * NT + tid, lr = p / LPR, piece = p % LPR;
+      if (ATT_TILE * LPR % NT && lr >= ATT_TILE) break;
+      const int r = min(r_begin + t * ATT_TILE + lr, r_end - 1);
+      if (r >= len) continue;                                  // (a node's row is read when it is wanted)
+      const long long row = at(r);
+      raw.k[j] = *reinterpret_cast<const uint4*>(a.k_c + row * CROWB + piece * 16);
+      raw.v[j] = *reinterpret_cast<const uint4*>(a.v_c + row * CROWB + piece * 16);
+      if constexpr (CACHE == CACHE_E2M1) {
+        raw.ks[j] = a.k_c[a.capacity * CROWB + row * (D / MX_BLOCK) + piece];
+        raw.vs[j] = a.v_c[a.capacity * CROWB + row * (D / MX_BLOCK) + piece];
+      }
+    }
+  };
+  const auto park = [&](int t) {
+#pragma unroll
+    for (int j = 0; j < LPT; ++j) {
+      const int p = j * NT + tid, lr = p / LPR, piece = p % LPR;
+      if (ATT_TILE * LPR % NT && lr >= ATT_TILE) break;
+      const int r = min(r_begin + t * ATT_TILE + lr, r_end - 1);
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+        unsigned char* to = lds + ((t & 1) + 2 * which) * Tile::BYTES + lr * ROWB;
+        const unsigned char* nodes = which ? vn : kn;
+        uint4 y[EPL / 8 ? EPL / 8 : 1];
+        if (r >= len) {
+          const uint4* from = reinterpret_cast<const uint4*>(nodes + (long long)(r - len) * ROWB + piece * EPL * 2);
+#pragma unroll
+          for (int i = 0; i < EPL / 8; ++i) y[i] = from[i];
+          if constexpr (CACHE == CACHE_E2M1) {
+            as_mx4(y);
+          } else if constexpr (CACHE == CACHE_E4M3) {
+#pragma unroll
+            for (int i = 0; i < EPL / 8; ++i) {
+              const uint2 lo = from_e4m3(e4m3_of(y[i].x, y[i].y)), hi = from_e4m3(e4m3_of(y[i].z, y[i].w));
+              y[i] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            }
+          }
+        } else {
+          const uint4 z = which ? raw.v[j] : raw.k[j];
+          if constexpr (CACHE == CACHE_E2M1) {
+            const uint32_t scale = which ? raw.vs[j] : raw.ks[j];
+            y[0] = mx_decode8(z.x, scale); y[1] = mx_decode8(z.y, scale); y[2] = mx_decode8(z.z, scale); y[3] = mx_decode8(z.w, scale);
+          } else if constexpr (CACHE == CACHE_E4M3) {
+            const uint2 e0 = from_e4m3(z.x), e1 = from_e4m3(z.y), e2 = from_e4m3(z.z), e3 = from_e4m3(z.w);
+            y[0] = make_uint4(e0.x, e0.y, e1.x, e1.y); y[1] = make_uint4(e2.x, e2.y, e3.x, e3.y);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < EPL / 8; ++i) {
+          const int s = which ? Tile::v_slot(lr, piece * (EPL / 8) + i) : Tile::k_slot(lr, piece * (EPL / 8) + i);
+          *reinterpret_cast<uint4*>(to + s * 16) = y[i];
+        }
+      }
+    }
+  };
+
+  AttnState<T, D, 1> st;
+  bool careful = false;
+  const auto compute = [&](int t) {
+    const int k32 = r_begin + t * ATT_TILE + 32 * wk;
+    if (k32 >= r_end) return;
+    const unsigned char* kt = lds + (t & 1) * Tile::BYTES;
+    const unsigned char* vt = lds + (2 + (t & 1)) * Tile::BYTES;
+    at_f32x16_t s[1];
+    float p[16], more;
+    typename Tile::template Weights<PARTS> w[1];
+    Tile::template scores<1>(kt, 32 * wk, lane, q, s);
+    const bool cut = k32 + 32 > min(len, r_end);
+    const auto sees = [&](int key) { const int r = k32 + key; return r < r_end && (r < len || (mask >> (r - len) & 1)); };
+    if (cut) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[0][i] = sees(key_of(i, half)) ? s[0][i] : -__builtin_inff();
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], a.scale_log2, -st.ref[0]));
+    more = sum16(p);
+    if (cut || __builtin_amdgcn_ballot_w64(!(st.sum[0] + more < ATT_FAR))) attn_look<T, D, 1>(st, 0, s[0], p, more, a.scale_log2);
+    st.sum[0] += more;
+    Tile::template pack<PARTS>(p, w[0]);
+    if (careful && (PARTS > 1 || cut)) {
+#pragma unroll 1
+      for (int key = 0; key < 32; ++key) {                     // its weight is with one of the column's lanes, element i of its 16
+        const int i = 4 * (key >> 3) + (key & 3), owner = col + 32 * ((key >> 2) & 1);
+        const float f = __shfl(Tile::template weight<PARTS>(w[0], i), owner, 64);
+        if (!sees(key)) continue;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const at_f32x4_t y = Tile::value4(vt, 32 * wk + key, 32 * db + 8 * g + 4 * half);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) st.o[0][db][4 * g + e] = fmaf(f, y[e], st.o[0][db][4 * g + e]);
+          }
+      }
+    } else {
+      Tile::template add<PARTS, 1>(vt, 32 * wk, lane, w, st.o);
+    }
+  };
+  for (;;) {
+    st.clear();
+    if (ntiles > 0) {
+      if constexpr (CACHE) { fetch(0); park(0); }
+      else load_direct(0);
+    }
+#pragma unroll 1
+    for (int t = 0; t < ntiles; ++t) {
+      // tile t is there for everybody, and nobody reads tile t - 1 any more
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (t + 1 < ntiles) {
+        if constexpr (CACHE) fetch(t + 1);
+        else load_direct(t + 1);
+      }
+      compute(t);
+      if constexpr (CACHE) { if (t + 1 < ntiles) park(t + 1); }
+    }
+    const int again = __syncthreads_or(!careful && not_finite(st));
+    if (!again) break;
+    careful = true;
+  }
+
+  // ---- the two halves of a tile's keys: the second wave of a block leaves its results in LDS, [column][D + 4]
+  float* s_o = reinterpret_cast<float*>(lds) + wc * 32 * (D + 4);
+  float sum = both_sum(st.sum[0]);
+  if (wk) {
+    if (half == 0) { s_ml[wc * 32 + col][0] = st.ref[0]; s_ml[wc * 32 + col][1] = sum; }
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<at_f32x4_t*>(s_o + col * (D + 4) + 32 * db + 8 * g + 4 * half) = at_f32x4_t{st.o[0][db][4 * g], st.o[0][db][4 * g + 1], st.o[0][db][4 * g + 2], st.o[0][db][4 * g + 3]};
+  }
+  __syncthreads();
+  const long long record = hidx * a.groups + group;
+  const __amdgpu_buffer_rsrc_t rec = agent_buffer(a.part + record * a.slots * COLS * D, a.slots * COLS * D * 4);
+  const __amdgpu_buffer_rsrc_t rec_ml = agent_buffer(a.part_ml + record * a.slots * COLS * 2, a.slots * COLS * 8);
+  if (!wk) {
+    const float ref2 = s_ml[wc * 32 + col][0], sum2 = s_ml[wc * 32 + col][1];
+    const float m = fmaxf(st.ref[0], ref2);
+    // (a half that has seen nothing: reference -inf, weight 0)
+    const float f1 = st.ref[0] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(st.ref[0] - m), f2 = ref2 == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ref2 - m);
+    sum = sum * f1 + sum2 * f2;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const at_f32x4_t y = *reinterpret_cast<const at_f32x4_t*>(s_o + col * (D + 4) + 32 * db + 8 * g + 4 * half);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) st.o[0][db][4 * g + e] = st.o[0][db][4 * g + e] * f1 + y[e] * f2;
+      }
+    if (pieces == 1) {
+      store_column<OT, D>(reinterpret_cast<OT*>(a.out) + (hidx * a.R + c) * D, c == c_own, half, st.o[0], 1.f / sum);
+    } else {
+      const int cc = wc * 32 + col;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(du32x4_t, at_f32x4_t{st.o[0][db][4 * g], st.o[0][db][4 * g + 1], st.o[0][db][4 * g + 2], st.o[0][db][4 * g + 3]}), rec,
+                                                 (cc * D + 32 * db + 8 * g + 4 * half) * 4, chunk * (COLS * D * 4), AGENT);
+      if (half == 0) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(du32x2_t, make_float2(m, sum)), rec_ml, cc * 8, chunk * (COLS * 8), AGENT);
+    }
+  }
+  if (pieces == 1) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // the wave's stores are where everybody sees them
+  __syncthreads();
+  if (tid == 0) {
+    uint32_t* count = a.count + (hidx * a.G + group) * MEET_COUNT_STRIDE;
+    const uint32_t arrived = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    s_last = arrived + 1u == (uint32_t)pieces;
+    if (s_last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (!s_last) return;
+  // ---- the last one: four dims of a column per thread
+  constexpr int TL = D / 4, MB = 8;
+  const int t4 = tid % TL;
+  for (int cc = tid / TL; cc < min(COLS, a.R - group * COLS); cc += NT / TL) {
+    float m = -__builtin_inff(), l = 0.f;
+    at_f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    for (int c0 = 0; c0 < pieces; c0 += MB) {
+      at_f32x4_t y[MB]; float2 ml[MB];
+#pragma unroll
+      for (int j = 0; j < MB; ++j) {
+        const bool there = c0 + j < pieces;
+        ml[j] = __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(rec_ml, there ? (c0 + j) * (COLS * 8) + cc * 8 : NOWHERE, 0, AGENT));
+        y[j] = __builtin_bit_cast(at_f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rec, there ? (c0 + j) * (COLS * D * 4) + (cc * D + 4 * t4) * 4 : NOWHERE, 0, AGENT));
+      }
+      float bm = m;
+#pragma unroll
+      for (int j = 0; j < MB; ++j) {
+        if (c0 + j >= pieces) ml[j].x = -__builtin_inff();
+        bm = fmaxf(bm, ml[j].x);
+      }
+      const float f = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - bm);
+      l *= f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] *= f;
+#pragma unroll
+      for (int j = 0; j < MB; ++j) {
+        const float g = ml[j].x == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ml[j].x - bm);
+        l = fmaf(ml[j].y, g, l);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(y[j][e], g, o[e]);
+      }
+      m = bm;
+    }
+    OT* to = reinterpret_cast<OT*>(a.out) + (hidx * a.R + group * COLS + cc) * D + 4 * t4;
+    const float inv = 1.f / l;
+    if constexpr (sizeof(OT) == 4) {
+      *reinterpret_cast<at_f32x4_t*>(to) = at_f32x4_t{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    } else {
+      *reinterpret_cast<uint2*>(to) = make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector((at_f32x2_t{o[0] * inv, o[1] * inv}), at_bf16x2_t)),
+                                                 __builtin_bit_cast(uint32_t, __builtin_convertvector((at_f32x2_t{o[2] * inv, o[3] * inv}), at_bf16x2_t)));
+    }
+  }
+}
+
+// Blocks of columns of a workgroup, workgroups of a head side by side, rows per piece, most pieces, pieces of the grid.
+struct TreePlan { int wc, groups, chunk_rows, max_chunks, slots; };
+static TreePlan tree_plan(const Dims& dm, const madakv_config& c, int T, int longest_rows) {
+  TreePlan p;
+  const int R = dm.G * T;
+  p.wc = R <= 32 ? 1 : R <= 64 ? 2 : 4;
+  p.groups = (R + 32 * p.wc - 1) / (32 * p.wc);                // (at most G, which is how many counters a head has: T <= 32 wc)
+  const long long typical = std::min(c.budget, c.ctx_len) + (long long)T;
+  const long long want = std::max<long long>(1, 512 / ((long long)dm.heads * p.groups));
+  p.chunk_rows = (int)std::max<long long>(128, (typical / want + ATT_TILE - 1) / ATT_TILE * ATT_TILE);
+  p.max_chunks = (int)((std::max(2, c.hcc_rho) * typical + p.chunk_rows - 1) / p.chunk_rows);
+  const int longest = std::max(1, std::min(longest_rows, c.ctx_len + c.max_new_tokens)) + T;
+  p.slots = std::min(p.max_chunks, (longest + p.chunk_rows - 1) / p.chunk_rows);
+  return p;
+}
+size_t tree_ws_bytes(const Dims& dm, const madakv_config& c, int T, int longest_rows) {
+  const TreePlan p = tree_plan(dm, c, T, longest_rows);
+  return p.slots == 1 ? 16 : (size_t)dm.heads * p.groups * p.slots * p.wc * 32 * (dm.d + 2) * sizeof(float);
+}
+
+template <typename T, typename OT, int CACHE, int D>
+static hipError_t launch_tree(const Dims& dm, const TreeArgs& a, const TreePlan& p, hipStream_t st) {
+  const dim3 grid(dm.heads * p.groups, p.slots);
+  if (p.wc == 1) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 1>), grid, dim3(128), 0, st, a);
+  else if (p.wc == 2) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 2>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 4>), grid, dim3(512), 0, st, a);
+  return hipGetLastError();
+}
+template <typename T, typename OT, int CACHE>
+static hipError_t launch_tree_d(const Dims& dm, const TreeArgs& a, const TreePlan& p, hipStream_t st) {
+  return dm.d == 128 ? launch_tree<T, OT, CACHE, 128>(dm, a, p, st) : launch_tree<T, OT, CACHE, 64>(dm, a, p, st);
+}
+template <int CACHE>
+static hipError_t launch_tree_o(const Dims& dm, const madakv_config& c, const TreeArgs& a, const TreePlan& p, hipStream_t st) {
+  return c.out_fp32 ? launch_tree_d<uint16_t, float, CACHE>(dm, a, p, st) : launch_tree_d<uint16_t, uint16_t, CACHE>(dm, a, p, st);
+}
+hipError_t launch_tree_attn(const Dims& dm, const madakv_config& c, int T, const void* q, const void* k_new, const void* v_new, const void* tree, const void* k_c,
+                            const void* v_c, const int64_t* kv_off, const int32_t* kv_len, void* out, const Meet& meet, void* ws, long long capacity_tokens, int longest_rows,
+                            const Paging& pg, int layer0, hipStream_t st) {
+  const TreePlan p = tree_plan(dm, c, T, longest_rows);
+  const long long head0 = (long long)layer0 * dm.B * dm.H;
+  TreeArgs a;
+  a.q = q; a.k_new = k_new; a.v_new = v_new; a.k_c = static_cast<const unsigned char*>(k_c); a.v_c = static_cast<const unsigned char*>(v_c);
+  a.tree = static_cast<const unsigned long long*>(tree); a.kv_off = kv_off; a.kv_len = kv_len; a.out = out;
+  a.B = dm.B; a.H = dm.H; a.G = dm.G; a.T = T; a.R = dm.G * T; a.groups = p.groups;
+  a.chunk_rows = p.chunk_rows; a.max_chunks = std::min(p.max_chunks, p.slots); a.slots = p.slots;
+  a.part = static_cast<float*>(ws); a.part_ml = a.part + (size_t)dm.heads * p.groups * p.slots * p.wc * 32 * dm.d;
+  a.count = meet.count + head0 * dm.G * MEET_COUNT_STRIDE;
+  a.capacity = capacity_tokens;
+  a.page_rows = pg.page_rows; a.tbl_entries = pg.entries; a.page_shift = 0;
+  while (pg.page_rows && (1 << a.page_shift) < pg.page_rows) ++a.page_shift;
+  a.page_tbl = pg.page_rows ? pg.table + head0 * pg.entries : nullptr;
+  a.scale_log2 = (c.softmax_scale > 0.f ? c.softmax_scale : 1.0f / sqrtf((float)dm.d)) * 1.4426950408889634f;
+  if (c.dtype != MADAKV_BF16) return launch_tree_d<float, float, 0>(dm, a, p, st);
+  if (c.cache_fp8 == CACHE_E2M1) return launch_tree_o<CACHE_E2M1>(dm, c, a, p, st);
+  if (c.cache_fp8 == CACHE_E4M3) return launch_tree_o<CACHE_E4M3>(dm, c, a, p, st);
+  return launch_tree_o<0>(dm, c, a, p, st);
+}
+
+// ---- the accepted nodes' rows ---------------------------------------------------------------------------
+// One workgroup per head.  The new rows' places follow from what the eviction left the head (Meet::len1) and `start`, not from its present
+// length: the call can be repeated, and can take rows back.
+struct CommitArgs {
+  const unsigned char* k_new; const unsigned char* v_new; const int32_t* path; const int32_t* n_path; const int32_t* start;
+  unsigned char* k_c; unsigned char* v_c; const int64_t* kv_off; int32_t* kv_len;
+  const int32_t* len1;                 // of the call's first head
+  int B, H, T, max_path, most;
+  long long capacity;
+  int page_rows, page_shift, tbl_entries;
+  int32_t* page_tbl;                   // of the call's first head
+  unsigned long long* pool_top;
+  long long region_pages;
+};
+
+template <typename T, int CACHE, int D>
+__global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
+  constexpr int EPL = 16 / (int)sizeof(T), LPR = D / EPL;      // elements per thread, threads per row
+  __shared__ int s_path[64];
+  const int tid = threadIdx.x;
+  const long long hidx = blockIdx.x;
+  const int b = (int)(hidx / a.H % a.B);
+  const int kept = a.len1[hidx] - 1, len = a.kv_len[hidx], from = a.start[b];
+  const long long off = a.kv_off[hidx];
+  if (kept <= 0 || len <= 0) return;                           // never evicted, or an empty segment, which stays empty
+  const int have = len - kept;
+  if (from < 0 || from > have || (a.page_rows && from != have)) {
+    // rows that are not there: the head is left as it is, but for what is more than `most`
+    if (!a.page_rows && have > a.most && tid == 0) a.kv_len[hidx] = kept + a.most;
+    return;
+  }
+  int n = max(0, min(min(a.n_path[b], a.max_path), a.most - from));
+  {                                                            // (every wave for itself: an entry that is no node ends the path)
+    const int lane = tid & 63;
+    const int node = lane < n ? a.path[b * a.max_path + lane] : 0;
+    const unsigned long long bad = __builtin_amdgcn_ballot_w64(lane < n && (node < 0 || node >= a.T));
+    if (bad) n = min(n, (int)__builtin_ctzll(bad));
+    if (tid < 64) s_path[tid] = node;
+  }
+  RowMap at;
+  at.off = off; at.init_rows = 0x7fffffff; at.tbl = nullptr; at.shift = 0; at.fresh_slot = -1; at.fresh_page = 0;
+  if (a.page_rows) {
+    int32_t* tbl = a.page_tbl + hidx * a.tbl_entries;
+    at.tbl = tbl; at.shift = a.page_shift; at.init_rows = tbl[0] << a.page_shift;
+    if (tid == 0) {
+      const int q0 = len - at.init_rows, P = a.page_rows;
+      const int j0 = q0 <= 0 ? 0 : (q0 + P - 1) >> a.page_shift, j1 = q0 + n <= 0 ? 0 : (q0 + n + P - 1) >> a.page_shift;     // pages the head has, will have
+      if (j1 > j0) {
+        const unsigned long long nth = atomicAdd(a.pool_top + b, (unsigned long long)(j1 - j0));
+        for (int j = j0; j < j1; ++j) tbl[1 + j] = (int32_t)((b + 1) * a.region_pages - 1 - (long long)nth - (j - j0));
+      }
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < n * 2 * LPR; i += 256) {
+    const int which = i / LPR & 1, piece = i % LPR, step = i / (2 * LPR);
+    const unsigned char* src = (which ? a.v_new : a.k_new) + ((hidx * a.T + s_path[step]) * D + piece * EPL) * (long long)sizeof(T);
+    const uint4 x = *reinterpret_cast<const uint4*>(src);
+    const long long row = at(kept + from + step);
+    unsigned char* cache = which ? a.v_c : a.k_c;
+    if constexpr (CACHE == 0) {
+      *reinterpret_cast<uint4*>(cache + (row * D + piece * EPL) * (long long)sizeof(T)) = x;
+    } else if constexpr (CACHE == CACHE_E4M3) {
+      *reinterpret_cast<uint2*>(cache + row * D + piece * EPL) = make_uint2(e4m3_of(x.x, x.y), e4m3_of(x.z, x.w));
+    } else {                                                   // (rows are whole quads of threads)
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+      uint32_t scale;
+      const uint32_t code = mx_encode8(w, scale);
+      *reinterpret_cast<uint32_t*>(cache + row * (D / 2) + piece * 4) = code;
+      if ((piece & 3) == 0) cache[a.capacity * (D / 2) + row * (D / MX_BLOCK) + piece / 4] = (uint8_t)scale;
+    }
+  }
+  if (tid == 0) a.kv_len[hidx] = kept + from + n;
+}
+
+template <typename T, int CACHE>
+static hipError_t launch_commit(const Dims& dm, const CommitArgs& a, hipStream_t st) {
+  if (dm.d == 128) hipLaunchKernelGGL((tree_commit_kernel<T, CACHE, 128>), dim3(dm.heads), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((tree_commit_kernel<T, CACHE, 64>), dim3(dm.heads), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+hipError_t launch_tree_commit(const Dims& dm, const madakv_config& c, int T, const void* k_new, const void* v_new, const int32_t* path, const int32_t* n_path, int max_path,
+                              const int32_t* start, int most, void* k_c, void* v_c, const int64_t* kv_off, int32_t* kv_len, const Meet& meet, long long capacity_tokens,
+                              const Paging& pg, int layer0, hipStream_t st) {
+  const long long head0 = (long long)layer0 * dm.B * dm.H;
+  CommitArgs a;
+  a.k_new = static_cast<const unsigned char*>(k_new); a.v_new = static_cast<const unsigned char*>(v_new); a.path = path; a.n_path = n_path; a.start = start;
+  a.k_c = static_cast<unsigned char*>(k_c); a.v_c = static_cast<unsigned char*>(v_c); a.kv_off = kv_off; a.kv_len = kv_len; a.len1 = meet.len1 + head0;
+  a.B = dm.B; a.H = dm.H; a.T = T; a.max_path = max_path; a.most = most; a.capacity = capacity_tokens;
+  a.page_rows = pg.page_rows; a.tbl_entries = pg.entries; a.page_shift = 0;
+  while (pg.page_rows && (1 << a.page_shift) < pg.page_rows) ++a.page_shift;
+  a.page_tbl = pg.page_rows ? pg.table + head0 * pg.entries : nullptr; a.pool_top = pg.pool_top;
+  a.region_pages = pg.page_rows ? pg.region_tokens / pg.page_rows : 0;
+  if (c.dtype != MADAKV_BF16) return launch_commit<float, 0>(dm, a, st);
+  if (c.cache_fp8 == CACHE_E2M1) return launch_commit<uint16_t, CACHE_E2M1>(dm, a, st);
+  if (c.cache_fp8 == CACHE_E4M3) return launch_commit<uint16_t, CACHE_E4M3>(dm, a, st);
+  return launch_commit<uint16_t, 0>(dm, a, st);
+}
+
+}  // namespace madakv
