@@ -1,5 +1,5 @@
 // Attention of many query rows over tiles of 64 keys that lie in LDS: what the kernels of prompt attention and of attention of a
-// drafted tree share.  A wave owns NQ blocks of 32 query rows ("columns": they are operand B) and keeps their softmax and output in
+// drafted tree share.  A wave owns 32 query rows ("columns": they are operand B) and keeps their softmax and output in
 // registers; K and V of a tile are operand A.
 //   S^T[key][col] = K . Q^T      a lane then has 16 of 32 keys for ONE column, lane i and lane i + 32 the two halves: maximum, sum
 //                                and weights of a column are in-lane work
@@ -59,25 +59,28 @@ template <int D> struct AttnTile<uint16_t, D> {
   static constexpr int DB = D / 32;             // blocks of 32 dims of the output
   struct Query { at_bf16x8_t x[KS]; };
   template <int PARTS> struct Weights { at_bf16x8_t part[PARTS][2]; };          // of 32 keys, as operand B
-  static __device__ __forceinline__ int k_slot(int row, int piece) { return piece ^ (row % PPR); }
+  static __device__ __forceinline__ int k_slot(int row, int piece) { return piece ^ (D == 128 ? row & 15 : row >> 1 & 7); }
   static __device__ __forceinline__ int v_slot(int row, int piece) { return piece ^ (D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1)); }
   // a column's query: for step ks elements [half D/2 + 8 ks, + 8)
   static __device__ __forceinline__ void load(Query& q, const uint16_t* row, int half) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) q.x[ks] = *reinterpret_cast<const at_bf16x8_t*>(row + half * (D / 2) + ks * 8);
   }
-  // logits of the 32 keys from row0 of the tile on, against NQ blocks of columns
-  template <int NQ>
-  static __device__ __forceinline__ void scores(const unsigned char* kt, int row0, int lane, const Query (&q)[NQ], at_f32x16_t (&s)[NQ]) {
-    const int half = lane >> 5, row = row0 + (lane & 31);
+  // (here and now: a wait for the query in a loop would be one for the tiles on their way as well)
+  static __device__ __forceinline__ void await(Query& q) {
 #pragma unroll
-    for (int b = 0; b < NQ; ++b) s[b] = zero16();
+    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(q.x[ks]));
+  }
+  // logits of the 32 keys from row0 of the tile on
+  static __device__ __forceinline__ at_f32x16_t scores(const unsigned char* kt, int row0, int lane, const Query& q) {
+    const int half = lane >> 5, row = row0 + (lane & 31);
+    at_f32x16_t s = zero16();
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const at_bf16x8_t a = *reinterpret_cast<const at_bf16x8_t*>(kt + row * ROWB + k_slot(row, half * KS + ks) * 16);
-#pragma unroll
-      for (int b = 0; b < NQ; ++b) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[b].x[ks], s[b], 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q.x[ks], s, 0, 0, 0);
     }
+    return s;
   }
   template <int PARTS>
   static __device__ __forceinline__ void pack(const float (&p)[16], Weights<PARTS>& w) {
@@ -110,8 +113,8 @@ template <int D> struct AttnTile<uint16_t, D> {
     return x;
   }
   // output += V^T . P^T over the 32 keys from row0 on
-  template <int PARTS, int NQ>
-  static __device__ __forceinline__ void add(const unsigned char* vt, int row0, int lane, const Weights<PARTS> (&w)[NQ], at_f32x16_t (&o)[NQ][DB]) {
+  template <int PARTS>
+  static __device__ __forceinline__ void add(const unsigned char* vt, int row0, int lane, const Weights<PARTS>& w, at_f32x16_t (&o)[DB]) {
     // A transposing read takes, per 16 lanes, four rows of 16 dims: lane j points at dims 4 (j & 3).. of row j >> 2 and gets dim j of
     // the four rows.  Lanes 0-15 take dims 0-15, 16-31 dims 16-31 of keys 0-3, lanes 32-63 the same of keys 4-7.
     const int half = lane >> 5, r = row0 + 4 * half + ((lane & 15) >> 2);
@@ -127,9 +130,7 @@ template <int D> struct AttnTile<uint16_t, D> {
         const at_s16x4_t v0 = read(r + 16 * s), v1 = read(r + 16 * s + 8);
         const at_bf16x8_t a = __builtin_bit_cast(at_bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-        for (int b = 0; b < NQ; ++b)
-#pragma unroll
-          for (int k = PARTS - 1; k >= 0; --k) o[b][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w[b].part[k][s], o[b][db], 0, 0, 0);
+        for (int k = PARTS - 1; k >= 0; --k) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w.part[k][s], o[db], 0, 0, 0);
       }
   }
   // four neighbouring dims of a row of V
@@ -166,22 +167,23 @@ template <int D> struct AttnTile<float, D> {
       for (int e = 0; e < 4; ++e) q.x[4 * i + e] = x[e];
     }
   }
-  template <int NQ>
-  static __device__ __forceinline__ void scores(const unsigned char* kt, int row0, int lane, const Query (&q)[NQ], at_f32x16_t (&s)[NQ]) {
-    const int half = lane >> 5, row = row0 + (lane & 31);
+  static __device__ __forceinline__ void await(Query& q) {
 #pragma unroll
-    for (int b = 0; b < NQ; ++b) s[b] = zero16();
+    for (int i = 0; i < D / 2; ++i) asm volatile("" : "+v"(q.x[i]));
+  }
+  static __device__ __forceinline__ at_f32x16_t scores(const unsigned char* kt, int row0, int lane, const Query& q) {
+    const int half = lane >> 5, row = row0 + (lane & 31);
+    at_f32x16_t s = zero16();
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) {
       const at_f32x4_t a = *reinterpret_cast<const at_f32x4_t*>(kt + row * ROWB + k_slot(row, half * (D / 8) + i) * 16);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int b = 0; b < NQ; ++b) s[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], q[b].x[4 * i + e], s[b], 0, 0, 0);
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], q.x[4 * i + e], s, 0, 0, 0);
     }
+    return s;
   }
-  template <int PARTS, int NQ>
-  static __device__ __forceinline__ void add(const unsigned char* vt, int row0, int lane, const Weights<PARTS> (&w)[NQ], at_f32x16_t (&o)[NQ][DB]) {
+  template <int PARTS>
+  static __device__ __forceinline__ void add(const unsigned char* vt, int row0, int lane, const Weights<PARTS>& w, at_f32x16_t (&o)[DB]) {
     const int half = lane >> 5;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -190,8 +192,7 @@ template <int D> struct AttnTile<float, D> {
       for (int db = 0; db < DB; ++db) {
         const int dim = 32 * db + (lane & 31);
         const float a = *reinterpret_cast<const float*>(vt + row * ROWB + v_slot(row, dim / 4) * 16 + (dim & 3) * 4);
-#pragma unroll
-        for (int b = 0; b < NQ; ++b) o[b][db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[b].x[i], o[b][db], 0, 0, 0);
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.x[i], o[db], 0, 0, 0);
       }
     }
   }
@@ -200,18 +201,15 @@ template <int D> struct AttnTile<float, D> {
   }
 };
 
-// What a wave holds of a block of 32 columns: the lane's column, half of its keys in ref / sum (ref is the same in both lanes of a
-// column), dims key_of(i, half) of each block of 32 in o.
-template <typename T, int D, int NQ> struct AttnState {
-  float ref[NQ], sum[NQ];                       // log2 units, -inf: nothing seen yet
-  at_f32x16_t o[NQ][D / 32];
+// What a wave holds of its columns: a lane has half of the keys of one column in sum (ref is the same in both lanes of a column), dims
+// key_of(i, half) of each block of 32 in o.
+template <int D> struct AttnState {
+  float ref, sum;                               // ref: log2 units, -inf: nothing seen yet
+  at_f32x16_t o[D / 32];
   __device__ __forceinline__ void clear() {
+    ref = -__builtin_inff(); sum = 0.f;
 #pragma unroll
-    for (int b = 0; b < NQ; ++b) {
-      ref[b] = -__builtin_inff(); sum[b] = 0.f;
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db) o[b][db] = zero16();
-    }
+    for (int db = 0; db < D / 32; ++db) o[db] = zero16();
   }
 };
 
@@ -245,15 +243,13 @@ __device__ __forceinline__ void store_column(OT* to, bool mine, int half, const 
   }
 }
 // what is not finite anywhere in a wave's output
-template <typename T, int D, int NQ>
-__device__ __forceinline__ bool not_finite(const AttnState<T, D, NQ>& st) {
+template <int D>
+__device__ __forceinline__ bool not_finite(const AttnState<D>& st) {
   float z = 0.f;
 #pragma unroll
-  for (int b = 0; b < NQ; ++b)
+  for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) z = fmaf(st.o[b][db][i], 0.f, z);
+    for (int i = 0; i < 16; ++i) z = fmaf(st.o[db][i], 0.f, z);
   return z != z;
 }
 
@@ -261,31 +257,50 @@ __device__ __forceinline__ float sum16(const float (&p)[16]) {
   return (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]))) + (((p[8] + p[9]) + (p[10] + p[11])) + ((p[12] + p[13]) + (p[14] + p[15])));
 }
 
-// The logits of a subtile of one block of columns -> weights and their sum t, against the column's reference, which moves where it has to:
+// What another wave has of the same columns from other keys, added: its reference and sum, its output [dims].  (One that has seen nothing: reference
+// -inf, weight 0.)
+template <int D>
+__device__ __forceinline__ void merge_halves(AttnState<D>& st, float& sum, const float (&ml)[2], const float* o, int half) {
+  const float m = fmaxf(st.ref, ml[0]);
+  const float f1 = st.ref == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(st.ref - m), f2 = ml[0] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m);
+  // (what is no number stays none)
+  sum = (st.ref == -__builtin_inff() && sum == 0.f ? 0.f : sum * f1) + (ml[0] == -__builtin_inff() && ml[1] == 0.f ? 0.f : ml[1] * f2);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const at_f32x4_t y = *reinterpret_cast<const at_f32x4_t*>(o + 32 * db + 8 * g + 4 * half);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) st.o[db][4 * g + e] = st.o[db][4 * g + e] * f1 + y[e] * f2;
+    }
+  st.ref = m;
+}
+
+// The logits of a subtile -> weights and their sum t, against the column's reference, which moves where it has to:
 // where a column has none yet, has left it far behind, or holds no number.  s: masked logits are -inf.
-template <typename T, int D, int NQ>
-__device__ __forceinline__ void attn_look(AttnState<T, D, NQ>& st, int b, const at_f32x16_t& s, float (&p)[16], float& t, float scale_log2) {
+template <int D>
+__device__ __forceinline__ void attn_look(AttnState<D>& st, const at_f32x16_t& s, float (&p)[16], float& t, float scale_log2) {
   float top = s[0];
 #pragma unroll
   for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
   top = both_max(top) * scale_log2;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale_log2, -st.ref[b]));
+  for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale_log2, -st.ref));
   t = sum16(p);
-  if (both_sum(st.sum[b] + t) < ATT_FAR) return;         // (the same in both lanes of a column; not: no number)
+  if (both_sum(st.sum + t) < ATT_FAR) return;         // (the same in both lanes of a column; not: no number)
   if (top > -__builtin_inff()) {
-    const float r = fmaxf(st.ref[b], top);
-    const float f = st.ref[b] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(st.ref[b] - r);
-    st.sum[b] *= f;
+    const float r = fmaxf(st.ref, top);
+    const float f = st.ref == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(st.ref - r);
+    st.sum *= f;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) st.o[b][db][i] *= f;
-    st.ref[b] = r;
+      for (int i = 0; i < 16; ++i) st.o[db][i] *= f;
+    st.ref = r;
 #pragma unroll
     for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale_log2, -r));
     t = sum16(p);
-  } else if (st.ref[b] == -__builtin_inff()) {           // nothing but masked keys, and nothing before
+  } else if (st.ref == -__builtin_inff()) {           // nothing but masked keys, and nothing before
     bool number = true;
 #pragma unroll
     for (int i = 0; i < 16; ++i) number = number && s[i] == s[i];

@@ -153,7 +153,7 @@ hipError_t launch_prompt_attn(const Dims& dm, const madakv_config& c, const void
 constexpr int TREE_NODES = 64;           // most nodes of a tree: a node's mask is one word
 size_t tree_ws_bytes(const Dims& dm, const madakv_config& c, int T, int longest_rows);
 hipError_t launch_tree_attn(const Dims& dm, const madakv_config& c, int T, const void* q, const void* k_new, const void* v_new, const void* tree, const void* k_c,
-                            const void* v_c, const int64_t* kv_off, const int32_t* kv_len, void* out, const Meet& meet, void* ws, long long capacity_tokens, int longest_rows,
+                            const void* v_c, const int64_t* kv_off, const int32_t* kv_len, void* out, void* ws, long long capacity_tokens, int longest_rows,
                             const Paging& pg, int layer0, hipStream_t st);
 hipError_t launch_tree_commit(const Dims& dm, const madakv_config& c, int T, const void* k_new, const void* v_new, const int32_t* path, const int32_t* n_path, int max_path,
                               const int32_t* start, int most, void* k_c, void* v_c, const int64_t* kv_off, int32_t* kv_len, const Meet& meet, long long capacity_tokens,

@@ -888,7 +888,7 @@ int32_t madakv_tree_attn(madakv_handle* h, int32_t layer0, int32_t n, int32_t n_
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   // (a layer that a captured step appends to may be longer than the host knows)
   const int longest = longest_rows(h, layer0, n, replayed_later(st), true);
-  return hip_fail(h, launch_tree_attn(dm, c, n_nodes, q, k_new, v_new, tree, k_c, v_c, kv_off, kv_len, out, h->meet, ws, region_tokens(c) * c.batch, longest,
+  return hip_fail(h, launch_tree_attn(dm, c, n_nodes, q, k_new, v_new, tree, k_c, v_c, kv_off, kv_len, out, ws, region_tokens(c) * c.batch, longest,
                                       make_paging(h), layer0, st));
 }
 

@@ -10,6 +10,7 @@
 #include "attn_tile.h"
 
 #include <algorithm>
+#include <climits>
 
 namespace madakv {
 
@@ -23,43 +24,54 @@ __device__ __forceinline__ at_u32x4_t buffer_words(const void* p, int bytes) {
   return at_u32x4_t{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)u), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32)), (uint32_t)bytes, 0x00020000u};
 }
 
+constexpr int PA_WAVES = 4;
+
 struct PromptAttnArgs {
   const void* q; const void* k; const void* v;       // [n, B, Hq, L, d], [n, B, H, L, d]
   void* out; float* row_lse;                         // row_lse null: not wanted
   const int32_t* seq_off;                            // [B][n_seq + 1] or null
   int n_seq, B, Hq, G, L;
-  int blocks, total;                                 // workgroups of a query head, of all
+  int blocks, heads;                                 // workgroups of a query head, query heads
   float scale_log2;
 };
 
-// T: Q, K, V; OT: out (bf16 bits or float); NW waves of 32 NQ rows
-template <typename T, typename OT, int D, int NW, int NQ>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 && NQ == 1 ? 2 : 1, sizeof(T) == 2 && NQ == 1 ? 2 : 1))) void prompt_attn_kernel(PromptAttnArgs a) {
+// T: Q, K, V; OT: out (bf16 bits or float); WK waves share 32 rows and take halves of every tile; WAVES: of a SIMD
+template <typename T, typename OT, int D, int WK, int WAVES>
+__global__ __launch_bounds__(PA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) void prompt_attn_kernel(PromptAttnArgs a) {
   using Tile = AttnTile<T, D>;
   constexpr int PARTS = sizeof(T) == 2 && sizeof(OT) == 4 ? 3 : 1;
-  constexpr int WR = NQ * 32, BQ = NW * WR, ROWB = Tile::ROWB, PPR = Tile::PPR;
+  constexpr int NW = PA_WAVES, BQ = NW / WK * 32, ROWB = Tile::ROWB, PPR = Tile::PPR;
   constexpr int LPT = ATT_TILE * PPR / (NW * 64);    // load instructions per wave, tile and tensor, 1 KB each
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * Tile::BYTES];       // two tiles of K, two of V
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * Tile::BYTES];       // two tiles of K, two of V; with WK = 2 the second halves' results
   __shared__ int s_start[BQ], s_base;
+  __shared__ float s_ml[WK == 2 ? BQ : 1][2];
 
-  const int per_xcd = (a.total + 7) / 8;
-  const int idx = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-  if (idx >= a.total || (int)(blockIdx.x >> 3) >= per_xcd) return;
-  const int qh = idx / a.blocks, r0 = (a.blocks - 1 - (idx - qh * a.blocks)) * BQ;       // (rows that see the most first)
+  // Workgroup -> query head and block of rows.  Workgroups go to the 8 XCDs in turn: each takes an eighth of the heads one after the other, whose
+  // keys its L2 then holds, and an eighth of the blocks of the heads that are left; those that see the most keys first.
+  const int xcd = (int)(blockIdx.x & 7), nth = (int)(blockIdx.x >> 3), whole = a.heads / 8, rest = a.heads % 8;
+  int qh, rb;
+  if (nth < whole * a.blocks) {
+    qh = xcd * whole + nth / a.blocks;
+    rb = nth % a.blocks;
+  } else {
+    const int m = (nth - whole * a.blocks) * 8 + xcd;
+    if (m >= rest * a.blocks) return;
+    qh = whole * 8 + m % rest;
+    rb = m / rest;
+  }
+  const int r0 = (a.blocks - 1 - rb) * BQ;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, col = lane & 31;
 
   // the rows [first, end) that are in some sequence, the start of every row's own
-  int first = 0, end = a.L, kmin = 0, start[NQ];
-  const int w0 = r0 + wave * WR;
-#pragma unroll
-  for (int b = 0; b < NQ; ++b) start[b] = 0;
+  int first = 0, end = a.L, kmin = 0, start = 0;
+  const int block = wave / WK, wk = wave % WK, w0 = r0 + block * 32;
   if (a.seq_off) {
     const int32_t* off = a.seq_off + (long long)(qh / a.Hq % a.B) * (a.n_seq + 1);
     first = max(off[0], 0);
     end = min(off[a.n_seq], a.L);
     if (r0 >= end || r0 + BQ <= first) return;
-    for (int i = tid; i < BQ; i += NW * 64) s_start[i] = 0;
+    if (tid < BQ) s_start[tid] = 0;
     if (tid == 0) s_base = 0;
     __syncthreads();
     for (int i = tid; i < a.n_seq; i += NW * 64) {
@@ -69,46 +81,26 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
     }
     __syncthreads();
     kmin = r0 >= first ? s_base : first;
-    // the latest start in front of every row: a running maximum, 32 rows at a time
-    int carry = s_base;
-    for (int c = 0; c < (wave + 1) * NQ; ++c) {
-      int x = s_start[c * 32 + col];
-      for (int s = 1; s < 32; s *= 2) { const int y = __shfl_up(x, s, 32); x = col >= s ? max(x, y) : x; }
-      x = max(x, carry);
-      carry = __builtin_amdgcn_readlane(x, 31);
-#pragma unroll
-      for (int b = 0; b < NQ; ++b) start[b] = c == wave * NQ + b ? x : start[b];
+    start = s_base;                                  // the latest start in front of every row: a running maximum, 32 rows at a time
+    for (int c = 0; c <= block; ++c) {
+      const int before = __builtin_amdgcn_readlane(start, 31);
+      start = s_start[c * 32 + col];
+      for (int s = 1; s < 32; s *= 2) { const int y = __shfl_up(start, s, 32); start = col >= s ? max(start, y) : start; }
+      start = max(start, before);
     }
   }
   // the wave's rows [wfirst, wlast]; a column without one has a copy of another one's, which is not stored
-  const int wfirst = max(w0, first), wlast = min(w0 + WR - 1, end - 1);
+  const int wfirst = max(w0, first), wlast = min(w0 + 31, end - 1);
   const bool any = wfirst <= wlast;                  // uniform
-  int row[NQ], min_start = 0, max_start = 0;
-  {
-    int own[NQ];
-#pragma unroll
-    for (int b = 0; b < NQ; ++b) own[b] = start[b];
-    const auto start_of = [&](int r) {               // of row w0 + r, r the same in all lanes
-      int x = __builtin_amdgcn_readlane(own[0], r & 31);
-#pragma unroll
-      for (int b = 1; b < NQ; ++b) { const int y = __builtin_amdgcn_readlane(own[b], r & 31); x = r >= 32 * b ? y : x; }
-      return x;
-    };
-    if (any) { min_start = start_of(wfirst - w0); max_start = start_of(wlast - w0); }       // (starts ascend)
-#pragma unroll
-    for (int b = 0; b < NQ; ++b) {
-      const int r = w0 + 32 * b + col;
-      row[b] = any ? min(max(r, wfirst), wlast) : min(r, a.L - 1);
-      start[b] = r < wfirst ? min_start : r > wlast ? max_start : start[b];
-    }
-  }
+  const int row = any ? min(max(w0 + col, wfirst), wlast) : min(w0 + col, a.L - 1);
+  const int min_start = __builtin_amdgcn_readlane(start, any ? wfirst - w0 : 0), max_start = __builtin_amdgcn_readlane(start, any ? wlast - w0 : 0);       // (starts ascend)
+  start = w0 + col < wfirst ? min_start : w0 + col > wlast ? max_start : start;
   const int tile0 = kmin / ATT_TILE, ntiles = (min(r0 + BQ, end) + ATT_TILE - 1) / ATT_TILE - tile0;
-  // the subtiles of 32 keys that the wave's rows see something of, counted from tile0
-  const int u0 = any ? min_start / 32 - tile0 * 2 : 0, u1 = any ? wlast / 32 + 1 - tile0 * 2 : 0;
-
-  typename Tile::Query q[NQ];
-#pragma unroll
-  for (int b = 0; b < NQ; ++b) Tile::load(q[b], reinterpret_cast<const T*>(a.q) + ((long long)qh * a.L + row[b]) * D, half);
+  // The wave's subtiles of 32 keys: of tile t both (number j = 2 t, 2 t + 1), or with WK = 2 one (j = t).  Its rows see something of those from j0 to j1 - 1.
+  const auto first_key = [&](int j) { return (tile0 * 2 + (WK == 2 ? 2 * j + wk : j)) * 32; };
+  const auto row_in_tile = [&](int j) { return (WK == 2 ? wk : j & 1) * 32; };
+  const auto number = [&](int x) { x -= tile0 * 2; return WK == 2 ? (x - wk + 1) >> 1 : x; };          // of the first of them from key 32 x on
+  const int j0 = any ? number(min_start / 32) : 0, j1 = any ? number(wlast / 32 + 1) : 0;
 
   // Tiles -> LDS.  Load j of wave w fills pieces [(w LPT + j) 64, + 64) of the tile, lane i slot P mod PPR of row P / PPR, P = (w LPT +
   // j) 64 + i.  Through buffers that end with the prompt: rows past its end are zeros.
@@ -127,144 +119,182 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
     for (int j = 0; j < LPT; ++j) tile_load(buffer, lds0 + (uint32_t)(slot * Tile::BYTES + (wave * LPT + j) * 1024), off[j], (tile0 + t) * (ATT_TILE * ROWB));
   };
 
-  AttnState<T, D, NQ> st;
+  // Phase t of the loop below reads tile t of K and tile t - WK of V and sends for the ones after them.
+  const auto send = [&](int t) {
+    if (t + 1 < ntiles) issue(kb, koff, (t + 1) & 1, t + 1);
+    const int v = t + 1 - WK;
+    if (v >= 0 && v < ntiles) issue(vb, voff, 2 + (v & 1), v);
+  };
+  send(-1);
+
+  typename Tile::Query q;
+  Tile::load(q, reinterpret_cast<const T*>(a.q) + ((long long)qh * a.L + row) * D, half);
+  Tile::await(q);
+
+  AttnState<D> st;
   using Weights = typename Tile::template Weights<PARTS>;
-  Weights w[NQ], w_next[NQ];                         // of the subtile before the one that s has the logits of
-  at_f32x16_t s[NQ], s_next[NQ];
+  Weights w, w_next;                                 // of the subtile before the one that s has the logits of
+  at_f32x16_t s, s_next;
   bool careful = false;
-  const auto cut = [&](int u) {                      // some row does not see all of the subtile
-    const int k32 = (tile0 * 2 + u) * 32;
+  const auto cut = [&](int j) {                      // some row does not see all of the subtile
+    const int k32 = first_key(j);
     return k32 + 31 > wfirst || k32 < max_start;
   };
-  const auto row_in_tile = [](int u) { return (u & 1) * 32; };
   // logits -> weights against the present references; whether these still serve
-  const auto fast = [&](const at_f32x16_t (&x)[NQ], Weights (&to)[NQ]) {
-    float p[NQ][16], t[NQ];
-    bool far = false;
+  const auto fast = [&](const at_f32x16_t& x, Weights& to) {
+    float p[16];
 #pragma unroll
-    for (int b = 0; b < NQ; ++b) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) p[b][i] = __builtin_amdgcn_exp2f(fmaf(x[b][i], a.scale_log2, -st.ref[b]));
-      t[b] = st.sum[b] + sum16(p[b]);
-      Tile::template pack<PARTS>(p[b], to[b]);
-      far = far || !(t[b] < ATT_FAR);
-    }
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(far) != 0, 0)) return false;
-#pragma unroll
-    for (int b = 0; b < NQ; ++b) st.sum[b] = t[b];
+    for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(x[i], a.scale_log2, -st.ref));
+    const float t = st.sum + sum16(p);
+    Tile::template pack<PARTS>(p, to);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(t < ATT_FAR)) != 0, 0)) return false;
+    st.sum = t;
     return true;
   };
   for (;;) {
     st.clear();
-    issue(kb, koff, 0, 0);
-    // Step u: the logits of subtile u + 1, the weights of subtile u, and what subtile u - 1 adds to the output.  None of them needs another
+    // Step j: the logits of subtile j + 1, the weights of subtile j, and what subtile j - 1 adds to the output.  None of them needs another
     // one's results: the matrix instructions of the first and the last run beside the vector instructions of the second.
-    // Steps 2t - 1 and 2t read tile t of K and tile t - 1 of V.
-#pragma unroll 1
-    for (int t = 0; t <= ntiles; ++t) {
-      // they are there for everybody, and nobody reads the tiles before them any more
+    // Phase t has steps 2 t - 1 and 2 t, or with WK = 2 step t - 1.
+    const auto begin = [&](int t) {
+      // the phase's tiles are there for everybody, and nobody reads those before them any more
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      if (t + 1 < ntiles) issue(kb, koff, (t + 1) & 1, t + 1);
-      if (t < ntiles) issue(vb, voff, 2 + (t & 1), t);
-      const unsigned char* kt = lds + (t & 1) * Tile::BYTES;
-      const unsigned char* vt = lds + (2 + ((t + 1) & 1)) * Tile::BYTES;
-      int u = 2 * t - 1;
-      bool formed = false;                           // the step's logits and sums are there
-      if (__builtin_expect(u - 1 >= u0 && u + 2 < u1 && !cut(u) && !cut(u + 1) && !careful, 1)) {
-        Tile::template scores<NQ>(kt, 0, lane, q, s_next);
-        Tile::template add<PARTS, NQ>(vt, 0, lane, w, st.o);
-        formed = !fast(s, w_next);
-        if (!formed) {
-          ++u;
-          Tile::template scores<NQ>(kt, 32, lane, q, s);
-          Tile::template add<PARTS, NQ>(vt, 32, lane, w_next, st.o);
-          formed = !fast(s_next, w);
-          if (!formed) continue;
-#pragma unroll
-          for (int b = 0; b < NQ; ++b) { const at_f32x16_t x = s[b]; s[b] = s_next[b]; s_next[b] = x; }
-        }
-      }
+      send(t);
+    };
+    const auto k_tile = [&](int t) { return lds + (t & 1) * Tile::BYTES; };
+    const auto v_tile = [&](int t) { return lds + (2 + ((t - WK) & 1)) * Tile::BYTES; };
+    // phases t0 .. t1 - 1: every row sees all keys of their steps
+    const int ja = max(j0 + 1, number((max_start + 31) / 32)), jb = min(j1 - 1, number((wfirst + 1) / 32));          // steps [ja, jb)
+    const int t0 = careful ? INT_MAX : WK == 2 ? ja + 1 : (ja + 2) >> 1, t1 = WK == 2 ? jb + 1 : (jb + 1) >> 1;
+    const int phases = ntiles + WK;
+    int t = 0;
 #pragma unroll 1
-      for (; u <= 2 * t; ++u) {
+    while (t < phases) {
+      begin(t);
+      bool formed = false;                           // the step's logits and sums are there
+      int j = WK == 2 ? t - 1 : 2 * t - 1;
+      if (t >= t0 && t < t1) {
+#pragma unroll 1
+        for (;;) {
+          const unsigned char* kt = k_tile(t);
+          const unsigned char* vt = v_tile(t);
+          j = WK == 2 ? t - 1 : 2 * t - 1;
+          s_next = Tile::scores(kt, row_in_tile(j + 1), lane, q);
+          Tile::template add<PARTS>(vt, row_in_tile(j - 1), lane, w, st.o);
+          formed = !fast(s, w_next);
+          if (formed) break;
+          if constexpr (WK == 1) {
+            ++j;
+            s = Tile::scores(kt, row_in_tile(j + 1), lane, q);
+            Tile::template add<PARTS>(vt, row_in_tile(j - 1), lane, w_next, st.o);
+            formed = !fast(s_next, w);
+            if (formed) {
+              const at_f32x16_t x = s;
+              s = s_next; s_next = x;
+              break;
+            }
+          } else {
+            s = s_next; w = w_next;
+          }
+          ++t;
+          if (t >= t1) break;
+          begin(t);
+        }
+        if (!formed) continue;
+      }
+      const unsigned char* kt = k_tile(t);
+      const unsigned char* vt = v_tile(t);
+#pragma unroll 1
+      for (const int last = WK == 2 ? t - 1 : 2 * t; j <= last; ++j) {
         if (!formed) {
-          if (u + 1 >= u0 && u + 1 < u1) Tile::template scores<NQ>(kt, row_in_tile(u + 1), lane, q, s_next);
-          if (u - 1 >= u0 && u - 1 < u1) {
-            if (careful && (PARTS > 1 || cut(u - 1))) {
+          if (j + 1 >= j0 && j + 1 < j1) s_next = Tile::scores(kt, row_in_tile(j + 1), lane, q);
+          if (j - 1 >= j0 && j - 1 < j1) {
+            if (careful && (PARTS > 1 || cut(j - 1))) {
 #pragma unroll 1
               for (int key = 0; key < 32; ++key) {   // its weight is with one of the column's lanes, element i of its 16
-                const int i = 4 * (key >> 3) + (key & 3), owner = col + 32 * ((key >> 2) & 1), k = (tile0 * 2 + u - 1) * 32 + key;
+                const int i = 4 * (key >> 3) + (key & 3), owner = col + 32 * ((key >> 2) & 1), k = first_key(j - 1) + key;
+                const float x = __shfl(Tile::template weight<PARTS>(w, i), owner, 64);
+                if (k > row || k < start) continue;
 #pragma unroll
-                for (int b = 0; b < NQ; ++b) {
-                  const float x = __shfl(Tile::template weight<PARTS>(w[b], i), owner, 64);
-                  if (k > row[b] || k < start[b]) continue;
+                for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-                  for (int db = 0; db < D / 32; ++db)
+                  for (int g = 0; g < 4; ++g) {
+                    const at_f32x4_t y = Tile::value4(vt, row_in_tile(j - 1) + key, 32 * db + 8 * g + 4 * half);
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                      const at_f32x4_t y = Tile::value4(vt, row_in_tile(u - 1) + key, 32 * db + 8 * g + 4 * half);
-#pragma unroll
-                      for (int e = 0; e < 4; ++e) st.o[b][db][4 * g + e] = fmaf(x, y[e], st.o[b][db][4 * g + e]);
-                    }
-                }
+                    for (int e = 0; e < 4; ++e) st.o[db][4 * g + e] = fmaf(x, y[e], st.o[db][4 * g + e]);
+                  }
               }
             } else {
-              Tile::template add<PARTS, NQ>(vt, row_in_tile(u - 1), lane, w, st.o);
+              Tile::template add<PARTS>(vt, row_in_tile(j - 1), lane, w, st.o);
             }
           }
         }
         formed = false;
-        if (u >= u0 && u < u1) {
-          const int k32 = (tile0 * 2 + u) * 32;
+        if (j >= j0 && j < j1) {
+          float p[16], more;
+          if (cut(j)) {
+            const int k32 = first_key(j);
 #pragma unroll
-          for (int b = 0; b < NQ; ++b) {
-            float p[16], more;
-            if (cut(u)) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const int key = k32 + key_of(i, half);
-                s[b][i] = key <= row[b] && key >= start[b] ? s[b][i] : -__builtin_inff();
-              }
+            for (int i = 0; i < 16; ++i) {
+              const int key = k32 + key_of(i, half);
+              s[i] = key <= row && key >= start ? s[i] : -__builtin_inff();
             }
-            attn_look<T, D, NQ>(st, b, s[b], p, more, a.scale_log2);
-            st.sum[b] += more;
-            Tile::template pack<PARTS>(p, w[b]);
           }
+          attn_look<D>(st, s, p, more, a.scale_log2);
+          st.sum += more;
+          Tile::template pack<PARTS>(p, w);
         }
-#pragma unroll
-        for (int b = 0; b < NQ; ++b) s[b] = s_next[b];
+        s = s_next;
       }
+      ++t;
     }
     // outputs that are no numbers: the formula's, or those of rows of V that nobody may see
     const int again = __syncthreads_or(!careful && any && not_finite(st));
     if (!again) break;
     careful = true;
+    send(-1);
+  }
+  float sum = both_sum(st.sum);
+  if constexpr (WK == 2) {                           // the second half's results go through LDS
+    constexpr int RS = D + 4;
+    static_assert(BQ * RS * 4 <= 4 * Tile::BYTES, "the results must fit the tiles' place");
+    float* result = reinterpret_cast<float*>(lds) + (block * 32 + col) * RS;
+    if (wk) {
+      if (half == 0) { s_ml[block * 32 + col][0] = st.ref; s_ml[block * 32 + col][1] = sum; }
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<at_f32x4_t*>(result + 32 * db + 8 * g + 4 * half) = at_f32x4_t{st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]};
+    }
+    __syncthreads();
+    if (wk) return;
+    merge_halves<D>(st, sum, s_ml[block * 32 + col], result, half);
   }
   if (!any) return;
 
-#pragma unroll
-  for (int b = 0; b < NQ; ++b) {
-    const float sum = both_sum(st.sum[b]);
-    const bool mine = w0 + 32 * b + col == row[b];
-    const long long o = (long long)qh * a.L + row[b];
-    if (a.row_lse && mine && half == 0) a.row_lse[o] = (st.ref[b] + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
-    store_column<OT, D>(reinterpret_cast<OT*>(a.out) + o * D, mine, half, st.o[b], 1.f / sum);
-  }
+  const bool mine = w0 + col == row;
+  const long long o = (long long)qh * a.L + row;
+  if (a.row_lse && mine && half == 0) a.row_lse[o] = (st.ref + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
+  store_column<OT, D>(reinterpret_cast<OT*>(a.out) + o * D, mine, half, st.o, 1.f / sum);
 }
 
-template <typename T, typename OT, int D, int NW, int NQ>
+template <typename T, typename OT, int D, int WK, int WAVES>
 static hipError_t launch_rows(PromptAttnArgs& a, int heads, hipStream_t st) {
-  constexpr int BQ = NW * NQ * 32;
+  constexpr int BQ = PA_WAVES / WK * 32;
   a.blocks = (a.L + BQ - 1) / BQ;
-  a.total = heads * a.blocks;
-  hipLaunchKernelGGL((prompt_attn_kernel<T, OT, D, NW, NQ>), dim3((a.total + 7) / 8 * 8), dim3(NW * 64), 0, st, a);
+  a.heads = heads;
+  const unsigned each = (unsigned)(heads / 8) * a.blocks + (unsigned)((long long)(heads % 8) * a.blocks + 7) / 8;        // of an XCD
+  hipLaunchKernelGGL((prompt_attn_kernel<T, OT, D, WK, WAVES>), dim3(each * 8), dim3(PA_WAVES * 64), 0, st, a);
   return hipGetLastError();
 }
 template <typename T, typename OT, int D>
 static hipError_t launch_pa(PromptAttnArgs& a, int heads, hipStream_t st) {
-  if constexpr (sizeof(T) == 2) {
-    if ((long long)heads * a.L >= 256 * 256) return launch_rows<T, OT, D, 4, 2>(a, heads, st);
-  }
-  return launch_rows<T, OT, D, 4, 1>(a, heads, st);
+  const long long blocks = (long long)heads * ((a.L + 127) / 128);
+  constexpr int WAVES = sizeof(T) == 2 ? 2 : 1;
+  if (blocks <= 512) return launch_rows<T, OT, D, 2, WAVES>(a, heads, st);
+  if constexpr (sizeof(T) == 2 && D == 64) if (blocks > 1536) return launch_rows<T, OT, D, 1, 3>(a, heads, st);
+  return launch_rows<T, OT, D, 1, WAVES>(a, heads, st);
 }
 hipError_t launch_prompt_attn(const Dims& dm, const madakv_config& c, const void* q, const void* k, const void* v, const int32_t* seq_off, int n_seq,
                               void* out, float* row_lse, hipStream_t st) {

@@ -22,12 +22,22 @@ struct TreeArgs {
   int groups;                          // column groups of a head
   int chunk_rows, max_chunks, slots;
   float* part; float* part_ml;         // [heads][groups][slots][columns of a group][D], [2]
-  uint32_t* count;                     // Meet::count of the call's first head
   long long capacity;
   int page_rows, page_shift, tbl_entries;
   const int32_t* page_tbl;             // of the call's first head
   float scale_log2;
 };
+
+// Rows per piece of a head of so many (rows and nodes), and how many pieces that makes.
+__device__ __forceinline__ int piece_rows(const TreeArgs& a, int total) {
+  if (total <= a.chunk_rows * a.max_chunks) return a.chunk_rows;
+  return ((total + a.max_chunks - 1) / a.max_chunks + ATT_TILE - 1) / ATT_TILE * ATT_TILE;
+}
+__device__ __forceinline__ int pieces_of_tree(const TreeArgs& a, int len) {
+  if (len <= 0) return 1;
+  const int rows = piece_rows(a, len + a.T);
+  return (len + a.T + rows - 1) / rows;
+}
 
 // 32 elements of a node's row as the 4-bit cache would have them: in place
 __device__ __forceinline__ void as_mx4(uint4 (&x)[4]) {
@@ -64,7 +74,7 @@ __device__ __forceinline__ uint32_t e4m3_of(uint32_t a, uint32_t b) {          /
 
 // T: Q, nodes' rows; CACHE: 0 rows of T, CACHE_E4M3, CACHE_E2M1; WC blocks of 32 columns
 template <typename T, typename OT, int CACHE, int D, int WC>
-__global__ __launch_bounds__(WC * 128) void tree_attn_kernel(TreeArgs a) {
+__global__ __launch_bounds__(WC * 128) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 && (WC > 1 || D == 64) ? 2 : 1, 2))) void tree_attn_kernel(TreeArgs a) {
   using Tile = AttnTile<T, D>;
   constexpr int PARTS = sizeof(T) == 2 && sizeof(OT) == 4 ? 3 : 1;
   constexpr int NT = WC * 128, COLS = WC * 32, ROWB = Tile::ROWB, PPR = Tile::PPR;
@@ -75,7 +85,6 @@ __global__ __launch_bounds__(WC * 128) void tree_attn_kernel(TreeArgs a) {
   constexpr int RES = COLS * (D + 4) * 4;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * Tile::BYTES > RES ? 4 * Tile::BYTES : RES];      // two tiles of K, two of V; later the second halves' results
   __shared__ float s_ml[COLS][2];
-  __shared__ int s_last;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wc = wave >> 1, wk = wave & 1, half = lane >> 5, col = lane & 31;
@@ -86,9 +95,7 @@ __global__ __launch_bounds__(WC * 128) void tree_attn_kernel(TreeArgs a) {
   const int len = a.kv_len[hidx];
   const long long off = a.kv_off[hidx];
   const int total = len > 0 ? len + a.T : 0;                   // (an empty segment: its budgets did not fit the cache)
-  int rows = a.chunk_rows;
-  if (total > rows * a.max_chunks) rows = ((total + a.max_chunks - 1) / a.max_chunks + ATT_TILE - 1) / ATT_TILE * ATT_TILE;
-  const int pieces = max(1, (total + rows - 1) / rows);
+  const int rows = piece_rows(a, total), pieces = pieces_of_tree(a, len);
   if (chunk >= pieces) return;
   const int r_begin = chunk * rows, r_end = min(total, r_begin + rows);
   const int ntiles = (r_end - r_begin + ATT_TILE - 1) / ATT_TILE;
@@ -97,9 +104,11 @@ __global__ __launch_bounds__(WC * 128) void tree_attn_kernel(TreeArgs a) {
   if (a.page_rows) { at.tbl = a.page_tbl + hidx * a.tbl_entries; at.shift = a.page_shift; at.init_rows = at.tbl[0] << a.page_shift; }
 
   const int c_own = group * COLS + wc * 32 + col, c = min(c_own, a.R - 1);       // (a column without a query: the last one's once more, not stored)
-  typename Tile::Query q[1];
-  Tile::load(q[0], reinterpret_cast<const T*>(a.q) + (hidx * a.R + c) * D, half);
+  typename Tile::Query q;
+  Tile::load(q, reinterpret_cast<const T*>(a.q) + (hidx * a.R + c) * D, half);
   const unsigned long long mask = a.tree[(hidx / a.H % a.B) * a.T + c % a.T];
+
+  Tile::await(q);
 
   const unsigned char* kn = reinterpret_cast<const unsigned char*>(a.k_new) + hidx * a.T * ROWB;
   const unsigned char* vn = reinterpret_cast<const unsigned char*>(a.v_new) + hidx * a.T * ROWB;
@@ -126,9 +135,7 @@ __global__ __launch_bounds__(WC * 128) void tree_attn_kernel(TreeArgs a) {
     for (int j = 0; j < LPT; ++j) {
       const int p = j * NT + tid, lr = p / LPR, piece = p % LPR;
       if (ATT_TILE * LPR % NT && lr >= ATT_TILE) break;
-      const int r = min(r_begin + t * ATT_TILE + lr, r_end - 1);
-      if (r >= len) continue;                                  // (a node's row is read when it is wanted)
-      const long long row = at(r);
+      const long long row = at(min(r_begin + t * ATT_TILE + lr, min(r_end, len) - 1));        // (a node's row is read when it is wanted)
       raw.k[j] = *reinterpret_cast<const uint4*>(a.k_c + row * CROWB + piece * 16);
       raw.v[j] = *reinterpret_cast<const uint4*>(a.v_c + row * CROWB + piece * 16);
       if constexpr (CACHE == CACHE_E2M1) {
@@ -180,34 +187,33 @@ __global__ __launch_bounds__(WC * 128) void tree_attn_kernel(TreeArgs a) {
     }
   };
 
-  AttnState<T, D, 1> st;
+  AttnState<D> st;
   bool careful = false;
   const auto compute = [&](int t) {
     const int k32 = r_begin + t * ATT_TILE + 32 * wk;
     if (k32 >= r_end) return;
     const unsigned char* kt = lds + (t & 1) * Tile::BYTES;
     const unsigned char* vt = lds + (2 + (t & 1)) * Tile::BYTES;
-    at_f32x16_t s[1];
     float p[16], more;
-    typename Tile::template Weights<PARTS> w[1];
-    Tile::template scores<1>(kt, 32 * wk, lane, q, s);
+    typename Tile::template Weights<PARTS> w;
+    at_f32x16_t s = Tile::scores(kt, 32 * wk, lane, q);
     const bool cut = k32 + 32 > min(len, r_end);
     const auto sees = [&](int key) { const int r = k32 + key; return r < r_end && (r < len || (mask >> (r - len) & 1)); };
     if (cut) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[0][i] = sees(key_of(i, half)) ? s[0][i] : -__builtin_inff();
+      for (int i = 0; i < 16; ++i) s[i] = sees(key_of(i, half)) ? s[i] : -__builtin_inff();
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], a.scale_log2, -st.ref[0]));
+    for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, -st.ref));
     more = sum16(p);
-    if (cut || __builtin_amdgcn_ballot_w64(!(st.sum[0] + more < ATT_FAR))) attn_look<T, D, 1>(st, 0, s[0], p, more, a.scale_log2);
-    st.sum[0] += more;
-    Tile::template pack<PARTS>(p, w[0]);
+    if (cut || __builtin_amdgcn_ballot_w64(!(st.sum + more < ATT_FAR))) attn_look<D>(st, s, p, more, a.scale_log2);
+    st.sum += more;
+    Tile::template pack<PARTS>(p, w);
     if (careful && (PARTS > 1 || cut)) {
 #pragma unroll 1
       for (int key = 0; key < 32; ++key) {                     // its weight is with one of the column's lanes, element i of its 16
         const int i = 4 * (key >> 3) + (key & 3), owner = col + 32 * ((key >> 2) & 1);
-        const float f = __shfl(Tile::template weight<PARTS>(w[0], i), owner, 64);
+        const float f = __shfl(Tile::template weight<PARTS>(w, i), owner, 64);
         if (!sees(key)) continue;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
@@ -215,11 +221,11 @@ __global__ __launch_bounds__(WC * 128) void tree_attn_kernel(TreeArgs a) {
           for (int g = 0; g < 4; ++g) {
             const at_f32x4_t y = Tile::value4(vt, 32 * wk + key, 32 * db + 8 * g + 4 * half);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) st.o[0][db][4 * g + e] = fmaf(f, y[e], st.o[0][db][4 * g + e]);
+            for (int e = 0; e < 4; ++e) st.o[db][4 * g + e] = fmaf(f, y[e], st.o[db][4 * g + e]);
           }
       }
     } else {
-      Tile::template add<PARTS, 1>(vt, 32 * wk, lane, w, st.o);
+      Tile::template add<PARTS>(vt, 32 * wk, lane, w, st.o);
     }
   };
   for (;;) {
@@ -246,111 +252,90 @@ __global__ __launch_bounds__(WC * 128) void tree_attn_kernel(TreeArgs a) {
 
   // ---- the two halves of a tile's keys: the second wave of a block leaves its results in LDS, [column][D + 4]
   float* s_o = reinterpret_cast<float*>(lds) + wc * 32 * (D + 4);
-  float sum = both_sum(st.sum[0]);
+  float sum = both_sum(st.sum);
   if (wk) {
-    if (half == 0) { s_ml[wc * 32 + col][0] = st.ref[0]; s_ml[wc * 32 + col][1] = sum; }
+    if (half == 0) { s_ml[wc * 32 + col][0] = st.ref; s_ml[wc * 32 + col][1] = sum; }
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<at_f32x4_t*>(s_o + col * (D + 4) + 32 * db + 8 * g + 4 * half) = at_f32x4_t{st.o[0][db][4 * g], st.o[0][db][4 * g + 1], st.o[0][db][4 * g + 2], st.o[0][db][4 * g + 3]};
+        *reinterpret_cast<at_f32x4_t*>(s_o + col * (D + 4) + 32 * db + 8 * g + 4 * half) = at_f32x4_t{st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]};
   }
   __syncthreads();
-  const long long record = hidx * a.groups + group;
-  const __amdgpu_buffer_rsrc_t rec = agent_buffer(a.part + record * a.slots * COLS * D, a.slots * COLS * D * 4);
-  const __amdgpu_buffer_rsrc_t rec_ml = agent_buffer(a.part_ml + record * a.slots * COLS * 2, a.slots * COLS * 8);
   if (!wk) {
-    const float ref2 = s_ml[wc * 32 + col][0], sum2 = s_ml[wc * 32 + col][1];
-    const float m = fmaxf(st.ref[0], ref2);
-    // (a half that has seen nothing: reference -inf, weight 0)
-    const float f1 = st.ref[0] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(st.ref[0] - m), f2 = ref2 == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ref2 - m);
-    sum = sum * f1 + sum2 * f2;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const at_f32x4_t y = *reinterpret_cast<const at_f32x4_t*>(s_o + col * (D + 4) + 32 * db + 8 * g + 4 * half);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) st.o[0][db][4 * g + e] = st.o[0][db][4 * g + e] * f1 + y[e] * f2;
-      }
+    merge_halves<D>(st, sum, s_ml[wc * 32 + col], s_o + col * (D + 4), half);
     if (pieces == 1) {
-      store_column<OT, D>(reinterpret_cast<OT*>(a.out) + (hidx * a.R + c) * D, c == c_own, half, st.o[0], 1.f / sum);
-    } else {
-      const int cc = wc * 32 + col;
+      store_column<OT, D>(reinterpret_cast<OT*>(a.out) + (hidx * a.R + c) * D, c == c_own, half, st.o, 1.f / sum);
+    } else if (c == c_own) {
+      const long long record = (hidx * a.slots + chunk) * a.R + c;
+      float* to = a.part + record * D;
 #pragma unroll
       for (int db = 0; db < D / 32; ++db)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(du32x4_t, at_f32x4_t{st.o[0][db][4 * g], st.o[0][db][4 * g + 1], st.o[0][db][4 * g + 2], st.o[0][db][4 * g + 3]}), rec,
-                                                 (cc * D + 32 * db + 8 * g + 4 * half) * 4, chunk * (COLS * D * 4), AGENT);
-      if (half == 0) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(du32x2_t, make_float2(m, sum)), rec_ml, cc * 8, chunk * (COLS * 8), AGENT);
+          *reinterpret_cast<at_f32x4_t*>(to + 32 * db + 8 * g + 4 * half) = at_f32x4_t{st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]};
+      if (half == 0) *reinterpret_cast<float2*>(a.part_ml + record * 2) = make_float2(st.ref, sum);
     }
   }
-  if (pieces == 1) return;
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // the wave's stores are where everybody sees them
-  __syncthreads();
-  if (tid == 0) {
-    uint32_t* count = a.count + (hidx * a.G + group) * MEET_COUNT_STRIDE;
-    const uint32_t arrived = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    s_last = arrived + 1u == (uint32_t)pieces;
-    if (s_last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  __syncthreads();
-  if (!s_last) return;
-  // ---- the last one: four dims of a column per thread
+}
+
+// The pieces of a head joined, in their order: four dims of a column per thread.
+template <typename OT, int D>
+__global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int n_columns) {
   constexpr int TL = D / 4, MB = 8;
-  const int t4 = tid % TL;
-  for (int cc = tid / TL; cc < min(COLS, a.R - group * COLS); cc += NT / TL) {
-    float m = -__builtin_inff(), l = 0.f;
-    at_f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    for (int c0 = 0; c0 < pieces; c0 += MB) {
-      at_f32x4_t y[MB]; float2 ml[MB];
+  const int x = (int)blockIdx.x * (256 / TL) + (int)threadIdx.x / TL, t4 = threadIdx.x % TL;
+  if (x >= n_columns) return;
+  const long long hidx = x / a.R;
+  const int c = x % a.R;
+  const int len = a.kv_len[hidx], pieces = pieces_of_tree(a, len);
+  if (pieces == 1) return;                                     // (its output is there)
+  float m = -__builtin_inff(), l = 0.f;
+  at_f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+  for (int c0 = 0; c0 < pieces; c0 += MB) {
+    at_f32x4_t y[MB]; float2 ml[MB];
 #pragma unroll
-      for (int j = 0; j < MB; ++j) {
-        const bool there = c0 + j < pieces;
-        ml[j] = __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(rec_ml, there ? (c0 + j) * (COLS * 8) + cc * 8 : NOWHERE, 0, AGENT));
-        y[j] = __builtin_bit_cast(at_f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rec, there ? (c0 + j) * (COLS * D * 4) + (cc * D + 4 * t4) * 4 : NOWHERE, 0, AGENT));
-      }
-      float bm = m;
+    for (int j = 0; j < MB; ++j) {
+      const long long record = (hidx * a.slots + min(c0 + j, pieces - 1)) * a.R + c;
+      ml[j] = *reinterpret_cast<const float2*>(a.part_ml + record * 2);
+      y[j] = *reinterpret_cast<const at_f32x4_t*>(a.part + record * D + 4 * t4);
+    }
 #pragma unroll
-      for (int j = 0; j < MB; ++j) {
-        if (c0 + j >= pieces) ml[j].x = -__builtin_inff();
-        bm = fmaxf(bm, ml[j].x);
-      }
-      const float f = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - bm);
-      l *= f;
+    for (int j = 0; j < MB; ++j) {
+      if (c0 + j >= pieces) break;
+      const float bm = fmaxf(m, ml[j].x);
+      // (a piece that has seen nothing: reference -inf, sum 0)
+      const float f = m == -__builtin_inff() ? (l == 0.f ? 0.f : l) : __builtin_amdgcn_exp2f(m - bm);
+      const float g = ml[j].x == -__builtin_inff() && ml[j].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[j].x - bm);
+      l = l * f + ml[j].y * g;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] *= f;
-#pragma unroll
-      for (int j = 0; j < MB; ++j) {
-        const float g = ml[j].x == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(ml[j].x - bm);
-        l = fmaf(ml[j].y, g, l);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = fmaf(y[j][e], g, o[e]);
-      }
+      for (int e = 0; e < 4; ++e) o[e] = o[e] * f + y[j][e] * g;
       m = bm;
     }
-    OT* to = reinterpret_cast<OT*>(a.out) + (hidx * a.R + group * COLS + cc) * D + 4 * t4;
-    const float inv = 1.f / l;
-    if constexpr (sizeof(OT) == 4) {
-      *reinterpret_cast<at_f32x4_t*>(to) = at_f32x4_t{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-    } else {
-      *reinterpret_cast<uint2*>(to) = make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector((at_f32x2_t{o[0] * inv, o[1] * inv}), at_bf16x2_t)),
-                                                 __builtin_bit_cast(uint32_t, __builtin_convertvector((at_f32x2_t{o[2] * inv, o[3] * inv}), at_bf16x2_t)));
-    }
+  }
+  OT* to = reinterpret_cast<OT*>(a.out) + (long long)x * D + 4 * t4;
+  const float inv = 1.f / l;
+  if constexpr (sizeof(OT) == 4) {
+    *reinterpret_cast<at_f32x4_t*>(to) = at_f32x4_t{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  } else {
+    *reinterpret_cast<uint2*>(to) = make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector((at_f32x2_t{o[0] * inv, o[1] * inv}), at_bf16x2_t)),
+                                               __builtin_bit_cast(uint32_t, __builtin_convertvector((at_f32x2_t{o[2] * inv, o[3] * inv}), at_bf16x2_t)));
   }
 }
 
 // Blocks of columns of a workgroup, workgroups of a head side by side, rows per piece, most pieces, pieces of the grid.
 struct TreePlan { int wc, groups, chunk_rows, max_chunks, slots; };
+#ifndef TW
+#define TW 512
+#define TMIN 128
+#endif
 static TreePlan tree_plan(const Dims& dm, const madakv_config& c, int T, int longest_rows) {
   TreePlan p;
   const int R = dm.G * T;
   p.wc = R <= 32 ? 1 : R <= 64 ? 2 : 4;
-  p.groups = (R + 32 * p.wc - 1) / (32 * p.wc);                // (at most G, which is how many counters a head has: T <= 32 wc)
+  p.groups = (R + 32 * p.wc - 1) / (32 * p.wc);
   const long long typical = std::min(c.budget, c.ctx_len) + (long long)T;
-  const long long want = std::max<long long>(1, 512 / ((long long)dm.heads * p.groups));
-  p.chunk_rows = (int)std::max<long long>(128, (typical / want + ATT_TILE - 1) / ATT_TILE * ATT_TILE);
+  const long long want = std::max<long long>(1, TW / ((long long)dm.heads * p.groups));
+  p.chunk_rows = (int)std::max<long long>(TMIN, (typical / want + ATT_TILE - 1) / ATT_TILE * ATT_TILE);
   p.max_chunks = (int)((std::max(2, c.hcc_rho) * typical + p.chunk_rows - 1) / p.chunk_rows);
   const int longest = std::max(1, std::min(longest_rows, c.ctx_len + c.max_new_tokens)) + T;
   p.slots = std::min(p.max_chunks, (longest + p.chunk_rows - 1) / p.chunk_rows);
@@ -358,7 +343,7 @@ static TreePlan tree_plan(const Dims& dm, const madakv_config& c, int T, int lon
 }
 size_t tree_ws_bytes(const Dims& dm, const madakv_config& c, int T, int longest_rows) {
   const TreePlan p = tree_plan(dm, c, T, longest_rows);
-  return p.slots == 1 ? 16 : (size_t)dm.heads * p.groups * p.slots * p.wc * 32 * (dm.d + 2) * sizeof(float);
+  return p.slots == 1 ? 16 : (size_t)dm.heads * p.slots * dm.G * T * (dm.d + 2) * sizeof(float);
 }
 
 template <typename T, typename OT, int CACHE, int D>
@@ -367,6 +352,10 @@ static hipError_t launch_tree(const Dims& dm, const TreeArgs& a, const TreePlan&
   if (p.wc == 1) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 1>), grid, dim3(128), 0, st, a);
   else if (p.wc == 2) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 2>), grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 4>), grid, dim3(512), 0, st, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.slots == 1) return e;
+  const int n = dm.heads * a.R, per = 256 / (D / 4);
+  hipLaunchKernelGGL((tree_join_kernel<OT, D>), dim3((n + per - 1) / per), dim3(256), 0, st, a, n);
   return hipGetLastError();
 }
 template <typename T, typename OT, int CACHE>
@@ -378,7 +367,7 @@ static hipError_t launch_tree_o(const Dims& dm, const madakv_config& c, const Tr
   return c.out_fp32 ? launch_tree_d<uint16_t, float, CACHE>(dm, a, p, st) : launch_tree_d<uint16_t, uint16_t, CACHE>(dm, a, p, st);
 }
 hipError_t launch_tree_attn(const Dims& dm, const madakv_config& c, int T, const void* q, const void* k_new, const void* v_new, const void* tree, const void* k_c,
-                            const void* v_c, const int64_t* kv_off, const int32_t* kv_len, void* out, const Meet& meet, void* ws, long long capacity_tokens, int longest_rows,
+                            const void* v_c, const int64_t* kv_off, const int32_t* kv_len, void* out, void* ws, long long capacity_tokens, int longest_rows,
                             const Paging& pg, int layer0, hipStream_t st) {
   const TreePlan p = tree_plan(dm, c, T, longest_rows);
   const long long head0 = (long long)layer0 * dm.B * dm.H;
@@ -387,8 +376,7 @@ hipError_t launch_tree_attn(const Dims& dm, const madakv_config& c, int T, const
   a.tree = static_cast<const unsigned long long*>(tree); a.kv_off = kv_off; a.kv_len = kv_len; a.out = out;
   a.B = dm.B; a.H = dm.H; a.G = dm.G; a.T = T; a.R = dm.G * T; a.groups = p.groups;
   a.chunk_rows = p.chunk_rows; a.max_chunks = std::min(p.max_chunks, p.slots); a.slots = p.slots;
-  a.part = static_cast<float*>(ws); a.part_ml = a.part + (size_t)dm.heads * p.groups * p.slots * p.wc * 32 * dm.d;
-  a.count = meet.count + head0 * dm.G * MEET_COUNT_STRIDE;
+  a.part = static_cast<float*>(ws); a.part_ml = a.part + (size_t)dm.heads * p.slots * a.R * dm.d;
   a.capacity = capacity_tokens;
   a.page_rows = pg.page_rows; a.tbl_entries = pg.entries; a.page_shift = 0;
   while (pg.page_rows && (1 << a.page_shift) < pg.page_rows) ++a.page_shift;
