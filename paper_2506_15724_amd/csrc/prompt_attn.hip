@@ -11,6 +11,7 @@
 
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 namespace madakv {
 
@@ -125,17 +126,13 @@ __global__ __launch_bounds__(PA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(W
     const int v = t + 1 - WK;
     if (v >= 0 && v < ntiles) issue(vb, voff, 2 + (v & 1), v);
   };
-  send(-1);
-
   typename Tile::Query q;
   Tile::load(q, reinterpret_cast<const T*>(a.q) + ((long long)qh * a.L + row) * D, half);
-  Tile::await(q);
 
   AttnState<D> st;
   using Weights = typename Tile::template Weights<PARTS>;
   Weights w, w_next;                                 // of the subtile before the one that s has the logits of
   at_f32x16_t s, s_next;
-  bool careful = false;
   const auto cut = [&](int j) {                      // some row does not see all of the subtile
     const int k32 = first_key(j);
     return k32 + 31 > wfirst || k32 < max_start;
@@ -151,8 +148,10 @@ __global__ __launch_bounds__(PA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(W
     st.sum = t;
     return true;
   };
-  for (;;) {
+  const auto pass = [&](auto careful) {
     st.clear();
+    send(-1);
+    if (!decltype(careful)::value) Tile::await(q);
     // Step j: the logits of subtile j + 1, the weights of subtile j, and what subtile j - 1 adds to the output.  None of them needs another
     // one's results: the matrix instructions of the first and the last run beside the vector instructions of the second.
     // Phase t has steps 2 t - 1 and 2 t, or with WK = 2 step t - 1.
@@ -165,7 +164,7 @@ __global__ __launch_bounds__(PA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(W
     const auto v_tile = [&](int t) { return lds + (2 + ((t - WK) & 1)) * Tile::BYTES; };
     // phases t0 .. t1 - 1: every row sees all keys of their steps
     const int ja = max(j0 + 1, number((max_start + 31) / 32)), jb = min(j1 - 1, number((wfirst + 1) / 32));          // steps [ja, jb)
-    const int t0 = careful ? INT_MAX : WK == 2 ? ja + 1 : (ja + 2) >> 1, t1 = WK == 2 ? jb + 1 : (jb + 1) >> 1;
+    const int t0 = decltype(careful)::value ? INT_MAX : WK == 2 ? ja + 1 : (ja + 2) >> 1, t1 = WK == 2 ? jb + 1 : (jb + 1) >> 1;
     const int phases = ntiles + WK;
     int t = 0;
 #pragma unroll 1
@@ -173,7 +172,7 @@ __global__ __launch_bounds__(PA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(W
       begin(t);
       bool formed = false;                           // the step's logits and sums are there
       int j = WK == 2 ? t - 1 : 2 * t - 1;
-      if (t >= t0 && t < t1) {
+      if (!decltype(careful)::value && t >= t0 && t < t1) {
 #pragma unroll 1
         for (;;) {
           const unsigned char* kt = k_tile(t);
@@ -209,7 +208,7 @@ __global__ __launch_bounds__(PA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(W
         if (!formed) {
           if (j + 1 >= j0 && j + 1 < j1) s_next = Tile::scores(kt, row_in_tile(j + 1), lane, q);
           if (j - 1 >= j0 && j - 1 < j1) {
-            if (careful && (PARTS > 1 || cut(j - 1))) {
+            if (decltype(careful)::value && (PARTS > 1 || cut(j - 1))) {
 #pragma unroll 1
               for (int key = 0; key < 32; ++key) {   // its weight is with one of the column's lanes, element i of its 16
                 const int i = 4 * (key >> 3) + (key & 3), owner = col + 32 * ((key >> 2) & 1), k = first_key(j - 1) + key;
@@ -248,11 +247,12 @@ __global__ __launch_bounds__(PA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(W
       }
       ++t;
     }
-    // outputs that are no numbers: the formula's, or those of rows of V that nobody may see
-    const int again = __syncthreads_or(!careful && any && not_finite(st));
-    if (!again) break;
-    careful = true;
-    send(-1);
+  };
+  pass(std::false_type{});
+  // outputs that are no numbers: the formula's, or those of rows of V that nobody may see
+  if (__builtin_expect(__syncthreads_or(any && not_finite(st)), 0)) {
+    pass(std::true_type{});
+    __syncthreads();
   }
   float sum = both_sum(st.sum);
   if constexpr (WK == 2) {                           // the second half's results go through LDS

@@ -11,6 +11,7 @@
 #include "decode_pieces.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace madakv {
 
@@ -28,15 +29,21 @@ struct TreeArgs {
   float scale_log2;
 };
 
-// Rows per piece of a head of so many (rows and nodes), and how many pieces that makes.
-__device__ __forceinline__ int piece_rows(const TreeArgs& a, int total) {
-  if (total <= a.chunk_rows * a.max_chunks) return a.chunk_rows;
-  return ((total + a.max_chunks - 1) / a.max_chunks + ATT_TILE - 1) / ATT_TILE * ATT_TILE;
+// Rows per piece of a head of so many, and how many pieces that makes; the nodes are with the last one.
+__device__ __forceinline__ int piece_rows(const TreeArgs& a, int len) {
+  if (len <= a.chunk_rows * a.max_chunks) return a.chunk_rows;
+  return ((len + a.max_chunks - 1) / a.max_chunks + ATT_TILE - 1) / ATT_TILE * ATT_TILE;
 }
 __device__ __forceinline__ int pieces_of_tree(const TreeArgs& a, int len) {
-  if (len <= 0) return 1;
-  const int rows = piece_rows(a, len + a.T);
-  return (len + a.T + rows - 1) / rows;
+  const int rows = piece_rows(a, len);
+  return max(1, (len + rows - 1) / rows);
+}
+
+// four neighbouring elements of the output
+__device__ __forceinline__ void store4(float* to, const at_f32x4_t& o, float inv) { *reinterpret_cast<at_f32x4_t*>(to) = at_f32x4_t{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv}; }
+__device__ __forceinline__ void store4(uint16_t* to, const at_f32x4_t& o, float inv) {
+  *reinterpret_cast<uint2*>(to) = make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector((at_f32x2_t{o[0] * inv, o[1] * inv}), at_bf16x2_t)),
+                                             __builtin_bit_cast(uint32_t, __builtin_convertvector((at_f32x2_t{o[2] * inv, o[3] * inv}), at_bf16x2_t)));
 }
 
 // 32 elements of a node's row as the 4-bit cache would have them: in place
@@ -65,11 +72,18 @@ __device__ __forceinline__ void as_mx4(uint4 (&x)[4]) {
 }
 // four E4M3 bytes -> four bf16 (exact)
 __device__ __forceinline__ uint2 from_e4m3(uint32_t w) {
-  const df32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-  return make_uint2((__float_as_uint(a[0]) >> 16) | (__float_as_uint(a[1]) & 0xffff0000u), (__float_as_uint(b[0]) >> 16) | (__float_as_uint(b[1]) & 0xffff0000u));
+  return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true)));
 }
-__device__ __forceinline__ uint32_t e4m3_of(uint32_t a, uint32_t b) {          // two bf16 pairs
-  return f32_to_e4m3(bf16_lo(a)) | f32_to_e4m3(bf16_hi(a)) << 8 | f32_to_e4m3(bf16_lo(b)) << 16 | f32_to_e4m3(bf16_hi(b)) << 24;
+// two bf16 pairs -> four E4M3 bytes, as f32_to_e4m3 (checked on every bf16): the instruction rounds to nearest even, magnitudes above 448 and NaN are made 448 first
+__device__ __forceinline__ uint32_t e4m3_of(uint32_t a, uint32_t b) {
+  const auto clamped = [](uint32_t x) {
+    return __builtin_bit_cast(mx_bf16x2_t, __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(mx_u16x2_t, x & 0x7fff7fffu), mx_u16x2_t{0x43e0, 0x43e0})) | (x & 0x80008000u));
+  };
+  typedef __attribute__((ext_vector_type(2))) short i16x2_t;
+  i16x2_t code = {0, 0};
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(code, clamped(a), 1.f, false);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(code, clamped(b), 1.f, true);
+  return __builtin_bit_cast(uint32_t, code);
 }
 
 // T: Q, nodes' rows; CACHE: 0 rows of T, CACHE_E4M3, CACHE_E2M1; WC blocks of 32 columns
@@ -95,9 +109,9 @@ __global__ __launch_bounds__(WC * 128) __attribute__((amdgpu_waves_per_eu(sizeof
   const int len = a.kv_len[hidx];
   const long long off = a.kv_off[hidx];
   const int total = len > 0 ? len + a.T : 0;                   // (an empty segment: its budgets did not fit the cache)
-  const int rows = piece_rows(a, total), pieces = pieces_of_tree(a, len);
+  const int rows = piece_rows(a, len), pieces = pieces_of_tree(a, len);
   if (chunk >= pieces) return;
-  const int r_begin = chunk * rows, r_end = min(total, r_begin + rows);
+  const int r_begin = chunk * rows, r_end = chunk == pieces - 1 ? total : r_begin + rows;
   const int ntiles = (r_end - r_begin + ATT_TILE - 1) / ATT_TILE;
   RowMap at;
   at.off = off; at.init_rows = 0x7fffffff; at.tbl = nullptr; at.shift = 0; at.fresh_slot = -1; at.fresh_page = 0;
@@ -123,7 +137,7 @@ __global__ __launch_bounds__(WC * 128) __attribute__((amdgpu_waves_per_eu(sizeof
       const long long row = node ? r - len : at(r);
       const unsigned char* kp = (node ? kn : a.k_c) + row * ROWB + Tile::k_slot(lr, s) * 16;
       const unsigned char* vp = (node ? vn : a.v_c) + row * ROWB + Tile::v_slot(lr, s) * 16;
-      const uint32_t to = lds0 + (uint32_t)((t & 1) * Tile::BYTES + (wave * LPT + j) * 1024);
+      const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds0 + (uint32_t)((t & 1) * Tile::BYTES + (wave * LPT + j) * 1024)));
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(kp));
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + 2 * Tile::BYTES), "v"(vp));
     }
@@ -188,8 +202,7 @@ __global__ __launch_bounds__(WC * 128) __attribute__((amdgpu_waves_per_eu(sizeof
   };
 
   AttnState<D> st;
-  bool careful = false;
-  const auto compute = [&](int t) {
+  const auto compute = [&](auto careful, int t) {
     const int k32 = r_begin + t * ATT_TILE + 32 * wk;
     if (k32 >= r_end) return;
     const unsigned char* kt = lds + (t & 1) * Tile::BYTES;
@@ -199,17 +212,23 @@ __global__ __launch_bounds__(WC * 128) __attribute__((amdgpu_waves_per_eu(sizeof
     at_f32x16_t s = Tile::scores(kt, 32 * wk, lane, q);
     const bool cut = k32 + 32 > min(len, r_end);
     const auto sees = [&](int key) { const int r = k32 + key; return r < r_end && (r < len || (mask >> (r - len) & 1)); };
-    if (cut) {
+    bool look = cut;
+    if (!cut) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = sees(key_of(i, half)) ? s[i] : -__builtin_inff();
+      for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, -st.ref));
+      more = sum16(p);
+      look = __builtin_amdgcn_ballot_w64(!(st.sum + more < ATT_FAR)) != 0;
     }
+    if (__builtin_expect(look, 0)) {
+      if (cut) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, -st.ref));
-    more = sum16(p);
-    if (cut || __builtin_amdgcn_ballot_w64(!(st.sum + more < ATT_FAR))) attn_look<D>(st, s, p, more, a.scale_log2);
+        for (int i = 0; i < 16; ++i) s[i] = sees(key_of(i, half)) ? s[i] : -__builtin_inff();
+      }
+      attn_look<D>(st, s, p, more, a.scale_log2);
+    }
     st.sum += more;
     Tile::template pack<PARTS>(p, w);
-    if (careful && (PARTS > 1 || cut)) {
+    if (decltype(careful)::value && (PARTS > 1 || cut)) {
 #pragma unroll 1
       for (int key = 0; key < 32; ++key) {                     // its weight is with one of the column's lanes, element i of its 16
         const int i = 4 * (key >> 3) + (key & 3), owner = col + 32 * ((key >> 2) & 1);
@@ -228,7 +247,7 @@ __global__ __launch_bounds__(WC * 128) __attribute__((amdgpu_waves_per_eu(sizeof
       Tile::template add<PARTS>(vt, 32 * wk, lane, w, st.o);
     }
   };
-  for (;;) {
+  const auto pass = [&](auto careful) {
     st.clear();
     if (ntiles > 0) {
       if constexpr (CACHE) { fetch(0); park(0); }
@@ -242,12 +261,14 @@ __global__ __launch_bounds__(WC * 128) __attribute__((amdgpu_waves_per_eu(sizeof
         if constexpr (CACHE) fetch(t + 1);
         else load_direct(t + 1);
       }
-      compute(t);
+      compute(careful, t);
       if constexpr (CACHE) { if (t + 1 < ntiles) park(t + 1); }
     }
-    const int again = __syncthreads_or(!careful && not_finite(st));
-    if (!again) break;
-    careful = true;
+  };
+  pass(std::false_type{});
+  if (__builtin_expect(__syncthreads_or(not_finite(st)), 0)) {
+    pass(std::true_type{});
+    __syncthreads();
   }
 
   // ---- the two halves of a tile's keys: the second wave of a block leaves its results in LDS, [column][D + 4]
@@ -275,6 +296,300 @@ __global__ __launch_bounds__(WC * 128) __attribute__((amdgpu_waves_per_eu(sizeof
         for (int g = 0; g < 4; ++g)
           *reinterpret_cast<at_f32x4_t*>(to + 32 * db + 8 * g + 4 * half) = at_f32x4_t{st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]};
       if (half == 0) *reinterpret_cast<float2*>(a.part_ml + record * 2) = make_float2(st.ref, sum);
+    }
+  }
+}
+
+// ---- up to 32 columns ------------------------------------------------------------------------------------
+// Hardly more arithmetic per byte than decode: what counts is how much is on its way.  Every wave works for itself on tiles of 32 rows, without barriers:
+// rows of 16 bits come straight into LDS tiles of the wave's own, those of 8 and 4 bits as operand A of K (a lane has one row's dims of 16 bytes at a time, and Q the
+// same order of dims) and through registers into an LDS tile of V.  The next tile's are sent for as soon as there is room for them: eight waves on a
+// compute unit have up to 128 KB of 16-bit rows on their way.
+template <typename OT, int CACHE, int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_narrow_kernel(TreeArgs a) {
+  using Tile = AttnTile<uint16_t, D>;
+  constexpr int NW = 4, PARTS = sizeof(OT) == 4 ? 3 : 1, ROWB = Tile::ROWB, RS = D + 4;
+  constexpr int EPL = CACHE == CACHE_E2M1 ? 32 : CACHE == CACHE_E4M3 ? 16 : 8;         // elements of a 16-byte load
+  constexpr int LPR = D / EPL, CROWB = LPR * 16;                                        // loads of a row, its bytes
+  constexpr int KL = LPR / 2 ? LPR / 2 : 1, VL = LPR / 2 ? LPR / 2 : 1;                 // loads of a lane per tile: K, V
+  static_assert(LPR >= 2, "both lanes of a row have something of it");
+  constexpr int TILEB = 32 * ROWB, WAVEB = CACHE ? TILEB : 2 * TILEB, RESB = 32 * RS * 4;          // a wave's tiles (V, K), later its results
+  constexpr int EACH = WAVEB > RESB ? WAVEB : RESB;
+  __shared__ __attribute__((aligned(1024))) unsigned char s_tiles[NW * EACH];
+  __shared__ float s_ml[NW][32][2];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, col = lane & 31;
+  const int xy = (int)(blockIdx.x + blockIdx.y), x = xy < (int)gridDim.x ? xy : xy % (int)gridDim.x, chunk = blockIdx.y;       // (the pieces of a head on different XCDs)
+  const int len = a.kv_len[x];
+  const long long off = a.kv_off[x];
+  const int rows = piece_rows(a, len), pieces = pieces_of_tree(a, len);
+  if (chunk >= pieces) return;
+  const int r_begin = chunk * rows, n_rows = max(0, min(len - r_begin, rows));          // (an empty segment sees nothing: its sums stay zero)
+  const int row_tiles = (n_rows + 31) / 32, node_tiles = chunk == pieces - 1 && len > 0 ? (a.T + 31) / 32 : 0;
+  RowMap at;
+  at.off = off; at.init_rows = 0x7fffffff; at.tbl = nullptr; at.shift = 0; at.fresh_slot = -1; at.fresh_page = 0;
+  if (a.page_rows) { at.tbl = a.page_tbl + (long long)x * a.tbl_entries; at.shift = a.page_shift; at.init_rows = at.tbl[0] << a.page_shift; }
+  const int c = min(col, a.R - 1);                             // (a column without a query: the last one's once more, not stored)
+  // the query: for step i EPL / 8 + e dims [(2 i + half) EPL + 8 e, + 8)
+  typename Tile::Query q;
+  const auto dim_of = [&](int ks) { return (2 * (ks / (EPL / 8)) + half) * EPL + 8 * (ks % (EPL / 8)); };
+  {
+    const uint16_t* qr = reinterpret_cast<const uint16_t*>(a.q) + ((long long)x * a.R + c) * D;
+    if constexpr (CACHE == 0) {
+      Tile::load(q, qr, half);
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < Tile::KS; ++ks) q.x[ks] = *reinterpret_cast<const at_bf16x8_t*>(qr + dim_of(ks));
+    }
+  }
+  const unsigned long long mask = a.tree[(long long)(x / a.H % a.B) * a.T + c % a.T];
+
+  unsigned char* vt = s_tiles + wave * EACH;
+  unsigned char* kt = vt + TILEB;                              // (16-bit rows)
+  // Where the rows of a tile are, r0 its first one in the piece: two stretches of 16, each within a page, that need not follow each other.
+  struct Place { long long lo, hi; };
+  const auto place = [&](int r0) {
+    const int r = r_begin + r0;
+    if (!a.page_rows) return Place{off + r, off + r + 16};
+    return Place{at(r), r0 + 16 < n_rows ? at(r + 16) : 0};
+  };
+  // 8-bit and 4-bit rows: 16 bytes of row lr (past the end: the last one once more, masked where it is used) at byte `byte`
+  struct Raw { uint4 k[KL], v[VL]; uint32_t ks[KL], vs[VL]; } raw;
+  const auto row_of = [&](const Place& at, int r0, int lr) { lr = min(lr, n_rows - 1 - r0); return (lr < 16 ? at.lo : at.hi) + (lr & 15); };
+  const auto load_k = [&](const Place& at, int r0) {
+    const long long row = row_of(at, r0, col);
+    const unsigned char* p = a.k_c + row * CROWB + half * 16;
+#pragma unroll
+    for (int i = 0; i < KL; ++i) {
+      raw.k[i] = *reinterpret_cast<const uint4*>(p + 32 * i);
+      if constexpr (CACHE == CACHE_E2M1) raw.ks[i] = a.k_c[a.capacity * CROWB + row * (D / MX_BLOCK) + 2 * i + half];
+    }
+  };
+  const auto load_v = [&](const Place& at, int r0) {
+#pragma unroll
+    for (int j = 0; j < VL; ++j) {
+      const int p = j * 64 + lane;
+      const long long row = row_of(at, r0, p / LPR);
+      raw.v[j] = *reinterpret_cast<const uint4*>(a.v_c + row * CROWB + p % LPR * 16);
+      if constexpr (CACHE == CACHE_E2M1) raw.vs[j] = a.v_c[a.capacity * CROWB + row * (D / MX_BLOCK) + p % LPR];
+    }
+  };
+  // 16-bit rows: a load takes 1 KB, whole rows of one of the two stretches
+  constexpr int GROUP = 1024 / ROWB, LOADS = 32 / GROUP;
+  const uint32_t lds_v = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)vt;
+  const auto send = [&](bool v, const Place& at, int r0) {
+    const unsigned char* cache = v ? a.v_c : a.k_c;
+    const unsigned char* from[2] = {cache + at.lo * ROWB, cache + at.hi * ROWB};
+    const int valid = n_rows - r0;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      int lr = j * GROUP + lane / Tile::PPR;
+      const int s = (v ? Tile::v_slot(lr, lane % Tile::PPR) : Tile::k_slot(lr, lane % Tile::PPR)) * 16;
+      uint64_t p = reinterpret_cast<uint64_t>(from[2 * j / LOADS]);
+      if (valid < 32) {                                        // (uniform)
+        lr = min(lr, valid - 1);
+        if (valid <= 16) p = reinterpret_cast<uint64_t>(from[0]);
+        else if (2 * j >= LOADS) lr = max(lr, 16);
+      }
+      const uint64_t same = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane((int)(lds_v + (v ? 0u : (uint32_t)TILEB) + j * 1024u))), "v"((lr & 15) * ROWB + s), "s"(same));
+    }
+  };
+  // 16 bytes of a cache row -> EPL bf16
+  const auto unpack = [&](const uint4& z, uint32_t scale, uint4 (&y)[EPL / 8]) {
+    if constexpr (CACHE == CACHE_E2M1) {
+      y[0] = mx_decode8(z.x, scale); y[1] = mx_decode8(z.y, scale); y[2] = mx_decode8(z.z, scale); y[3] = mx_decode8(z.w, scale);
+    } else if constexpr (CACHE == CACHE_E4M3) {
+      const uint2 e0 = from_e4m3(z.x), e1 = from_e4m3(z.y), e2 = from_e4m3(z.z), e3 = from_e4m3(z.w);
+      y[0] = make_uint4(e0.x, e0.y, e1.x, e1.y); y[1] = make_uint4(e2.x, e2.y, e3.x, e3.y);
+    } else {
+      y[0] = z;
+    }
+  };
+  // EPL elements of a node's row, with the values that the cache would give them
+  const auto node_part = [&](const void* nodes, int node, int piece, uint4 (&y)[EPL / 8]) {
+    const uint4* from = reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(nodes) + ((long long)x * a.T + min(node, a.T - 1)) * D + piece * EPL);
+#pragma unroll
+    for (int i = 0; i < EPL / 8; ++i) y[i] = from[i];
+    if constexpr (CACHE == CACHE_E2M1) {
+      as_mx4(y);
+    } else if constexpr (CACHE == CACHE_E4M3) {
+#pragma unroll
+      for (int i = 0; i < EPL / 8; ++i) {
+        const uint2 lo = from_e4m3(e4m3_of(y[i].x, y[i].y)), hi = from_e4m3(e4m3_of(y[i].z, y[i].w));
+        y[i] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+      }
+    }
+  };
+  const auto park = [&](int j, const uint4 (&y)[EPL / 8]) {    // piece j of the lane's V
+    const int p = j * 64 + lane, lr = p / LPR;
+#pragma unroll
+    for (int i = 0; i < EPL / 8; ++i) *reinterpret_cast<uint4*>(vt + lr * ROWB + Tile::v_slot(lr, p % LPR * (EPL / 8) + i) * 16) = y[i];
+  };
+  AttnState<D> st;
+  // (the tile that its lanes have written, read with another lane mapping: same wave, in order)
+  const auto settle = [] {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+  const auto weigh = [&](at_f32x16_t& s, bool cut, uint32_t keys, typename Tile::template Weights<PARTS>& w) {
+    float p[16], more;
+    bool look = cut;
+    if (!cut) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, -st.ref));
+      more = sum16(p);
+      look = __builtin_amdgcn_ballot_w64(!(st.sum + more < ATT_FAR)) != 0;
+    }
+    if (__builtin_expect(look, 0)) {
+      const uint32_t mine = keys >> (4 * half);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = mine >> key_of(i, 0) & 1 ? s[i] : -__builtin_inff();
+      attn_look<D>(st, s, p, more, a.scale_log2);
+    }
+    st.sum += more;
+    Tile::template pack<PARTS>(p, w);
+  };
+  const auto add = [&](auto careful, bool cut, uint32_t keys, const typename Tile::template Weights<PARTS>& w) {
+    settle();
+    if (decltype(careful)::value && (PARTS > 1 || cut)) {
+#pragma unroll 1
+      for (int key = 0; key < 32; ++key) {                     // its weight is with one of the column's lanes, element i of its 16
+        const int i = 4 * (key >> 3) + (key & 3), owner = col + 32 * ((key >> 2) & 1);
+        const float f = __shfl(Tile::template weight<PARTS>(w, i), owner, 64);
+        if (!(keys >> key & 1)) continue;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const at_f32x4_t y = Tile::value4(vt, key, 32 * db + 8 * g + 4 * half);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) st.o[db][4 * g + e] = fmaf(f, y[e], st.o[db][4 * g + e]);
+          }
+      }
+    } else {
+      Tile::template add<PARTS>(vt, 0, lane, w, st.o);
+    }
+    settle();
+  };
+  // once more, carefully, where outputs are no numbers: the formula's, or those of rows of V that nobody may see (see prompt_attn.hip)
+  const auto pass = [&](auto careful) {
+    st.clear();
+    int r0 = wave * 32;
+    const int last = (row_tiles - 1) * 32;                     // (past the end: the last tile, which nobody looks at; it keeps the count of loads in flight)
+    if (r0 < n_rows) {
+      const Place here = place(r0);
+      if constexpr (CACHE == 0) { send(false, here, r0); send(true, here, r0); }
+      else { load_k(here, r0); load_v(here, r0); }
+    }
+    Tile::await(q);
+#pragma unroll 1
+    for (; r0 < n_rows; r0 += NW * 32) {
+      const int next = min(r0 + NW * 32, last);
+      const Place there = place(next);
+      const bool cut = r0 + 32 > n_rows;
+      const uint32_t keys = cut ? (1u << (n_rows - r0)) - 1u : ~0u;
+      typename Tile::template Weights<PARTS> w;
+      at_f32x16_t s;
+      if constexpr (CACHE == 0) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");       // K is there
+        s = Tile::scores(kt, 0, lane, q);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        send(false, there, next);
+        weigh(s, cut, keys, w);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");       // V is there
+        add(careful, cut, keys, w);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        send(true, there, next);
+      } else {
+        s = zero16();
+#pragma unroll
+        for (int i = 0; i < KL; ++i) {
+          uint4 y[EPL / 8];
+          unpack(raw.k[i], raw.ks[i], y);
+#pragma unroll
+          for (int e = 0; e < EPL / 8; ++e) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(at_bf16x8_t, y[e]), q.x[i * (EPL / 8) + e], s, 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        load_k(there, next);
+#pragma unroll
+        for (int j = 0; j < VL; ++j) {
+          uint4 y[EPL / 8];
+          unpack(raw.v[j], raw.vs[j], y);
+          park(j, y);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        load_v(there, next);
+        weigh(s, cut, keys, w);
+        __builtin_amdgcn_sched_barrier(0);
+        add(careful, cut, keys, w);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if constexpr (CACHE == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // (what was sent for past the end goes to LDS, too)
+#pragma unroll 1
+    for (int t = 0; t < node_tiles; ++t) {
+      if ((row_tiles + t) % NW != wave) continue;
+      at_f32x16_t s = zero16();
+#pragma unroll
+      for (int i = 0; i < KL; ++i) {
+        uint4 y[EPL / 8];
+        node_part(a.k_new, 32 * t + col, CACHE ? 2 * i + half : half * KL + i, y);
+#pragma unroll
+        for (int e = 0; e < EPL / 8; ++e) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(at_bf16x8_t, y[e]), q.x[i * (EPL / 8) + e], s, 0, 0, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < VL; ++j) {
+        uint4 y[EPL / 8];
+        node_part(a.v_new, 32 * t + (j * 64 + lane) / LPR, (j * 64 + lane) % LPR, y);
+        park(j, y);
+      }
+      typename Tile::template Weights<PARTS> w;
+      const int left = a.T - 32 * t;
+      const uint32_t keys = (uint32_t)(mask >> (32 * t)) & (left >= 32 ? ~0u : (1u << left) - 1u);
+      weigh(s, true, keys, w);
+      add(careful, true, keys, w);
+    }
+  };
+  pass(std::false_type{});
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(not_finite(st)) != 0, 0)) pass(std::true_type{});
+
+  // ---- the waves' results, joined in wave order: four dims of a column per thread
+  const float sum = both_sum(st.sum);
+  const auto result = [&](int w, int c) { return reinterpret_cast<float*>(s_tiles + w * EACH) + c * RS; };
+  if (half == 0) { s_ml[wave][col][0] = st.ref; s_ml[wave][col][1] = sum; }
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<at_f32x4_t*>(result(wave, col) + 32 * db + 8 * g + 4 * half) = at_f32x4_t{st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]};
+  __syncthreads();
+  constexpr int TL = D / 4;
+  const int t4 = tid % TL;
+#pragma unroll 1
+  for (int cc = tid / TL; cc < a.R; cc += 256 / TL) {
+    float m = s_ml[0][cc][0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) m = fmaxf(m, s_ml[w][cc][0]);
+    float l = 0.f;
+    at_f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      // (a wave that has seen nothing: reference -inf, sum 0)
+      const float ref = s_ml[w][cc][0], f = ref == -__builtin_inff() && s_ml[w][cc][1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ref - m);
+      const at_f32x4_t y = *reinterpret_cast<const at_f32x4_t*>(result(w, cc) + 4 * t4);
+      l += s_ml[w][cc][1] * f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += y[e] * f;
+    }
+    if (pieces > 1) {
+      const long long record = ((long long)x * a.slots + chunk) * a.R + cc;
+      *reinterpret_cast<at_f32x4_t*>(a.part + record * D + 4 * t4) = o;
+      if (t4 == 0) *reinterpret_cast<float2*>(a.part_ml + record * 2) = make_float2(m, l);
+    } else {
+      store4(reinterpret_cast<OT*>(a.out) + ((long long)x * a.R + cc) * D + 4 * t4, o, 1.f / l);
     }
   }
 }
@@ -312,32 +627,30 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int n_column
       m = bm;
     }
   }
-  OT* to = reinterpret_cast<OT*>(a.out) + (long long)x * D + 4 * t4;
-  const float inv = 1.f / l;
-  if constexpr (sizeof(OT) == 4) {
-    *reinterpret_cast<at_f32x4_t*>(to) = at_f32x4_t{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-  } else {
-    *reinterpret_cast<uint2*>(to) = make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector((at_f32x2_t{o[0] * inv, o[1] * inv}), at_bf16x2_t)),
-                                               __builtin_bit_cast(uint32_t, __builtin_convertvector((at_f32x2_t{o[2] * inv, o[3] * inv}), at_bf16x2_t)));
-  }
+  store4(reinterpret_cast<OT*>(a.out) + (long long)x * D + 4 * t4, o, 1.f / l);
 }
 
-// Blocks of columns of a workgroup, workgroups of a head side by side, rows per piece, most pieces, pieces of the grid.
-struct TreePlan { int wc, groups, chunk_rows, max_chunks, slots; };
 #ifndef TW
 #define TW 512
-#define TMIN 128
 #endif
+#ifndef TN
+#define TN 384
+#endif
+#ifndef TMIN
+#define TMIN 256
+#endif
+// Blocks of columns of a workgroup, workgroups of a head side by side, rows per piece, most pieces, pieces of the grid.
+struct TreePlan { int wc, groups, chunk_rows, max_chunks, slots; };       // wc = 0: tree_narrow_kernel
 static TreePlan tree_plan(const Dims& dm, const madakv_config& c, int T, int longest_rows) {
   TreePlan p;
   const int R = dm.G * T;
-  p.wc = R <= 32 ? 1 : R <= 64 ? 2 : 4;
-  p.groups = (R + 32 * p.wc - 1) / (32 * p.wc);
-  const long long typical = std::min(c.budget, c.ctx_len) + (long long)T;
-  const long long want = std::max<long long>(1, TW / ((long long)dm.heads * p.groups));
+  p.wc = R <= 32 ? (c.dtype == MADAKV_BF16 ? 0 : 1) : R <= 64 ? 2 : 4;
+  p.groups = p.wc ? (R + 32 * p.wc - 1) / (32 * p.wc) : 1;
+  const long long typical = std::min(c.budget, c.ctx_len);
+  const long long want = std::max<long long>(1, (p.wc ? TW : TN) / ((long long)dm.heads * p.groups));
   p.chunk_rows = (int)std::max<long long>(TMIN, (typical / want + ATT_TILE - 1) / ATT_TILE * ATT_TILE);
   p.max_chunks = (int)((std::max(2, c.hcc_rho) * typical + p.chunk_rows - 1) / p.chunk_rows);
-  const int longest = std::max(1, std::min(longest_rows, c.ctx_len + c.max_new_tokens)) + T;
+  const int longest = std::max(1, std::min(longest_rows, c.ctx_len + c.max_new_tokens));
   p.slots = std::min(p.max_chunks, (longest + p.chunk_rows - 1) / p.chunk_rows);
   return p;
 }
@@ -349,7 +662,8 @@ size_t tree_ws_bytes(const Dims& dm, const madakv_config& c, int T, int longest_
 template <typename T, typename OT, int CACHE, int D>
 static hipError_t launch_tree(const Dims& dm, const TreeArgs& a, const TreePlan& p, hipStream_t st) {
   const dim3 grid(dm.heads * p.groups, p.slots);
-  if (p.wc == 1) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 1>), grid, dim3(128), 0, st, a);
+  if (p.wc == 0) { if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((tree_narrow_kernel<OT, CACHE, D>), grid, dim3(256), 0, st, a); }
+  else if (p.wc == 1) { if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 1>), grid, dim3(128), 0, st, a); }
   else if (p.wc == 2) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 2>), grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 4>), grid, dim3(512), 0, st, a);
   hipError_t e = hipGetLastError();

@@ -64,7 +64,9 @@ for h in map(create, sys.argv[3:]):
         for n in (1, 2):
             assert tree(h, n=n, t=t, size=need(h, 2, 64)) == 0
             k = kinds()
-            assert len([x for x in k if x != "query"]) == 1 and "tree_attn" in k[-1], k
+            k = [x for x in k if x != "query"]
+            assert "tree_attn" in k[0] or "tree_narrow" in k[0], k
+            assert [("tree_join" in x) for x in k[1:]] in ([], [True]), k
 print("ok")
 """, good(), good(dtype=MB.FP32, head_dim=64, window=16), good(cache_fp8=1, out_fp32=0), good(cache_fp8=4, n_q_heads=64, window=8, page_rows=16))
     assert out.strip() == "ok"
@@ -124,7 +126,7 @@ h = create(sys.argv[3])
 assert lib.madakv_select_gather(h, I(0), I(2), *[P(T().p) for _ in range(10)], P(T().p), Z(1 << 40), P(0)) == 0
 fake.fake_events_done(1)
 log()
-grid = lambda: [x.rest[1] for x in log() if x.kind == "launch"][-1]
+grid = lambda: [x.rest[1] for x in log() if x.kind == "launch" and "tree_join" not in x.rest[3]][-1]
 assert tree(h) == 0
 short = grid()
 s = 0x77000
