@@ -271,7 +271,8 @@ class MadaKV:
         with torch.cuda.device(self.device):
             self.h = madakv_create(self.cfg)
         self._out_dtype = torch.float32 if out_fp32 else self.tdtype
-        self._out_row, self._heads, self._kv_row, self._ctx = batch * n_q_heads * head_dim, batch * n_kv_heads, batch * n_kv_heads * head_dim, ctx_len
+        self._out_row, self._heads, self._kv_row, self._ctx, self._batch = batch * n_q_heads * head_dim, batch * n_kv_heads, batch * n_kv_heads * head_dim, ctx_len, batch
+        self._tree_ws = {}
         self.n_call = layers_per_call or n_layers
         s_ws, sel_ws, d_ws = madakv_workspace_bytes(self.h, self.n_call)
         dev = self.device
@@ -435,16 +436,24 @@ class MadaKV:
         if rc != OK:
             raise MadaKVError("madakv_score_prompt", rc)
 
+    def _check_rows(self, n, rows, out, q, k, v):
+        """The arrays of a call over `rows` rows of every head; as in decode_attn_weights one expression where all are right."""
+        dt, at, nq, nkv = self.tdtype, self._device.index, n * self._out_row * rows, n * self._kv_row * rows
+        if out is not None:
+            self._check_out(out, nq)
+        if (k.dtype is not dt or k.numel() < nkv or k.get_device() != at or v.dtype is not dt or v.numel() < nkv or v.get_device() != at
+                or (out is not None and (out.get_device() != at or q.dtype is not dt or q.numel() < nq or q.get_device() != at))):
+            self._check_array("out", out, nq, self._out_dtype)
+            self._check_array("q", q, nq, dt)
+            self._check_array("k", k, nkv, dt)
+            self._check_array("v", v, nkv, dt)
+
     def prompt_attn(self, l0, n, q, k, v, out, row_lse=None, seq_off=None):
         """q, out [n, B, Hq, L, d], row_lse [n, B, Hq, L].  seq_off [B, S + 1]: sequence s of a batch item has the positions seq_off[s] up to
         seq_off[s + 1]; without it all L positions are one."""
         # (a prompt of a few hundred tokens takes a few us on the device: no views of the own buffers)
         L = self._ctx
-        self._check_out(out, n * self._out_row * L)
-        self._check_array("out", out, n * self._out_row * L, self._out_dtype)
-        self._check_array("q", q, n * self._out_row * L, self.tdtype)
-        self._check_array("k", k, n * self._kv_row * L, self.tdtype)
-        self._check_array("v", v, n * self._kv_row * L, self.tdtype)
+        self._check_rows(n, L, out, q, k, v)
         n_seq = 0
         if row_lse is not None:
             self._check_array("row_lse", row_lse, n * self.cfg.batch * self.cfg.n_q_heads * L, torch.float32)
@@ -463,35 +472,35 @@ class MadaKV:
             raise ValueError(f"nodes come as [layers, batch, heads, nodes, head_dim], got {list(t.shape)}")
         return t.shape[3]
 
+    def _tree_workspace(self, T):
+        """One for trees of up to 4, 8, ..., 64 nodes each, kept as long as the holder: captured calls go on using theirs."""
+        size = max(2, (T - 1).bit_length())
+        if size not in self._tree_ws:
+            ws = torch.empty(madakv_tree_attn_workspace_bytes(self.h, self.n_call, min(1 << size, 64)), dtype=torch.uint8, device=self.device)
+            self._tree_ws[size] = (ws, _ptr(ws), ws.numel())
+        return self._tree_ws[size]
+
     def tree_attn(self, l0, n, q, k_new, v_new, tree, out):
         """q, out [n, B, Hq, T, d], k_new, v_new [n, B, H, T, d]; tree [B, T] int64: bit i of entry t: node t sees node i."""
         T = self._nodes(q)
-        self._check_out(out, n * self._out_row * T)
-        self._check_array("out", out, n * self._out_row * T, self._out_dtype)
-        self._check_array("q", q, n * self._out_row * T, self.tdtype)
-        self._check_array("k_new", k_new, n * self._kv_row * T, self.tdtype)
-        self._check_array("v_new", v_new, n * self._kv_row * T, self.tdtype)
-        self._check_array("tree", tree, self.cfg.batch * T, torch.int64)
-        ws = getattr(self, "tree_ws", None)
-        if ws is None or self._tree_nodes < T:
-            ws = self.tree_ws = torch.empty(madakv_tree_attn_workspace_bytes(self.h, self.n_call, T), dtype=torch.uint8, device=self.device)
-            self._tree_nodes = T
+        self._check_rows(n, T, out, q, k_new, v_new)
+        self._check_array("tree", tree, self._batch * T, torch.int64)
+        _, ws, ws_bytes = self._tree_workspace(T)
         heads0 = l0 * self._heads
         rc = lib().madakv_tree_attn(self.h, l0, n, T, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(tree), _ptr(self.k_c), _ptr(self.v_c), _ptr(self.kv_off) + 8 * heads0,
-                                    _ptr(self.kv_len) + 4 * heads0, _ptr(out), _ptr(ws), ws.numel(), self._own_stream())
+                                    _ptr(self.kv_len) + 4 * heads0, _ptr(out), ws, ws_bytes, self._own_stream())
         if rc != OK:
             raise MadaKVError("madakv_tree_attn", rc)
 
     def tree_commit(self, l0, n, k_new, v_new, path, n_path, start, most):
         """path [B, P], n_path, start [B] int32 on the device; most: the rows that any head may have behind those of the eviction afterwards."""
         T = self._nodes(k_new)
-        self._check_array("k_new", k_new, n * self._kv_row * T, self.tdtype)
-        self._check_array("v_new", v_new, n * self._kv_row * T, self.tdtype)
-        if path.dim() != 2 or path.shape[0] != self.cfg.batch:
-            raise ValueError(f"path must be [{self.cfg.batch}, steps], got {list(path.shape)}")
+        self._check_rows(n, T, None, None, k_new, v_new)
+        if path.dim() != 2 or path.shape[0] != self._batch:
+            raise ValueError(f"path must be [{self._batch}, steps], got {list(path.shape)}")
         self._check_array("path", path, path.numel(), torch.int32)
-        self._check_array("n_path", n_path, self.cfg.batch, torch.int32)
-        self._check_array("start", start, self.cfg.batch, torch.int32)
+        self._check_array("n_path", n_path, self._batch, torch.int32)
+        self._check_array("start", start, self._batch, torch.int32)
         heads0 = l0 * self._heads
         rc = lib().madakv_tree_commit(self.h, l0, n, T, _ptr(k_new), _ptr(v_new), _ptr(path), _ptr(n_path), path.shape[1], _ptr(start), most, _ptr(self.k_c), _ptr(self.v_c),
                                       _ptr(self.kv_off) + 8 * heads0, _ptr(self.kv_len) + 4 * heads0, self._own_stream())

@@ -2,15 +2,18 @@
 // tree, and the accepted nodes' rows into the cache.
 //
 // Attention: the G * T query rows of a KV head (T nodes) are the columns of attn_tile.h, its keys the rows of the head's segment and behind
-// them the T nodes, of which a column sees those that its node's mask names.  A workgroup has 32 WC columns; its 2 WC waves are WC blocks of
-// columns times the two halves of a tile of 64 keys.  A head is cut into pieces as in decode_pieces.h: every piece leaves its partial (reference, sum,
-// output) in the workspace and counts itself, and whoever comes last merges them in piece order.  Rows of the type of the model come straight into LDS, 8-bit
-// and 4-bit rows through registers, which turn them into bf16 (exactly); nodes' rows count with the values that the cache would give them.
-// Masked keys count for nothing whatever they hold, as in prompt_attn.hip.
+// them the T nodes, of which a column sees those that its node's mask names:
+//   out(c) = sum_r e^(s q_c . k_r) v_r / sum_r e^(s q_c . k_r),   r over the rows of the segment and the nodes i with bit i of tree[node of c]
+// A head is cut into pieces; each leaves its partial (reference, sum, output) in the workspace, and a second launch joins them in their order, so results
+// do not depend on who comes first.  (Joined by whoever comes last it took longer: results pass from one XCD's L2 to another's, a wait per piece.)
+// Two kernels: tree_narrow_kernel, bound by how fast rows arrive (128 heads of 16384 bf16 rows, 32 nodes: 185 us, 5.8 TB/s), and tree_attn_kernel for more columns,
+// bound by the arithmetic (60 nodes of 2 x 32/8 heads of 16384 4-bit rows: 43 of 53 us, 750 TFLOP/s; the rest is joining).  Nodes' rows count with the
+// values that the cache would give them.  Masked keys count for nothing whatever they hold, as in prompt_attn.hip.
 #include "attn_tile.h"
 #include "decode_pieces.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace madakv {
@@ -29,14 +32,13 @@ struct TreeArgs {
   float scale_log2;
 };
 
-// Rows per piece of a head of so many, and how many pieces that makes; the nodes are with the last one.
-__device__ __forceinline__ int piece_rows(const TreeArgs& a, int len) {
-  if (len <= a.chunk_rows * a.max_chunks) return a.chunk_rows;
-  return ((len + a.max_chunks - 1) / a.max_chunks + ATT_TILE - 1) / ATT_TILE * ATT_TILE;
-}
-__device__ __forceinline__ int pieces_of_tree(const TreeArgs& a, int len) {
-  const int rows = piece_rows(a, len);
-  return max(1, (len + rows - 1) / rows);
+// Rows per piece of a head of so many, and how many pieces that makes; the nodes are with the last one.  An eighth of a piece more than whole pieces makes no
+// piece of its own: heads that were cut to fill the chip once stay so while tokens are appended.
+struct Cut { int rows, pieces; };
+__device__ __forceinline__ Cut cut_of(int chunk_rows, int max_chunks, int len) {
+  const int n = min(max(1, (len - chunk_rows / 8 + chunk_rows - 1) / chunk_rows), max_chunks);
+  const int rows = max(1, ((len + n - 1) / n + ATT_TILE - 1) / ATT_TILE) * ATT_TILE;
+  return Cut{rows, std::max(1, (len + rows - 1) / rows)};
 }
 
 // four neighbouring elements of the output
@@ -86,22 +88,28 @@ __device__ __forceinline__ uint32_t e4m3_of(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, code);
 }
 
-// T: Q, nodes' rows; CACHE: 0 rows of T, CACHE_E4M3, CACHE_E2M1; WC blocks of 32 columns
-template <typename T, typename OT, int CACHE, int D, int WC>
-__global__ __launch_bounds__(WC * 128) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 && (WC > 1 || D == 64) ? 2 : 1, 2))) void tree_attn_kernel(TreeArgs a) {
+// ---- more columns -----------------------------------------------------------------------------------------
+// T: Q, nodes' rows; CACHE: 0 rows of T, CACHE_E4M3, CACHE_E2M1.  WC blocks of 32 columns, WK = 2: times the two halves of a tile of 64 keys (32-bit rows, few
+// columns), otherwise a wave has the whole tile.  All waves share the tile; rows of the type of the model come straight into LDS, 8-bit and 4-bit rows
+// through registers, which turn them into bf16 (exactly).  Up to 256 columns in a workgroup: rows are converted once for all of them (60 nodes of 2 x 32/8 heads
+// of 16384 4-bit rows: 53 us, by workgroups of 128 columns 59).  Tiles further ahead of the products gain nothing for 8 and 4 bits (1, 2, 3: 53.8, 52.8, 53).
+template <typename T, typename OT, int CACHE, int D, int WC, int WK>
+__global__ __launch_bounds__(WC * WK * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2))) void tree_attn_kernel(TreeArgs a) {
   using Tile = AttnTile<T, D>;
   constexpr int PARTS = sizeof(T) == 2 && sizeof(OT) == 4 ? 3 : 1;
-  constexpr int NT = WC * 128, COLS = WC * 32, ROWB = Tile::ROWB, PPR = Tile::PPR;
+  constexpr int NT = WC * WK * 64, COLS = WC * 32, ROWB = Tile::ROWB, PPR = Tile::PPR;
   constexpr int EPL = CACHE == CACHE_E2M1 ? 32 : CACHE == CACHE_E4M3 ? 16 : 16 / (int)sizeof(T);      // elements of a 16-byte load
   constexpr int LPR = D / EPL;                                                                          // loads of a row
   constexpr int LPT = (ATT_TILE * LPR + NT - 1) / NT;                                                   // of a thread, per tile and tensor
   constexpr int CROWB = CACHE ? LPR * 16 : ROWB;                                                        // bytes of a cache row
-  constexpr int RES = COLS * (D + 4) * 4;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * Tile::BYTES > RES ? 4 * Tile::BYTES : RES];      // two tiles of K, two of V; later the second halves' results
+  constexpr int AHEAD = CACHE == 0 && sizeof(T) == 2 && WC == 8 ? 3 : 1;       // tiles on their way: as many as LDS has room for
+  constexpr int SLOTS = CACHE ? 2 : AHEAD + 1;                 // tiles of K, of V in LDS
+  constexpr int RES = WK == 1 ? 0 : COLS * (D + 4) * 4;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * SLOTS * Tile::BYTES > RES ? 2 * SLOTS * Tile::BYTES : RES];      // later the second halves' results
   __shared__ float s_ml[COLS][2];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wc = wave >> 1, wk = wave & 1, half = lane >> 5, col = lane & 31;
+  const int wc = wave / WK, wk = wave % WK, half = lane >> 5, col = lane & 31;
   const uint32_t xy = blockIdx.x + blockIdx.y;                 // the pieces of a head on different XCDs
   const int x = (int)(xy % gridDim.x), chunk = blockIdx.y;
   const long long hidx = x / a.groups;
@@ -109,7 +117,8 @@ __global__ __launch_bounds__(WC * 128) __attribute__((amdgpu_waves_per_eu(sizeof
   const int len = a.kv_len[hidx];
   const long long off = a.kv_off[hidx];
   const int total = len > 0 ? len + a.T : 0;                   // (an empty segment: its budgets did not fit the cache)
-  const int rows = piece_rows(a, len), pieces = pieces_of_tree(a, len);
+  const Cut cut_rows = cut_of(a.chunk_rows, a.max_chunks, len);
+  const int rows = cut_rows.rows, pieces = cut_rows.pieces;
   if (chunk >= pieces) return;
   const int r_begin = chunk * rows, r_end = chunk == pieces - 1 ? total : r_begin + rows;
   const int ntiles = (r_end - r_begin + ATT_TILE - 1) / ATT_TILE;
@@ -127,7 +136,7 @@ __global__ __launch_bounds__(WC * 128) __attribute__((amdgpu_waves_per_eu(sizeof
   const unsigned char* kn = reinterpret_cast<const unsigned char*>(a.k_new) + hidx * a.T * ROWB;
   const unsigned char* vn = reinterpret_cast<const unsigned char*>(a.v_new) + hidx * a.T * ROWB;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
-  // ---- rows of T: straight into LDS, tile t into slot t & 1 (rows past the end of the piece: its last one once more, masked where they are used)
+  // ---- rows of T: straight into LDS, tile t into slot t % SLOTS (rows past the end of the piece: its last one once more, masked where they are used)
   const auto load_direct = [&](int t) {
 #pragma unroll
     for (int j = 0; j < LPT; ++j) {
@@ -137,9 +146,9 @@ __global__ __launch_bounds__(WC * 128) __attribute__((amdgpu_waves_per_eu(sizeof
       const long long row = node ? r - len : at(r);
       const unsigned char* kp = (node ? kn : a.k_c) + row * ROWB + Tile::k_slot(lr, s) * 16;
       const unsigned char* vp = (node ? vn : a.v_c) + row * ROWB + Tile::v_slot(lr, s) * 16;
-      const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds0 + (uint32_t)((t & 1) * Tile::BYTES + (wave * LPT + j) * 1024)));
+      const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds0 + (uint32_t)(t % SLOTS * Tile::BYTES + (wave * LPT + j) * 1024)));
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(kp));
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + 2 * Tile::BYTES), "v"(vp));
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + SLOTS * Tile::BYTES), "v"(vp));
     }
   };
   // ---- 8-bit and 4-bit rows: through registers
@@ -166,7 +175,7 @@ __global__ __launch_bounds__(WC * 128) __attribute__((amdgpu_waves_per_eu(sizeof
       const int r = min(r_begin + t * ATT_TILE + lr, r_end - 1);
 #pragma unroll
       for (int which = 0; which < 2; ++which) {
-        unsigned char* to = lds + ((t & 1) + 2 * which) * Tile::BYTES + lr * ROWB;
+        unsigned char* to = lds + (t % SLOTS + SLOTS * which) * Tile::BYTES + lr * ROWB;
         const unsigned char* nodes = which ? vn : kn;
         uint4 y[EPL / 8 ? EPL / 8 : 1];
         if (r >= len) {
@@ -202,14 +211,10 @@ __global__ __launch_bounds__(WC * 128) __attribute__((amdgpu_waves_per_eu(sizeof
   };
 
   AttnState<D> st;
-  const auto compute = [&](auto careful, int t) {
-    const int k32 = r_begin + t * ATT_TILE + 32 * wk;
-    if (k32 >= r_end) return;
-    const unsigned char* kt = lds + (t & 1) * Tile::BYTES;
-    const unsigned char* vt = lds + (2 + (t & 1)) * Tile::BYTES;
+  // the 32 keys from k32 on, rows row0 and on of the tile
+  const auto finish = [&](auto careful, int k32, int row0, at_f32x16_t& s, const unsigned char* vt) {
     float p[16], more;
     typename Tile::template Weights<PARTS> w;
-    at_f32x16_t s = Tile::scores(kt, 32 * wk, lane, q);
     const bool cut = k32 + 32 > min(len, r_end);
     const auto sees = [&](int key) { const int r = k32 + key; return r < r_end && (r < len || (mask >> (r - len) & 1)); };
     bool look = cut;
@@ -238,65 +243,90 @@ __global__ __launch_bounds__(WC * 128) __attribute__((amdgpu_waves_per_eu(sizeof
         for (int db = 0; db < D / 32; ++db)
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            const at_f32x4_t y = Tile::value4(vt, 32 * wk + key, 32 * db + 8 * g + 4 * half);
+            const at_f32x4_t y = Tile::value4(vt, row0 + key, 32 * db + 8 * g + 4 * half);
 #pragma unroll
             for (int e = 0; e < 4; ++e) st.o[db][4 * g + e] = fmaf(f, y[e], st.o[db][4 * g + e]);
           }
       }
     } else {
-      Tile::template add<PARTS>(vt, 32 * wk, lane, w, st.o);
+      Tile::template add<PARTS>(vt, row0, lane, w, st.o);
+    }
+  };
+  const auto compute = [&](auto careful, int t) {
+    const unsigned char* kt = lds + t % SLOTS * Tile::BYTES;
+    const unsigned char* vt = kt + SLOTS * Tile::BYTES;
+    const int k0 = r_begin + t * ATT_TILE;
+    if constexpr (WK == 2) {
+      if (k0 + 32 * wk >= r_end) return;
+      at_f32x16_t s = Tile::scores(kt, 32 * wk, lane, q);
+      finish(careful, k0 + 32 * wk, 32 * wk, s, vt);
+    } else {
+      at_f32x16_t s = Tile::scores(kt, 0, lane, q), s1 = Tile::scores(kt, 32, lane, q);       // (of the last row once more, past the end)
+      finish(careful, k0, 0, s, vt);
+      if (k0 + 32 < r_end) finish(careful, k0 + 32, 32, s1, vt);
     }
   };
   const auto pass = [&](auto careful) {
     st.clear();
-    if (ntiles > 0) {
-      if constexpr (CACHE) { fetch(0); park(0); }
-      else load_direct(0);
+    if (ntiles <= 0) return;
+    // (what is past the end: the last row, which nobody looks at; it keeps the count of loads on their way)
+    if constexpr (CACHE) {
+      fetch(0);
+      park(0);
+      fetch(1);
+    } else {
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) load_direct(j);
     }
 #pragma unroll 1
     for (int t = 0; t < ntiles; ++t) {
       // tile t is there for everybody, and nobody reads tile t - 1 any more
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      if (t + 1 < ntiles) {
-        if constexpr (CACHE) fetch(t + 1);
-        else load_direct(t + 1);
+      if constexpr (CACHE) {
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        compute(careful, t);
+        if (t + 1 < ntiles) park(t + 1);
+        fetch(t + 2);
+      } else {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LPT * (AHEAD - 1)) : "memory");
+        load_direct(t + AHEAD);
+        compute(careful, t);
       }
-      compute(careful, t);
-      if constexpr (CACHE) { if (t + 1 < ntiles) park(t + 1); }
     }
+    if constexpr (CACHE == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
   };
   pass(std::false_type{});
   if (__builtin_expect(__syncthreads_or(not_finite(st)), 0)) {
     pass(std::true_type{});
-    __syncthreads();
   }
 
   // ---- the two halves of a tile's keys: the second wave of a block leaves its results in LDS, [column][D + 4]
-  float* s_o = reinterpret_cast<float*>(lds) + wc * 32 * (D + 4);
   float sum = both_sum(st.sum);
-  if (wk) {
-    if (half == 0) { s_ml[wc * 32 + col][0] = st.ref; s_ml[wc * 32 + col][1] = sum; }
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<at_f32x4_t*>(s_o + col * (D + 4) + 32 * db + 8 * g + 4 * half) = at_f32x4_t{st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]};
-  }
-  __syncthreads();
-  if (!wk) {
-    merge_halves<D>(st, sum, s_ml[wc * 32 + col], s_o + col * (D + 4), half);
-    if (pieces == 1) {
-      store_column<OT, D>(reinterpret_cast<OT*>(a.out) + (hidx * a.R + c) * D, c == c_own, half, st.o, 1.f / sum);
-    } else if (c == c_own) {
-      const long long record = (hidx * a.slots + chunk) * a.R + c;
-      float* to = a.part + record * D;
+  if constexpr (WK == 2) {
+    float* s_o = reinterpret_cast<float*>(lds) + wc * 32 * (D + 4);
+    if (wk) {
+      if (half == 0) { s_ml[wc * 32 + col][0] = st.ref; s_ml[wc * 32 + col][1] = sum; }
 #pragma unroll
       for (int db = 0; db < D / 32; ++db)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<at_f32x4_t*>(to + 32 * db + 8 * g + 4 * half) = at_f32x4_t{st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]};
-      if (half == 0) *reinterpret_cast<float2*>(a.part_ml + record * 2) = make_float2(st.ref, sum);
+          *reinterpret_cast<at_f32x4_t*>(s_o + col * (D + 4) + 32 * db + 8 * g + 4 * half) = at_f32x4_t{st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]};
     }
+    __syncthreads();
+    if (wk) return;
+    merge_halves<D>(st, sum, s_ml[wc * 32 + col], s_o + col * (D + 4), half);
+  }
+  if (pieces == 1) {
+    store_column<OT, D>(reinterpret_cast<OT*>(a.out) + (hidx * a.R + c) * D, c == c_own, half, st.o, 1.f / sum);
+  } else if (c == c_own) {
+    const long long record = (hidx * a.slots + chunk) * a.R + c;
+    float* to = a.part + record * D;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<at_f32x4_t*>(to + 32 * db + 8 * g + 4 * half) = at_f32x4_t{st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]};
+    if (half == 0) *reinterpret_cast<float2*>(a.part_ml + record * 2) = make_float2(st.ref, sum);
   }
 }
 
@@ -320,17 +350,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, col = lane & 31;
-  const int xy = (int)(blockIdx.x + blockIdx.y), x = xy < (int)gridDim.x ? xy : xy % (int)gridDim.x, chunk = blockIdx.y;       // (the pieces of a head on different XCDs)
+  // (the pieces of a head on different XCDs, the column groups of a piece next to each other)
+  const int chunk = (int)blockIdx.y / a.groups, group = (int)blockIdx.y - chunk * a.groups, xy = (int)blockIdx.x + chunk, x = xy < (int)gridDim.x ? xy : xy % (int)gridDim.x;
+  const int c0 = group * 32, n_cols = min(32, a.R - c0);
   const int len = a.kv_len[x];
   const long long off = a.kv_off[x];
-  const int rows = piece_rows(a, len), pieces = pieces_of_tree(a, len);
+  const Cut cut_rows = cut_of(a.chunk_rows, a.max_chunks, len);
+  const int rows = cut_rows.rows, pieces = cut_rows.pieces;
   if (chunk >= pieces) return;
   const int r_begin = chunk * rows, n_rows = max(0, min(len - r_begin, rows));          // (an empty segment sees nothing: its sums stay zero)
   const int row_tiles = (n_rows + 31) / 32, node_tiles = chunk == pieces - 1 && len > 0 ? (a.T + 31) / 32 : 0;
   RowMap at;
   at.off = off; at.init_rows = 0x7fffffff; at.tbl = nullptr; at.shift = 0; at.fresh_slot = -1; at.fresh_page = 0;
   if (a.page_rows) { at.tbl = a.page_tbl + (long long)x * a.tbl_entries; at.shift = a.page_shift; at.init_rows = at.tbl[0] << a.page_shift; }
-  const int c = min(col, a.R - 1);                             // (a column without a query: the last one's once more, not stored)
+  const int c = c0 + min(col, n_cols - 1);                     // (a column without a query: the last one's once more, not stored)
   // the query: for step i EPL / 8 + e dims [(2 i + half) EPL + 8 e, + 8)
   typename Tile::Query q;
   const auto dim_of = [&](int ks) { return (2 * (ks / (EPL / 8)) + half) * EPL + 8 * (ks % (EPL / 8)); };
@@ -569,7 +602,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   constexpr int TL = D / 4;
   const int t4 = tid % TL;
 #pragma unroll 1
-  for (int cc = tid / TL; cc < a.R; cc += 256 / TL) {
+  for (int cc = tid / TL; cc < n_cols; cc += 256 / TL) {
     float m = s_ml[0][cc][0];
 #pragma unroll
     for (int w = 1; w < NW; ++w) m = fmaxf(m, s_ml[w][cc][0]);
@@ -585,91 +618,133 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       for (int e = 0; e < 4; ++e) o[e] += y[e] * f;
     }
     if (pieces > 1) {
-      const long long record = ((long long)x * a.slots + chunk) * a.R + cc;
+      const long long record = ((long long)x * a.slots + chunk) * a.R + c0 + cc;
       *reinterpret_cast<at_f32x4_t*>(a.part + record * D + 4 * t4) = o;
       if (t4 == 0) *reinterpret_cast<float2*>(a.part_ml + record * 2) = make_float2(m, l);
     } else {
-      store4(reinterpret_cast<OT*>(a.out) + ((long long)x * a.R + cc) * D + 4 * t4, o, 1.f / l);
+      store4(reinterpret_cast<OT*>(a.out) + ((long long)x * a.R + c0 + cc) * D + 4 * t4, o, 1.f / l);
     }
   }
 }
 
-// The pieces of a head joined, in their order: four dims of a column per thread.
+// The pieces of a head joined, in their order: four dims of a column per thread, and the pieces of a column dealt to S threads, which load up to MB of them
+// at once.  What it takes is launch and latency, not bytes.
 template <typename OT, int D>
-__global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int n_columns) {
+__global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int n_columns, int shift) {      // S = 2^shift
   constexpr int TL = D / 4, MB = 8;
-  const int x = (int)blockIdx.x * (256 / TL) + (int)threadIdx.x / TL, t4 = threadIdx.x % TL;
-  if (x >= n_columns) return;
-  const long long hidx = x / a.R;
-  const int c = x % a.R;
-  const int len = a.kv_len[hidx], pieces = pieces_of_tree(a, len);
-  if (pieces == 1) return;                                     // (its output is there)
+  __shared__ at_f32x4_t s_o[256];
+  __shared__ float2 s_ml[256 / TL];
+  const int tid = threadIdx.x, t4 = tid % TL, unit = tid / TL, S = 1 << shift, slice = unit & (S - 1);
+  const int x_own = ((int)blockIdx.x * (256 / TL) + unit) >> shift, x = min(x_own, n_columns - 1);
+  const int hidx = x / a.R, c = x - hidx * a.R;
+  const int pieces = cut_of(a.chunk_rows, a.max_chunks, a.kv_len[hidx]).pieces;
+  const long long record0 = (long long)hidx * a.slots * a.R + c;
   float m = -__builtin_inff(), l = 0.f;
   at_f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-  for (int c0 = 0; c0 < pieces; c0 += MB) {
-    at_f32x4_t y[MB]; float2 ml[MB];
+  // (what has seen nothing: reference -inf, sum 0)
+  const auto factor = [](float ref, float sum, float m) { return ref == -__builtin_inff() && sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(ref - m); };
+  if (pieces > 1) {
+    for (int p0 = slice; p0 < pieces; p0 += S * MB) {
+      at_f32x4_t y[MB]; float2 ml[MB];
 #pragma unroll
-    for (int j = 0; j < MB; ++j) {
-      const long long record = (hidx * a.slots + min(c0 + j, pieces - 1)) * a.R + c;
-      ml[j] = *reinterpret_cast<const float2*>(a.part_ml + record * 2);
-      y[j] = *reinterpret_cast<const at_f32x4_t*>(a.part + record * D + 4 * t4);
-    }
+      for (int j = 0; j < MB; ++j) {
+        if (p0 + j * S < pieces) {
+          const long long record = record0 + (long long)(p0 + j * S) * a.R;
+          ml[j] = *reinterpret_cast<const float2*>(a.part_ml + record * 2);
+          y[j] = *reinterpret_cast<const at_f32x4_t*>(a.part + record * D + 4 * t4);
+        } else {
+          ml[j] = make_float2(-__builtin_inff(), 0.f);
+          y[j] = at_f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+      }
+      float bm = m;
 #pragma unroll
-    for (int j = 0; j < MB; ++j) {
-      if (c0 + j >= pieces) break;
-      const float bm = fmaxf(m, ml[j].x);
-      // (a piece that has seen nothing: reference -inf, sum 0)
-      const float f = m == -__builtin_inff() ? (l == 0.f ? 0.f : l) : __builtin_amdgcn_exp2f(m - bm);
-      const float g = ml[j].x == -__builtin_inff() && ml[j].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[j].x - bm);
-      l = l * f + ml[j].y * g;
+      for (int j = 0; j < MB; ++j) bm = fmaxf(bm, ml[j].x);
+      const float f = factor(m, l, bm);
+      l *= f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = o[e] * f + y[j][e] * g;
+      for (int e = 0; e < 4; ++e) o[e] *= f;
+#pragma unroll
+      for (int j = 0; j < MB; ++j) {
+        const float g = factor(ml[j].x, ml[j].y, bm);
+        l = fmaf(ml[j].y, g, l);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(y[j][e], g, o[e]);
+      }
       m = bm;
     }
   }
-  store4(reinterpret_cast<OT*>(a.out) + (long long)x * D + 4 * t4, o, 1.f / l);
+  s_o[tid] = o;
+  if (t4 == 0) s_ml[unit] = make_float2(m, l);
+  __syncthreads();
+  if (slice || pieces == 1 || x != x_own) return;              // (one piece: the output is there)
+  for (int i = 1; i < S; ++i) m = fmaxf(m, s_ml[unit + i].x);
+  float sum = 0.f;
+  o = at_f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < S; ++i) {
+    const float2 ml = s_ml[unit + i];
+    const at_f32x4_t y = s_o[tid + i * TL];
+    const float f = factor(ml.x, ml.y, m);
+    sum = fmaf(ml.y, f, sum);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], f, o[e]);
+  }
+  store4(reinterpret_cast<OT*>(a.out) + (long long)x * D + 4 * t4, o, 1.f / sum);
 }
 
-#ifndef TW
-#define TW 512
-#endif
-#ifndef TN
-#define TN 384
-#endif
-#ifndef TMIN
-#define TMIN 256
-#endif
-// Blocks of columns of a workgroup, workgroups of a head side by side, rows per piece, most pieces, pieces of the grid.
-struct TreePlan { int wc, groups, chunk_rows, max_chunks, slots; };       // wc = 0: tree_narrow_kernel
-static TreePlan tree_plan(const Dims& dm, const madakv_config& c, int T, int longest_rows) {
+// Which kernel, and how heads are cut.  All times: bf16 rows, heads of 128 dims, unless they say otherwise.
+//  - Narrow, where the columns of a head are at most two blocks of 32, or where there is little to do at all (columns * rows up to 2^23: 16 nodes of 28/4 heads
+//    of 2048 rows 13.5 us, by the wide kernel 14.4; 64 nodes of 32/8 heads of 4096 rows 20.5 and 28.3; but 32 nodes of 4 x 32/8 heads of 16384 rows 104 and 75).
+//  - As many pieces as there are workgroups at once: even heads one workgroup per compute unit (8 waves of 128 columns' worth, or 4 with all the loads that memory
+//    needs: 128 heads of 16384 rows 185 us, with two 193, with one and a half 200); 4-bit rows, bound by their conversion, two (64 heads of 8192 rows 24.0 us,
+//    with one 26.3).  Uneven heads make half a piece more each, and XCDs do not get the same: 448 of 512 (128 heads of 2048 rows in 8 bits 20.0 us; 512: 24.3; 320: 22.5).
+//  - But a piece costs its partial results, too: with n pieces per head 0.06 ns * columns * rows / n of arithmetic, 0.17 ns * columns * heads * n of traffic, and some
+//    tiles of latency whatever it has.  Least at rows per piece = sqrt(3 * rows * heads); measured between 1.4 (32 heads of 2048 rows, 4 nodes 14.8 us; 4 x 32/8
+//    heads, 16 nodes 21.8), 2 (12.9; 17.5) and 2.8 (13.0; 17.8, but 28/4 heads, 16 nodes 15.1 instead of 14.4).
+//  - Up to 512 rows one piece, whose results need no second launch (8 heads of 256 rows 7.7 us, in two pieces 10.2).
+constexpr double TREE_LITTLE = 8388608.;
+constexpr int TREE_ONE_PIECE = 512, TREE_LEAST_ROWS = 128;
+struct TreePlan { int wc, groups, chunk_rows, max_chunks, slots; };       // blocks of columns of a workgroup (0: tree_narrow_kernel), column groups, rows per piece, most pieces, pieces of the grid
+static TreePlan tree_plan(const Dims& dm, const madakv_config& c, int T, bool even, int longest_rows) {
   TreePlan p;
   const int R = dm.G * T;
-  p.wc = R <= 32 ? (c.dtype == MADAKV_BF16 ? 0 : 1) : R <= 64 ? 2 : 4;
-  p.groups = p.wc ? (R + 32 * p.wc - 1) / (32 * p.wc) : 1;
   const long long typical = std::min(c.budget, c.ctx_len);
-  const long long want = std::max<long long>(1, (p.wc ? TW : TN) / ((long long)dm.heads * p.groups));
-  p.chunk_rows = (int)std::max<long long>(TMIN, (typical / want + ATT_TILE - 1) / ATT_TILE * ATT_TILE);
+  if (c.dtype != MADAKV_BF16) p.wc = R <= 32 ? 1 : 4;
+  else p.wc = R <= 64 || (double)dm.heads * R * typical <= TREE_LITTLE ? 0 : R <= 128 ? 4 : 8;
+  p.groups = p.wc ? (R + 32 * p.wc - 1) / (32 * p.wc) : (R + 31) / 32;
+  const int resident = p.wc == 8 || (even && !(p.wc == 0 && c.cache_fp8 == CACHE_E2M1)) ? 256 : even || p.wc ? 512 : 448;
+  double want = (double)resident / ((double)dm.heads * p.groups);         // pieces per head
+  if (want >= 2) want = std::floor(want);
+  const double each = want < 1 ? 2. * typical : typical / (want - 0.375); // (cut_of: an eighth more than `want` of these is still `want`)
+  const double worth = typical <= TREE_ONE_PIECE ? TREE_ONE_PIECE : std::max<double>(TREE_LEAST_ROWS, std::sqrt(2. * typical * dm.heads));
+  p.chunk_rows = (int)std::ceil(std::max(each, worth));
   p.max_chunks = (int)((std::max(2, c.hcc_rho) * typical + p.chunk_rows - 1) / p.chunk_rows);
   const int longest = std::max(1, std::min(longest_rows, c.ctx_len + c.max_new_tokens));
-  p.slots = std::min(p.max_chunks, (longest + p.chunk_rows - 1) / p.chunk_rows);
+  p.slots = std::min(p.max_chunks, std::max(1, (longest - p.chunk_rows / 8 + p.chunk_rows - 1) / p.chunk_rows));      // (see cut_of)
   return p;
 }
+// All heads about as long as the typical one?
+static bool even_heads(const madakv_config& c, int longest_rows) { return longest_rows <= std::min(c.budget, c.ctx_len) + std::min(c.budget, c.ctx_len) / 8; }
 size_t tree_ws_bytes(const Dims& dm, const madakv_config& c, int T, int longest_rows) {
-  const TreePlan p = tree_plan(dm, c, T, longest_rows);
-  return p.slots == 1 ? 16 : (size_t)dm.heads * p.slots * dm.G * T * (dm.d + 2) * sizeof(float);
+  const int typical = std::min(c.budget, c.ctx_len);
+  const int slots = std::max(tree_plan(dm, c, T, false, longest_rows).slots, tree_plan(dm, c, T, true, typical + typical / 8).slots);
+  return slots == 1 ? 16 : (size_t)dm.heads * slots * dm.G * T * (dm.d + 2) * sizeof(float);
 }
 
 template <typename T, typename OT, int CACHE, int D>
 static hipError_t launch_tree(const Dims& dm, const TreeArgs& a, const TreePlan& p, hipStream_t st) {
   const dim3 grid(dm.heads * p.groups, p.slots);
-  if (p.wc == 0) { if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((tree_narrow_kernel<OT, CACHE, D>), grid, dim3(256), 0, st, a); }
-  else if (p.wc == 1) { if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 1>), grid, dim3(128), 0, st, a); }
-  else if (p.wc == 2) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 2>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 4>), grid, dim3(512), 0, st, a);
+  if (p.wc == 0) { if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((tree_narrow_kernel<OT, CACHE, D>), dim3(dm.heads, p.slots * p.groups), dim3(256), 0, st, a); }
+  else if (p.wc == 1) { if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 1, 2>), grid, dim3(128), 0, st, a); }
+  else if (p.wc == 4) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 4, 1>), grid, dim3(256), 0, st, a);
+  else if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 8, 1>), grid, dim3(512), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots == 1) return e;
-  const int n = dm.heads * a.R, per = 256 / (D / 4);
-  hipLaunchKernelGGL((tree_join_kernel<OT, D>), dim3((n + per - 1) / per), dim3(256), 0, st, a, n);
+  constexpr int UNITS = 256 / (D / 4);
+  int shift = 0;
+  while (2 << shift <= UNITS && 8 << shift < p.slots) ++shift;
+  const int n = dm.heads * a.R, per = UNITS >> shift;
+  hipLaunchKernelGGL((tree_join_kernel<OT, D>), dim3((n + per - 1) / per), dim3(256), 0, st, a, n, shift);
   return hipGetLastError();
 }
 template <typename T, typename OT, int CACHE>
@@ -683,7 +758,7 @@ static hipError_t launch_tree_o(const Dims& dm, const madakv_config& c, const Tr
 hipError_t launch_tree_attn(const Dims& dm, const madakv_config& c, int T, const void* q, const void* k_new, const void* v_new, const void* tree, const void* k_c,
                             const void* v_c, const int64_t* kv_off, const int32_t* kv_len, void* out, void* ws, long long capacity_tokens, int longest_rows,
                             const Paging& pg, int layer0, hipStream_t st) {
-  const TreePlan p = tree_plan(dm, c, T, longest_rows);
+  const TreePlan p = tree_plan(dm, c, T, even_heads(c, longest_rows), longest_rows);
   const long long head0 = (long long)layer0 * dm.B * dm.H;
   TreeArgs a;
   a.q = q; a.k_new = k_new; a.v_new = v_new; a.k_c = static_cast<const unsigned char*>(k_c); a.v_c = static_cast<const unsigned char*>(v_c);

@@ -139,5 +139,5 @@ log()
 assert tree(h) == 0 and grid() == room != short
 assert tree(h, l0=1) == 0 and grid() == short
 print("ok")
-""", good(n_q_heads=1, n_kv_heads=1, budget=100, max_new_tokens=1000))
+""", good(n_q_heads=1, n_kv_heads=1, ctx_len=2048, budget=1000, max_new_tokens=1000))
     assert out.strip() == "ok"
