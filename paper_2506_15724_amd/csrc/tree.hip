@@ -792,15 +792,20 @@ struct CommitArgs {
   long long region_pages;
 };
 
+// What it takes is a chain of waits (lengths and places, the nodes, their rows) and the bytes: 6 of 16 nodes of 32 layers of 4 x 32 heads, 8-bit rows, 6.6 us by
+// workgroups of 128 threads, all resident at once (256: 7.4; and 7.9 where every entry is asked for only when it is needed).  One layer of 4 heads: 2.8 us.
+constexpr int COMMIT_THREADS = 128;
 template <typename T, int CACHE, int D>
-__global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
+__global__ __launch_bounds__(COMMIT_THREADS) void tree_commit_kernel(CommitArgs a) {
   constexpr int EPL = 16 / (int)sizeof(T), LPR = D / EPL;      // elements per thread, threads per row
   __shared__ int s_path[64];
   const int tid = threadIdx.x;
   const long long hidx = blockIdx.x;
   const int b = (int)(hidx / a.H % a.B);
-  const int kept = a.len1[hidx] - 1, len = a.kv_len[hidx], from = a.start[b];
+  // (everything that the rows' places depend on is sent for at once: the kernel is a chain of waits)
+  const int kept = a.len1[hidx] - 1, len = a.kv_len[hidx], from = a.start[b], named = a.n_path[b], lane = tid & 63;
   const long long off = a.kv_off[hidx];
+  const int step_node = a.path[b * a.max_path + min(lane, a.max_path - 1)];
   if (kept <= 0 || len <= 0) return;                           // never evicted, or an empty segment, which stays empty
   const int have = len - kept;
   if (from < 0 || from > have || (a.page_rows && from != have)) {
@@ -808,10 +813,9 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
     if (!a.page_rows && have > a.most && tid == 0) a.kv_len[hidx] = kept + a.most;
     return;
   }
-  int n = max(0, min(min(a.n_path[b], a.max_path), a.most - from));
+  int n = max(0, min(min(named, a.max_path), a.most - from));
   {                                                            // (every wave for itself: an entry that is no node ends the path)
-    const int lane = tid & 63;
-    const int node = lane < n ? a.path[b * a.max_path + lane] : 0;
+    const int node = lane < n ? step_node : 0;
     const unsigned long long bad = __builtin_amdgcn_ballot_w64(lane < n && (node < 0 || node >= a.T));
     if (bad) n = min(n, (int)__builtin_ctzll(bad));
     if (tid < 64) s_path[tid] = node;
@@ -831,7 +835,7 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
     }
   }
   __syncthreads();
-  for (int i = tid; i < n * 2 * LPR; i += 256) {
+  for (int i = tid; i < n * 2 * LPR; i += COMMIT_THREADS) {
     const int which = i / LPR & 1, piece = i % LPR, step = i / (2 * LPR);
     const unsigned char* src = (which ? a.v_new : a.k_new) + ((hidx * a.T + s_path[step]) * D + piece * EPL) * (long long)sizeof(T);
     const uint4 x = *reinterpret_cast<const uint4*>(src);
@@ -854,8 +858,8 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitArgs a) {
 
 template <typename T, int CACHE>
 static hipError_t launch_commit(const Dims& dm, const CommitArgs& a, hipStream_t st) {
-  if (dm.d == 128) hipLaunchKernelGGL((tree_commit_kernel<T, CACHE, 128>), dim3(dm.heads), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((tree_commit_kernel<T, CACHE, 64>), dim3(dm.heads), dim3(256), 0, st, a);
+  if (dm.d == 128) hipLaunchKernelGGL((tree_commit_kernel<T, CACHE, 128>), dim3(dm.heads), dim3(COMMIT_THREADS), 0, st, a);
+  else hipLaunchKernelGGL((tree_commit_kernel<T, CACHE, 64>), dim3(dm.heads), dim3(COMMIT_THREADS), 0, st, a);
   return hipGetLastError();
 }
 hipError_t launch_tree_commit(const Dims& dm, const madakv_config& c, int T, const void* k_new, const void* v_new, const int32_t* path, const int32_t* n_path, int max_path,

@@ -106,6 +106,26 @@ def test_attention(T, lens, d, Hq, P, kind):
             assert torch.equal(out, attend(eng, q, k, v, tree)), "the same twice"
 
 
+WIDE = [(33, [40, 500], 128, 4, 0), (64, [63, 65], 64, 16, 0), (64, [1000, 100], 128, 14, 0), (31, [300, 17], 128, 16, 32), (13, [700], 128, 7, 16), (40, [77, 50, 9], 64, 9, 0),
+        (25, [8, 64, 128, 640], 128, 12, 0), (43, [900, 33], 64, 6, 64), (64, [31, 2000], 128, 16, 0)]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "fp4"])
+@pytest.mark.parametrize("T,lens,d,Hq,P", WIDE)
+def test_attention_of_many_columns(T, lens, d, Hq, P, kind):
+    """Caches with room for so many rows that launches take the kernel for many columns."""
+    for out_fp32 in (1, 0):
+        say(f"many columns T={T} lens={lens} d={d} Hq={Hq} P={P} {kind} out_fp32={out_fp32}")
+        L = (1 << 23) // (Hq * T) + 1016
+        eng, args, *_ = make(lens, n_q_heads=Hq, n_kv_heads=len(lens), head_dim=d, ctx_len=L, budget=L - 16, page_rows=P, out_fp32=out_fp32, **KINDS[kind])
+        q, k, v = nodes(eng, T, T)
+        for how in ("tree", "any", "chain"):
+            tree = some_tree(1, T, T, how)
+            out = attend(eng, q, k, v, tree)
+            check(eng, args, q, k, v, tree, out)
+            assert torch.equal(out, attend(eng, q, k, v, tree)), "the same twice"
+
+
 @pytest.mark.parametrize("kind", list(KINDS))
 @pytest.mark.parametrize("B,NL,H,Hq,d,L,T", [(2, 3, 4, 8, 64, 300, 9), (4, 2, 32, 32, 128, 257, 6), (1, 1, 2, 14, 128, 5000, 20), (3, 1, 1, 8, 64, 2500, 64)])
 def test_whole_caches(B, NL, H, Hq, d, L, T, kind):
@@ -213,6 +233,30 @@ def test_commit(kind, d):
     commit([9, 9, 9, 9], [0, 0, 0, 0], 20)
     commit([9, 9, 9, 9], [9, 9, 9, 9], 20)
     commit([9, 9, 9, 9], [18, 18, 18, 18], 20)
+
+
+@pytest.mark.parametrize("kind", ["fp8", "fp4"])
+def test_commit_encodes_every_value(kind):
+    """All 65536 16-bit patterns, infinities and NaN among them: the bytes that decode steps would append."""
+    say(f"every value {kind}")
+    kw = dict(n_q_heads=8, n_kv_heads=8, head_dim=128, ctx_len=70, max_new_tokens=64, **KINDS[kind])
+    (eng, *_), (one, *_) = make(None, **kw), make(None, **kw)
+    x = torch.arange(65536, dtype=torch.int32).to(torch.uint16).view(torch.bfloat16).view(1, 1, 8, 64, 128).to(DEV)
+    y = x.flip(-1).contiguous()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)      # noqa: E731
+    eng.tree_commit(0, 1, x, y, i32(list(range(64))), i32(64), i32(0), 64)
+    q, out = torch.zeros(1, 1, 8, 1, 128, device=DEV, dtype=torch.bfloat16), torch.zeros(1, 1, 8, 128, device=DEV)
+    for t in range(64):
+        one.decode_attn(0, 1, q, x[:, :, :, t].contiguous(), y[:, :, :, t].contiguous(), out)
+    torch.cuda.synchronize()
+    assert torch.equal(eng.kv_len, one.kv_len)
+    rows = torch.cat([int(eng.kv_off[0, 0, h]) + torch.arange(134) for h in range(8)])
+    size = 64 if kind == "fp4" else 128
+    for w in ("k_c", "v_c"):
+        a, b = (getattr(e, w).view(torch.uint8).cpu() for e in (eng, one))
+        assert torch.equal(a[:eng.capacity * size].view(-1, size)[rows], b[:eng.capacity * size].view(-1, size)[rows])
+        if kind == "fp4":
+            assert torch.equal(a[eng.capacity * size:].view(-1, 4)[rows], b[eng.capacity * size:].view(-1, 4)[rows])
 
 
 def test_commit_into_pages():
