@@ -307,13 +307,14 @@ def test_empty_segments():
 
 @pytest.mark.parametrize("kind", ["bf16", "fp32"])
 @pytest.mark.parametrize("out_fp32", [0, 1])
-def test_undefined_nodes(kind, out_fp32):
-    """Nodes that a query does not see may hold anything."""
+@pytest.mark.parametrize("T", [20, 30, 50])
+def test_undefined_nodes(kind, out_fp32, T):
+    """Nodes that a query does not see may hold anything.  (30, 50: room for so many rows that launches take the kernel for many columns.)"""
     if kind == "fp32" and not out_fp32:
         pytest.skip("32-bit outputs")
-    say(f"undefined nodes {kind} {out_fp32}")
-    eng, args, *_ = make([60, 300], n_q_heads=6, n_kv_heads=2, head_dim=128, ctx_len=400, out_fp32=out_fp32, **KINDS[kind])
-    T = 20
+    say(f"undefined nodes {kind} {out_fp32} T={T}")
+    L = 400 if T == 20 else (1 << 23) // (6 * T) + 1016
+    eng, args, *_ = make([60, 300], n_q_heads=6, n_kv_heads=2, head_dim=128, ctx_len=L, budget=180 if T == 20 else L - 16, out_fp32=out_fp32, **KINDS[kind])
     q, k, v = nodes(eng, T, 1)
     tree = some_tree(1, T, 8)
     masks = tree.cpu().numpy().view(np.uint64)[0]
@@ -373,6 +374,26 @@ def test_captured_speculation(P):
     # calls that go by what the heads hold now
     a, b = attend(eng, q, k, v, tree), attend(ref, q, k, v, tree)
     assert bool(((a - b).abs() <= 1e-5).all())
+
+
+def test_captured_call_keeps_its_workspace():
+    say("captured, then larger trees")
+    eng, args, *_ = make([1500, 900], n_q_heads=8, n_kv_heads=2, head_dim=128, ctx_len=1600)
+    small, large = nodes(eng, 4, 1), nodes(eng, 40, 2)
+    tree, wide = some_tree(1, 4, 1), some_tree(1, 40, 2)
+    want = attend(eng, *small, tree)
+    out = torch.empty_like(want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        eng.tree_attn(0, 1, *small, tree, out)
+    for _ in range(3):
+        check(eng, args, *large, wide, attend(eng, *large, wide))
+        taken = [torch.full((1 << 20,), math.nan, device=DEV) for _ in range(32)]          # (freed memory would be these)
+        out.fill_(-1)
+        g.replay()
+        torch.cuda.synchronize()
+        assert bool(((out - want).abs() <= 1e-5).all())
+        del taken
 
 
 def test_a_generation():
