@@ -280,14 +280,16 @@ __device__ __forceinline__ void merge_halves(AttnState<D>& st, float& sum, const
 // where a column has none yet, has left it far behind, or holds no number.  s: masked logits are -inf.
 template <int D>
 __device__ __forceinline__ void attn_look(AttnState<D>& st, const at_f32x16_t& s, float (&p)[16], float& t, float scale_log2) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale_log2, -st.ref));
+  t = sum16(p);
+  const bool near = both_sum(st.sum + t) < ATT_FAR;   // (the same in both lanes of a column; not: no number)
+  if (__builtin_amdgcn_ballot_w64(!near) == 0) return;
   float top = s[0];
 #pragma unroll
   for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
   top = both_max(top) * scale_log2;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale_log2, -st.ref));
-  t = sum16(p);
-  if (both_sum(st.sum + t) < ATT_FAR) return;         // (the same in both lanes of a column; not: no number)
+  if (near) return;
   if (top > -__builtin_inff()) {
     const float r = fmaxf(st.ref, top);
     const float f = st.ref == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(st.ref - r);

@@ -241,12 +241,9 @@ __global__ __launch_bounds__(PA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(W
         if (j >= j0 && j < j1) {
           float p[16], more;
           if (cut(j)) {
-            const int k32 = first_key(j);
+            const int behind = first_key(j) + 4 * half - start;          // (a key that the row sees: start <= key <= row)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int key = k32 + key_of(i, half);
-              s[i] = key <= row && key >= start ? s[i] : -__builtin_inff();
-            }
+            for (int i = 0; i < 16; ++i) s[i] = (unsigned)(behind + key_of(i, 0)) <= (unsigned)(row - start) ? s[i] : -__builtin_inff();
           }
           attn_look<D>(st, s, p, more, a.scale_log2);
           st.sum += more;
