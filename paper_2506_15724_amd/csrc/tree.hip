@@ -89,27 +89,24 @@ __device__ __forceinline__ uint32_t e4m3_of(uint32_t a, uint32_t b) {
 }
 
 // ---- more columns -----------------------------------------------------------------------------------------
-// T: Q, nodes' rows; CACHE: 0 rows of T, CACHE_E4M3, CACHE_E2M1.  WC blocks of 32 columns, WK = 2: times the two halves of a tile of 64 keys (32-bit rows, few
-// columns), otherwise a wave has the whole tile.  All waves share the tile; rows of the type of the model come straight into LDS, 8-bit and 4-bit rows
+// T: Q, nodes' rows; CACHE: 0 rows of T, CACHE_E4M3, CACHE_E2M1.  WC blocks of 32 columns, one per wave.  All waves share a tile of 64 keys; rows of the type of the model come straight into LDS, 8-bit and 4-bit rows
 // through registers, which turn them into bf16 (exactly).  Up to 256 columns in a workgroup: rows are converted once for all of them (60 nodes of 2 x 32/8 heads
 // of 16384 4-bit rows: 53 us, by workgroups of 128 columns 59).  Tiles further ahead of the products gain nothing for 8 and 4 bits (1, 2, 3: 53.8, 52.8, 53).
-template <typename T, typename OT, int CACHE, int D, int WC, int WK>
-__global__ __launch_bounds__(WC * WK * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2))) void tree_attn_kernel(TreeArgs a) {
+template <typename T, typename OT, int CACHE, int D, int WC>
+__global__ __launch_bounds__(WC * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2))) void tree_attn_kernel(TreeArgs a) {
   using Tile = AttnTile<T, D>;
   constexpr int PARTS = sizeof(T) == 2 && sizeof(OT) == 4 ? 3 : 1;
-  constexpr int NT = WC * WK * 64, COLS = WC * 32, ROWB = Tile::ROWB, PPR = Tile::PPR;
+  constexpr int NT = WC * 64, COLS = WC * 32, ROWB = Tile::ROWB, PPR = Tile::PPR;
   constexpr int EPL = CACHE == CACHE_E2M1 ? 32 : CACHE == CACHE_E4M3 ? 16 : 16 / (int)sizeof(T);      // elements of a 16-byte load
   constexpr int LPR = D / EPL;                                                                          // loads of a row
   constexpr int LPT = (ATT_TILE * LPR + NT - 1) / NT;                                                   // of a thread, per tile and tensor
   constexpr int CROWB = CACHE ? LPR * 16 : ROWB;                                                        // bytes of a cache row
   constexpr int AHEAD = CACHE == 0 && sizeof(T) == 2 && WC == 8 ? 3 : 1;       // tiles on their way: as many as LDS has room for
   constexpr int SLOTS = CACHE ? 2 : AHEAD + 1;                 // tiles of K, of V in LDS
-  constexpr int RES = WK == 1 ? 0 : COLS * (D + 4) * 4;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * SLOTS * Tile::BYTES > RES ? 2 * SLOTS * Tile::BYTES : RES];      // later the second halves' results
-  __shared__ float s_ml[COLS][2];
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * SLOTS * Tile::BYTES];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wc = wave / WK, wk = wave % WK, half = lane >> 5, col = lane & 31;
+  const int half = lane >> 5, col = lane & 31;
   const uint32_t xy = blockIdx.x + blockIdx.y;                 // the pieces of a head on different XCDs
   const int x = (int)(xy % gridDim.x), chunk = blockIdx.y;
   const long long hidx = x / a.groups;
@@ -126,7 +123,7 @@ __global__ __launch_bounds__(WC * WK * 64) __attribute__((amdgpu_waves_per_eu(si
   at.off = off; at.init_rows = 0x7fffffff; at.tbl = nullptr; at.shift = 0; at.fresh_slot = -1; at.fresh_page = 0;
   if (a.page_rows) { at.tbl = a.page_tbl + hidx * a.tbl_entries; at.shift = a.page_shift; at.init_rows = at.tbl[0] << a.page_shift; }
 
-  const int c_own = group * COLS + wc * 32 + col, c = min(c_own, a.R - 1);       // (a column without a query: the last one's once more, not stored)
+  const int c_own = group * COLS + wave * 32 + col, c = min(c_own, a.R - 1);       // (a column without a query: the last one's once more, not stored)
   typename Tile::Query q;
   Tile::load(q, reinterpret_cast<const T*>(a.q) + (hidx * a.R + c) * D, half);
   const unsigned long long mask = a.tree[(hidx / a.H % a.B) * a.T + c % a.T];
@@ -256,15 +253,9 @@ __global__ __launch_bounds__(WC * WK * 64) __attribute__((amdgpu_waves_per_eu(si
     const unsigned char* kt = lds + t % SLOTS * Tile::BYTES;
     const unsigned char* vt = kt + SLOTS * Tile::BYTES;
     const int k0 = r_begin + t * ATT_TILE;
-    if constexpr (WK == 2) {
-      if (k0 + 32 * wk >= r_end) return;
-      at_f32x16_t s = Tile::scores(kt, 32 * wk, lane, q);
-      finish(careful, k0 + 32 * wk, 32 * wk, s, vt);
-    } else {
-      at_f32x16_t s = Tile::scores(kt, 0, lane, q), s1 = Tile::scores(kt, 32, lane, q);       // (of the last row once more, past the end)
-      finish(careful, k0, 0, s, vt);
-      if (k0 + 32 < r_end) finish(careful, k0 + 32, 32, s1, vt);
-    }
+    at_f32x16_t s = Tile::scores(kt, 0, lane, q), s1 = Tile::scores(kt, 32, lane, q);       // (of the last row once more, past the end)
+    finish(careful, k0, 0, s, vt);
+    if (k0 + 32 < r_end) finish(careful, k0 + 32, 32, s1, vt);
   };
   const auto pass = [&](auto careful) {
     st.clear();
@@ -300,22 +291,7 @@ __global__ __launch_bounds__(WC * WK * 64) __attribute__((amdgpu_waves_per_eu(si
     pass(std::true_type{});
   }
 
-  // ---- the two halves of a tile's keys: the second wave of a block leaves its results in LDS, [column][D + 4]
-  float sum = both_sum(st.sum);
-  if constexpr (WK == 2) {
-    float* s_o = reinterpret_cast<float*>(lds) + wc * 32 * (D + 4);
-    if (wk) {
-      if (half == 0) { s_ml[wc * 32 + col][0] = st.ref; s_ml[wc * 32 + col][1] = sum; }
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<at_f32x4_t*>(s_o + col * (D + 4) + 32 * db + 8 * g + 4 * half) = at_f32x4_t{st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]};
-    }
-    __syncthreads();
-    if (wk) return;
-    merge_halves<D>(st, sum, s_ml[wc * 32 + col], s_o + col * (D + 4), half);
-  }
+  const float sum = both_sum(st.sum);
   if (pieces == 1) {
     store_column<OT, D>(reinterpret_cast<OT*>(a.out) + (hidx * a.R + c) * D, c == c_own, half, st.o, 1.f / sum);
   } else if (c == c_own) {
@@ -332,14 +308,16 @@ __global__ __launch_bounds__(WC * WK * 64) __attribute__((amdgpu_waves_per_eu(si
 
 // ---- up to 32 columns ------------------------------------------------------------------------------------
 // Hardly more arithmetic per byte than decode: what counts is how much is on its way.  Every wave works for itself on tiles of 32 rows, without barriers:
-// rows of 16 bits come straight into LDS tiles of the wave's own, those of 8 and 4 bits as operand A of K (a lane has one row's dims of 16 bytes at a time, and Q the
+// rows of the type of the model come straight into LDS tiles of the wave's own, those of 8 and 4 bits as operand A of K (a lane has one row's dims of 16 bytes at a time, and Q the
 // same order of dims) and through registers into an LDS tile of V.  The next tile's are sent for as soon as there is room for them: eight waves on a
-// compute unit have up to 128 KB of 16-bit rows on their way.
-template <typename OT, int CACHE, int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_narrow_kernel(TreeArgs a) {
-  using Tile = AttnTile<uint16_t, D>;
-  constexpr int NW = 4, PARTS = sizeof(OT) == 4 ? 3 : 1, ROWB = Tile::ROWB, RS = D + 4;
-  constexpr int EPL = CACHE == CACHE_E2M1 ? 32 : CACHE == CACHE_E4M3 ? 16 : 8;         // elements of a 16-byte load
+// compute unit have up to 128 KB of 16-bit rows on their way.  (32-bit rows of 128 dims: four waves; 32 heads of 8192 rows, 8 nodes, 83 us, bound by the fp32
+// matrix instructions, of whose 32 columns 8 are used; by the kernel for many columns, two waves, 392.)
+template <typename T, typename OT, int CACHE, int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2))) void tree_narrow_kernel(TreeArgs a) {
+  using Tile = AttnTile<T, D>;
+  constexpr int NW = 4, PARTS = sizeof(T) == 2 && sizeof(OT) == 4 ? 3 : 1, ROWB = Tile::ROWB, RS = D + 4;
+  constexpr int EPL = CACHE == CACHE_E2M1 ? 32 : CACHE == CACHE_E4M3 ? 16 : 16 / (int)sizeof(T);         // elements of a 16-byte load
+  constexpr int NY = CACHE ? EPL / 8 : 1;                                               // 16-byte pieces in the type of the model
   constexpr int LPR = D / EPL, CROWB = LPR * 16;                                        // loads of a row, its bytes
   constexpr int KL = LPR / 2 ? LPR / 2 : 1, VL = LPR / 2 ? LPR / 2 : 1;                 // loads of a lane per tile: K, V
   static_assert(LPR >= 2, "both lanes of a row have something of it");
@@ -364,11 +342,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   at.off = off; at.init_rows = 0x7fffffff; at.tbl = nullptr; at.shift = 0; at.fresh_slot = -1; at.fresh_page = 0;
   if (a.page_rows) { at.tbl = a.page_tbl + (long long)x * a.tbl_entries; at.shift = a.page_shift; at.init_rows = at.tbl[0] << a.page_shift; }
   const int c = c0 + min(col, n_cols - 1);                     // (a column without a query: the last one's once more, not stored)
-  // the query: for step i EPL / 8 + e dims [(2 i + half) EPL + 8 e, + 8)
+  // the query; of 8-bit and 4-bit rows for step i NY + e dims [(2 i + half) EPL + 8 e, + 8)
   typename Tile::Query q;
-  const auto dim_of = [&](int ks) { return (2 * (ks / (EPL / 8)) + half) * EPL + 8 * (ks % (EPL / 8)); };
+  const auto dim_of = [&](int ks) { return (2 * (ks / NY) + half) * EPL + 8 * (ks % NY); };
   {
-    const uint16_t* qr = reinterpret_cast<const uint16_t*>(a.q) + ((long long)x * a.R + c) * D;
+    const T* qr = reinterpret_cast<const T*>(a.q) + ((long long)x * a.R + c) * D;
     if constexpr (CACHE == 0) {
       Tile::load(q, qr, half);
     } else {
@@ -429,36 +407,34 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane((int)(lds_v + (v ? 0u : (uint32_t)TILEB) + j * 1024u))), "v"((lr & 15) * ROWB + s), "s"(same));
     }
   };
-  // 16 bytes of a cache row -> EPL bf16
-  const auto unpack = [&](const uint4& z, uint32_t scale, uint4 (&y)[EPL / 8]) {
+  // 16 bytes of an 8-bit or 4-bit row -> EPL bf16
+  const auto unpack = [&](const uint4& z, uint32_t scale, uint4 (&y)[NY]) {
     if constexpr (CACHE == CACHE_E2M1) {
       y[0] = mx_decode8(z.x, scale); y[1] = mx_decode8(z.y, scale); y[2] = mx_decode8(z.z, scale); y[3] = mx_decode8(z.w, scale);
     } else if constexpr (CACHE == CACHE_E4M3) {
       const uint2 e0 = from_e4m3(z.x), e1 = from_e4m3(z.y), e2 = from_e4m3(z.z), e3 = from_e4m3(z.w);
       y[0] = make_uint4(e0.x, e0.y, e1.x, e1.y); y[1] = make_uint4(e2.x, e2.y, e3.x, e3.y);
-    } else {
-      y[0] = z;
     }
   };
   // EPL elements of a node's row, with the values that the cache would give them
-  const auto node_part = [&](const void* nodes, int node, int piece, uint4 (&y)[EPL / 8]) {
-    const uint4* from = reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(nodes) + ((long long)x * a.T + min(node, a.T - 1)) * D + piece * EPL);
+  const auto node_part = [&](const void* nodes, int node, int piece, uint4 (&y)[NY]) {
+    const uint4* from = reinterpret_cast<const uint4*>(reinterpret_cast<const unsigned char*>(nodes) + ((long long)x * a.T + min(node, a.T - 1)) * ROWB) + piece * NY;
 #pragma unroll
-    for (int i = 0; i < EPL / 8; ++i) y[i] = from[i];
+    for (int i = 0; i < NY; ++i) y[i] = from[i];
     if constexpr (CACHE == CACHE_E2M1) {
       as_mx4(y);
     } else if constexpr (CACHE == CACHE_E4M3) {
 #pragma unroll
-      for (int i = 0; i < EPL / 8; ++i) {
+      for (int i = 0; i < NY; ++i) {
         const uint2 lo = from_e4m3(e4m3_of(y[i].x, y[i].y)), hi = from_e4m3(e4m3_of(y[i].z, y[i].w));
         y[i] = make_uint4(lo.x, lo.y, hi.x, hi.y);
       }
     }
   };
-  const auto park = [&](int j, const uint4 (&y)[EPL / 8]) {    // piece j of the lane's V
+  const auto park = [&](int j, const uint4 (&y)[NY]) {         // piece j of the lane's V
     const int p = j * 64 + lane, lr = p / LPR;
 #pragma unroll
-    for (int i = 0; i < EPL / 8; ++i) *reinterpret_cast<uint4*>(vt + lr * ROWB + Tile::v_slot(lr, p % LPR * (EPL / 8) + i) * 16) = y[i];
+    for (int i = 0; i < NY; ++i) *reinterpret_cast<uint4*>(vt + lr * ROWB + Tile::v_slot(lr, p % LPR * NY + i) * 16) = y[i];
   };
   AttnState<D> st;
   // (the tile that its lanes have written, read with another lane mapping: same wave, in order)
@@ -540,16 +516,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         s = zero16();
 #pragma unroll
         for (int i = 0; i < KL; ++i) {
-          uint4 y[EPL / 8];
+          uint4 y[NY];
           unpack(raw.k[i], raw.ks[i], y);
 #pragma unroll
-          for (int e = 0; e < EPL / 8; ++e) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(at_bf16x8_t, y[e]), q.x[i * (EPL / 8) + e], s, 0, 0, 0);
+          for (int e = 0; e < NY; ++e) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(at_bf16x8_t, y[e]), q.x[i * NY + e], s, 0, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
         load_k(there, next);
 #pragma unroll
         for (int j = 0; j < VL; ++j) {
-          uint4 y[EPL / 8];
+          uint4 y[NY];
           unpack(raw.v[j], raw.vs[j], y);
           park(j, y);
         }
@@ -565,17 +541,30 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll 1
     for (int t = 0; t < node_tiles; ++t) {
       if ((row_tiles + t) % NW != wave) continue;
-      at_f32x16_t s = zero16();
+      at_f32x16_t s;
+      if constexpr (CACHE == 0) {
 #pragma unroll
-      for (int i = 0; i < KL; ++i) {
-        uint4 y[EPL / 8];
-        node_part(a.k_new, 32 * t + col, CACHE ? 2 * i + half : half * KL + i, y);
+        for (int j = 0; j < VL; ++j) {
+          const int p = j * 64 + lane, lr = p / LPR;
+          uint4 y[1];
+          node_part(a.k_new, 32 * t + lr, p % LPR, y);
+          *reinterpret_cast<uint4*>(kt + lr * ROWB + Tile::k_slot(lr, p % LPR) * 16) = y[0];
+        }
+        settle();
+        s = Tile::scores(kt, 0, lane, q);
+      } else {
+        s = zero16();
 #pragma unroll
-        for (int e = 0; e < EPL / 8; ++e) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(at_bf16x8_t, y[e]), q.x[i * (EPL / 8) + e], s, 0, 0, 0);
+        for (int i = 0; i < KL; ++i) {
+          uint4 y[NY];
+          node_part(a.k_new, 32 * t + col, 2 * i + half, y);
+#pragma unroll
+          for (int e = 0; e < NY; ++e) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(at_bf16x8_t, y[e]), q.x[i * NY + e], s, 0, 0, 0);
+        }
       }
 #pragma unroll
       for (int j = 0; j < VL; ++j) {
-        uint4 y[EPL / 8];
+        uint4 y[NY];
         node_part(a.v_new, 32 * t + (j * 64 + lane) / LPR, (j * 64 + lane) % LPR, y);
         park(j, y);
       }
@@ -709,10 +698,10 @@ static TreePlan tree_plan(const Dims& dm, const madakv_config& c, int T, bool ev
   TreePlan p;
   const int R = dm.G * T;
   const long long typical = std::min(c.budget, c.ctx_len);
-  if (c.dtype != MADAKV_BF16) p.wc = R <= 32 ? 1 : 4;
-  else p.wc = R <= 64 || (double)dm.heads * R * typical <= TREE_LITTLE ? 0 : R <= 128 ? 4 : 8;
+  p.wc = R <= 64 || (double)dm.heads * R * typical <= TREE_LITTLE ? 0 : R <= 128 || c.dtype != MADAKV_BF16 ? 4 : 8;
   p.groups = p.wc ? (R + 32 * p.wc - 1) / (32 * p.wc) : (R + 31) / 32;
-  const int resident = p.wc == 8 || (even && !(p.wc == 0 && c.cache_fp8 == CACHE_E2M1)) ? 256 : even || p.wc ? 512 : 448;
+  const bool large = c.dtype != MADAKV_BF16 && dm.d == 128;              // (rows of 512 bytes: LDS has room for one workgroup)
+  const int resident = large || p.wc == 8 || (even && !(p.wc == 0 && c.cache_fp8 == CACHE_E2M1)) ? 256 : even || p.wc ? 512 : 448;
   double want = (double)resident / ((double)dm.heads * p.groups);         // pieces per head
   if (want >= 2) want = std::floor(want);
   const double each = want < 1 ? 2. * typical : typical / (want - 0.375); // (cut_of: an eighth more than `want` of these is still `want`)
@@ -734,10 +723,9 @@ size_t tree_ws_bytes(const Dims& dm, const madakv_config& c, int T, int longest_
 template <typename T, typename OT, int CACHE, int D>
 static hipError_t launch_tree(const Dims& dm, const TreeArgs& a, const TreePlan& p, hipStream_t st) {
   const dim3 grid(dm.heads * p.groups, p.slots);
-  if (p.wc == 0) { if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((tree_narrow_kernel<OT, CACHE, D>), dim3(dm.heads, p.slots * p.groups), dim3(256), 0, st, a); }
-  else if (p.wc == 1) { if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 1, 2>), grid, dim3(128), 0, st, a); }
-  else if (p.wc == 4) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 4, 1>), grid, dim3(256), 0, st, a);
-  else if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 8, 1>), grid, dim3(512), 0, st, a);
+  if (p.wc == 0) hipLaunchKernelGGL((tree_narrow_kernel<T, OT, CACHE, D>), dim3(dm.heads, p.slots * p.groups), dim3(256), 0, st, a);
+  else if (p.wc == 4) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 4>), grid, dim3(256), 0, st, a);
+  else if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((tree_attn_kernel<T, OT, CACHE, D, 8>), grid, dim3(512), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots == 1) return e;
   constexpr int UNITS = 256 / (D / 4);
