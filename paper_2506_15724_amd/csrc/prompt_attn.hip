@@ -7,6 +7,9 @@
 // causal mask and the starts of sequences are looked at in the tiles that they cut, where keys that no row may see count for nothing
 // whatever they hold: an infinite or undefined element of V, which zero weights would not keep out of a matrix product, is found by what it
 // does to the output, and the workgroup goes over its keys a second time, adding the rows of V of such tiles one by one.
+// Work: 4 D operations per query head, row and key it sees; bytes do not count (28/4 heads of 16384 rows: 1.9 TFLOP, 270 MB).  Bound by power there: 1.09-1.14 PFLOP/s
+// (1.69-1.79 ms) with the matrix unit busy 62% of the time at 1.7 GHz, 1.35 of the same code on zeros.  Short prompts are bound by what every workgroup has at its beginning,
+// on the diagonal and at its end: 4 x 32/8 heads of 2048 rows 150 us (0.91 PFLOP/s), 32/8 of 1024 20.
 #include "attn_tile.h"
 
 #include <algorithm>
@@ -297,10 +300,11 @@ static hipError_t launch_rows(PromptAttnArgs& a, int heads, hipStream_t st) {
 template <typename T, typename OT, int D>
 static hipError_t launch_pa(PromptAttnArgs& a, int heads, hipStream_t st) {
   const long long blocks = (long long)heads * ((a.L + 127) / 128);
-  constexpr int WAVES = sizeof(T) == 2 ? 2 : 1;
-  if (blocks <= 512) return launch_rows<T, OT, D, 2, WAVES>(a, heads, st);
-  if constexpr (sizeof(T) == 2 && D == 64) if (blocks > 1536) return launch_rows<T, OT, D, 1, 3>(a, heads, st);
-  return launch_rows<T, OT, D, 1, WAVES>(a, heads, st);
+  // Few blocks: two waves share 32 rows and take half of the keys each, so that the longest rows take half as long (us, 32 rows per wave / shared: 128 blocks of
+  // 2048 positions 38.3 / 28.7, 256 of 1024 24.8 / 21.5; 448 of 2048 47.4 / 49.2, 512 of 2048 50.4 / 54.7, 1024 of 64 dims 325 / 376).
+  if (blocks <= 384) return launch_rows<T, OT, D, 2, sizeof(T) == 2 ? 2 : 1>(a, heads, st);
+  // Waves of 64 dims are bound by the exponentials: three per SIMD (two: 1024 blocks 325 instead of 307, 1504 173 and 166, 3584 1032 and 974).
+  return launch_rows<T, OT, D, 1, sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2>(a, heads, st);
 }
 hipError_t launch_prompt_attn(const Dims& dm, const madakv_config& c, const void* q, const void* k, const void* v, const int32_t* seq_off, int n_seq,
                               void* out, float* row_lse, hipStream_t st) {
