@@ -692,7 +692,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int n_column
 //    heads, 16 nodes 21.8), 2 (12.9; 17.5) and 2.8 (13.0; 17.8, but 28/4 heads, 16 nodes 15.1 instead of 14.4).
 //  - Up to 512 rows one piece, whose results need no second launch (8 heads of 256 rows 7.7 us, in two pieces 10.2).
 constexpr double TREE_LITTLE = 8388608.;
-constexpr int TREE_ONE_PIECE = 512, TREE_LEAST_ROWS = 128;
+constexpr int TREE_ONE_PIECE = 512, TREE_LEAST_ROWS = 128, TREE_MOST_PIECES = 512;       // (more pieces of a head than the chip takes at once only cost room)
 struct TreePlan { int wc, groups, chunk_rows, max_chunks, slots; };       // blocks of columns of a workgroup (0: tree_narrow_kernel), column groups, rows per piece, most pieces, pieces of the grid
 static TreePlan tree_plan(const Dims& dm, const madakv_config& c, int T, bool even, int longest_rows) {
   TreePlan p;
@@ -707,7 +707,7 @@ static TreePlan tree_plan(const Dims& dm, const madakv_config& c, int T, bool ev
   const double each = want < 1 ? 2. * typical : typical / (want - 0.375); // (cut_of: an eighth more than `want` of these is still `want`)
   const double worth = typical <= TREE_ONE_PIECE ? TREE_ONE_PIECE : std::max<double>(TREE_LEAST_ROWS, std::sqrt(2. * typical * dm.heads));
   p.chunk_rows = (int)std::ceil(std::max(each, worth));
-  p.max_chunks = (int)((std::max(2, c.hcc_rho) * typical + p.chunk_rows - 1) / p.chunk_rows);
+  p.max_chunks = (int)std::min<long long>(TREE_MOST_PIECES, (std::max(2, c.hcc_rho) * typical + p.chunk_rows - 1) / p.chunk_rows);
   const int longest = std::max(1, std::min(longest_rows, c.ctx_len + c.max_new_tokens));
   p.slots = std::min(p.max_chunks, std::max(1, (longest - p.chunk_rows / 8 + p.chunk_rows - 1) / p.chunk_rows));      // (see cut_of)
   return p;

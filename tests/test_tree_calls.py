@@ -141,3 +141,16 @@ assert tree(h, l0=1) == 0 and grid() == short
 print("ok")
 """, good(n_q_heads=1, n_kv_heads=1, ctx_len=2048, budget=1000, max_new_tokens=1000))
     assert out.strip() == "ok"
+
+
+def test_pieces_of_lopsided_caches(runtime):  # noqa: F811
+    """Heads that may be far longer than the typical one: not more pieces than the chip takes at once."""
+    out = scenario(runtime, ARGS + """
+h = create(sys.argv[3])
+for t in (1, 8, 64):
+    assert need(h, 1, t) <= 8 * 512 * 8 * 64 * (128 + 2) * 4, need(h, 1, t)
+    log()
+    assert tree(h, t=t) == 0
+print("ok")
+""", good(n_q_heads=64, n_kv_heads=8, ctx_len=1 << 20, budget=2000, hcc_rho=1024))
+    assert out.strip() == "ok"
