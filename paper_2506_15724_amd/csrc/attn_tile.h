@@ -51,16 +51,18 @@ constexpr __device__ __forceinline__ at_f32x16_t zero16() {
 
 // How rows of D elements of T lie in LDS and enter the matrix instructions.  Rows are as long as in memory; their 16-byte pieces are
 // permuted (by an exclusive or with something of the row number), so that neither operand's reads collide in the banks.
-template <typename T, int D> struct AttnTile;
+// PARKED: V is written by threads that have two or four neighbouring pieces of a row each, whose stores would meet in the banks: rows permute the pieces of
+// every four as well.  (Rows of 4 bits gain 3-5%, of 8 bits nothing; where rows come straight into LDS prompts of 64 dims lose 3%.)
+template <typename T, int D, bool PARKED = false> struct AttnTile;
 
-template <int D> struct AttnTile<uint16_t, D> {
+template <int D, bool PARKED> struct AttnTile<uint16_t, D, PARKED> {
   static constexpr int ROWB = D * 2, PPR = D / 8, BYTES = ATT_TILE * ROWB;
   static constexpr int KS = D / 16;             // contraction steps of S^T
   static constexpr int DB = D / 32;             // blocks of 32 dims of the output
   struct Query { at_bf16x8_t x[KS]; };
   template <int PARTS> struct Weights { at_bf16x8_t part[PARTS][2]; };          // of 32 keys, as operand B
   static __device__ __forceinline__ int k_slot(int row, int piece) { return piece ^ (D == 128 ? row & 15 : row >> 1 & 7); }
-  static __device__ __forceinline__ int v_slot(int row, int piece) { return piece ^ (D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1)); }
+  static __device__ __forceinline__ int v_slot(int row, int piece) { return piece ^ (D == 128 ? 4 * (row & 3) : 4 * (row >> 1 & 1)) ^ (PARKED ? (D == 128 ? row & 3 : row >> 1 & 3) : 0); }
   // a column's query: for step ks elements [half D/2 + 8 ks, + 8)
   static __device__ __forceinline__ void load(Query& q, const uint16_t* row, int half) {
 #pragma unroll
@@ -140,7 +142,7 @@ template <int D> struct AttnTile<uint16_t, D> {
   }
 };
 
-template <int D> struct AttnTile<float, D> {
+template <int D, bool PARKED> struct AttnTile<float, D, PARKED> {
   static constexpr int ROWB = D * 4, PPR = D / 4, BYTES = ATT_TILE * ROWB;
   static constexpr int DB = D / 32;
   struct Query { float x[D / 2]; };

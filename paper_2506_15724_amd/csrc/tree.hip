@@ -7,7 +7,7 @@
 // A head is cut into pieces; each leaves its partial (reference, sum, output) in the workspace, and a second launch joins them in their order, so results
 // do not depend on who comes first.  (Joined by whoever comes last it took longer: results pass from one XCD's L2 to another's, a wait per piece.)
 // Two kernels: tree_narrow_kernel, bound by how fast rows arrive (128 heads of 16384 bf16 rows, 32 nodes: 185 us, 5.8 TB/s), and tree_attn_kernel for more columns,
-// bound by the arithmetic (60 nodes of 2 x 32/8 heads of 16384 4-bit rows: 43 of 53 us, 750 TFLOP/s; the rest is joining).  Nodes' rows count with the
+// bound by the arithmetic (60 nodes of 2 x 32/8 heads of 16384 4-bit rows: 43 of 51 us, 750 TFLOP/s, some 8 of them for 32 MB of partial results; the rest is joining).  Nodes' rows count with the
 // values that the cache would give them.  Masked keys count for nothing whatever they hold, as in prompt_attn.hip.
 #include "attn_tile.h"
 #include "decode_pieces.h"
@@ -94,7 +94,7 @@ __device__ __forceinline__ uint32_t e4m3_of(uint32_t a, uint32_t b) {
 // of 16384 4-bit rows: 53 us, by workgroups of 128 columns 59).  Tiles further ahead of the products gain nothing for 8 and 4 bits (1, 2, 3: 53.8, 52.8, 53).
 template <typename T, typename OT, int CACHE, int D, int WC>
 __global__ __launch_bounds__(WC * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2))) void tree_attn_kernel(TreeArgs a) {
-  using Tile = AttnTile<T, D>;
+  using Tile = AttnTile<T, D, CACHE != 0>;
   constexpr int PARTS = sizeof(T) == 2 && sizeof(OT) == 4 ? 3 : 1;
   constexpr int NT = WC * 64, COLS = WC * 32, ROWB = Tile::ROWB, PPR = Tile::PPR;
   constexpr int EPL = CACHE == CACHE_E2M1 ? 32 : CACHE == CACHE_E4M3 ? 16 : 16 / (int)sizeof(T);      // elements of a 16-byte load
@@ -314,7 +314,7 @@ __global__ __launch_bounds__(WC * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
 // matrix instructions, of whose 32 columns 8 are used; by the kernel for many columns, two waves, 392.)
 template <typename T, typename OT, int CACHE, int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2))) void tree_narrow_kernel(TreeArgs a) {
-  using Tile = AttnTile<T, D>;
+  using Tile = AttnTile<T, D, CACHE != 0>;
   constexpr int NW = 4, PARTS = sizeof(T) == 2 && sizeof(OT) == 4 ? 3 : 1, ROWB = Tile::ROWB, RS = D + 4;
   constexpr int EPL = CACHE == CACHE_E2M1 ? 32 : CACHE == CACHE_E4M3 ? 16 : 16 / (int)sizeof(T);         // elements of a 16-byte load
   constexpr int NY = CACHE ? EPL / 8 : 1;                                               // 16-byte pieces in the type of the model
