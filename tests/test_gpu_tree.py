@@ -110,11 +110,11 @@ WIDE = [(33, [40, 500], 128, 4, 0), (64, [63, 65], 64, 16, 0), (64, [1000, 100],
         (25, [8, 64, 128, 640], 128, 12, 0), (43, [900, 33], 64, 6, 64), (64, [31, 2000], 128, 16, 0)]
 
 
-@pytest.mark.parametrize("kind", ["bf16", "fp8", "fp4"])
+@pytest.mark.parametrize("kind", ["bf16", "fp8", "fp4", "fp32"])
 @pytest.mark.parametrize("T,lens,d,Hq,P", WIDE)
 def test_attention_of_many_columns(T, lens, d, Hq, P, kind):
     """Caches with room for so many rows that launches take the kernel for many columns."""
-    for out_fp32 in (1, 0):
+    for out_fp32 in (1,) if kind == "fp32" else (1, 0):
         say(f"many columns T={T} lens={lens} d={d} Hq={Hq} P={P} {kind} out_fp32={out_fp32}")
         L = (1 << 23) // (Hq * T) + 1016
         eng, args, *_ = make(lens, n_q_heads=Hq, n_kv_heads=len(lens), head_dim=d, ctx_len=L, budget=L - 16, page_rows=P, out_fp32=out_fp32, **KINDS[kind])
@@ -287,22 +287,23 @@ def test_commit_into_pages():
         eng.decode_attn(0, 1, q[:, :, :, 0].contiguous(), k[:, :, :, 0].contiguous(), v[:, :, :, 0].contiguous(), torch.empty(1, 1, 2, 64, device=DEV))
 
 
-def test_empty_segments():
+@pytest.mark.parametrize("N,L,T,first", [(60, 200, 5, 100), (900, 2500, 20, 1500), (59984, 60000, 40, 59980)])
+def test_empty_segments(N, L, T, first):
     """Heads that did not fit the cache stay empty, and their outputs are no numbers."""
-    say("empty segments")
-    eng, args, k0, v0, mask = make([60, 60], n_q_heads=4, n_kv_heads=2, head_dim=64, ctx_len=200)
+    say(f"empty segments {N}")
+    eng, args, k0, v0, mask = make([N, N], n_q_heads=8, n_kv_heads=2, head_dim=64, ctx_len=L)
     bud = torch.zeros(1, 1, 2, 2, dtype=torch.int32)
-    bud[..., 0] = torch.tensor([100, 60])
-    eng.select_gather(0, 1, k0, v0, mask, psi_pool=torch.rand(1, 1, 2, 192, device=DEV), budgets=bud.to(DEV))
+    bud[..., 0] = torch.tensor([first, N])
+    eng.select_gather(0, 1, k0, v0, mask, psi_pool=torch.rand(1, 1, 2, L - 8, device=DEV), budgets=bud.to(DEV))
     torch.cuda.synchronize()
-    assert eng.kv_len.view(-1).tolist() == [108, 0]
-    q, k, v = nodes(eng, 5, 1)
-    tree = some_tree(1, 5, 1)
+    assert eng.kv_len.view(-1).tolist() == [first + 8, 0]
+    q, k, v = nodes(eng, T, 1)
+    tree = some_tree(1, T, 1)
     check(eng, args, q, k, v, tree, attend(eng, q, k, v, tree))
     i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)      # noqa: E731
     eng.tree_commit(0, 1, k, v, i32([0, 1]), i32(2), i32(0), 4)
     torch.cuda.synchronize()
-    assert eng.kv_len.view(-1).tolist() == [110, 0]
+    assert eng.kv_len.view(-1).tolist() == [first + 10, 0]
 
 
 @pytest.mark.parametrize("kind", ["bf16", "fp32"])
