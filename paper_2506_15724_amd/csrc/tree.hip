@@ -25,7 +25,7 @@ struct TreeArgs {
   int B, H, G, T, R;                   // R = G * T columns
   int groups;                          // column groups of a head
   int chunk_rows, max_chunks, slots;
-  float* part; float* part_ml;         // [heads][groups][slots][columns of a group][D], [2]
+  float* part; float* part_ml;         // [heads][slots][R][D], [2]
   long long capacity;
   int page_rows, page_shift, tbl_entries;
   const int32_t* page_tbl;             // of the call's first head
@@ -684,8 +684,8 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int n_column
 // Which kernel, and how heads are cut.  All times: bf16 rows, heads of 128 dims, unless they say otherwise.
 //  - Narrow, where the columns of a head are at most two blocks of 32, or where there is little to do at all (columns * rows up to 2^23: 16 nodes of 28/4 heads
 //    of 2048 rows 13.5 us, by the wide kernel 14.4; 64 nodes of 32/8 heads of 4096 rows 20.5 and 28.3; but 32 nodes of 4 x 32/8 heads of 16384 rows 104 and 75).
-//  - As many pieces as there are workgroups at once: even heads one workgroup per compute unit (8 waves of 128 columns' worth, or 4 with all the loads that memory
-//    needs: 128 heads of 16384 rows 185 us, with two 193, with one and a half 200); 4-bit rows, bound by their conversion, two (64 heads of 8192 rows 24.0 us,
+//  - As many pieces as there are workgroups at once: even heads one workgroup per compute unit, whose four waves have all the loads on their way that memory
+//    needs (128 heads of 16384 rows 185 us, with two 193, with one and a half 200; 32 nodes of 4 x 32/8 heads of 16384 71, with two 75); 4-bit rows, bound by their conversion, two (64 heads of 8192 rows 24.0 us,
 //    with one 26.3).  Uneven heads make half a piece more each, and XCDs do not get the same: 448 of 512 (128 heads of 2048 rows in 8 bits 20.0 us; 512: 24.3; 320: 22.5).
 //  - But a piece costs its partial results, too: with n pieces per head 0.06 ns * columns * rows / n of arithmetic, 0.17 ns * columns * heads * n of traffic, and some
 //    tiles of latency whatever it has.  Least at rows per piece = sqrt(3 * rows * heads); measured between 1.4 (32 heads of 2048 rows, 4 nodes 14.8 us; 4 x 32/8
