@@ -125,6 +125,24 @@ def test_several_sequences(L, ends, Hq, H, d, kind):
     check(eng, q, k, v, *run(eng, q, k, v, off), off=off, heads=[0, Hq - 1] if Hq > 4 else None)
 
 
+@pytest.mark.parametrize("NL,B,Hq,H,L,d", [(1, 3, 16, 8, 150, 64), (2, 1, 5, 5, 70, 128), (1, 2, 28, 4, 200, 64), (1, 1, 20, 20, 2600, 64), (3, 1, 12, 2, 130, 128), (1, 4, 32, 8, 600, 64),
+                                           (1, 1, 1, 1, 1100, 64), (2, 2, 7, 1, 1000, 64), (1, 2, 24, 24, 1290, 128), (1, 1, 3, 1, 17000, 64)])
+def test_every_head(NL, B, Hq, H, L, d):
+    """All heads and blocks of rows have their workgroup, whichever way they are dealt to the XCDs; items of different lengths."""
+    say(f"every head n={NL} B={B} {Hq}/{H} L={L} d={d}")
+    eng = engine(L, Hq, H, d, B, NL, out_fp32=0)
+    q, k, v = inputs(eng, L)
+    out, lse = run(eng, q, k, v)
+    assert bool((lse != -77).all())
+    if L < 5000:
+        check(eng, q, k, v, out, lse)
+    off = torch.tensor([[L * b // (B + 1), L - b] for b in range(B)], dtype=torch.int32, device=DEV)
+    out, lse = run(eng, q, k, v, off)
+    if L < 5000:
+        check(eng, q, k, v, out, lse, off=off)
+    assert bool(((lse != -77) == torch.stack([(torch.arange(L, device=DEV) >= o[0]) & (torch.arange(L, device=DEV) < o[1]) for o in off])[None, :, None]).all())
+
+
 def test_many_short_sequences():
     L = 1500
     say("many short sequences")
