@@ -687,16 +687,20 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int n_column
 //  - As many pieces as there are workgroups at once: even heads one workgroup per compute unit, whose four waves have all the loads on their way that memory
 //    needs (128 heads of 16384 rows 185 us, with two 193, with one and a half 200; 32 nodes of 4 x 32/8 heads of 16384 71, with two 75); 4-bit rows, bound by their conversion, two (64 heads of 8192 rows 24.0 us,
 //    with one 26.3).  Uneven heads make half a piece more each, and XCDs do not get the same: 448 of 512 (128 heads of 2048 rows in 8 bits 20.0 us; 512: 24.3; 320: 22.5).
+//    Heads are even where the cache keeps everything.  (Not where the host has heard that they are: nothing here but the grid depends on what it knows of lengths, so
+//    that a call gives the same bits before and after they have reached it, and when it is replayed.)
 //  - But a piece costs its partial results, too: with n pieces per head 0.06 ns * columns * rows / n of arithmetic, 0.17 ns * columns * heads * n of traffic, and some
 //    tiles of latency whatever it has.  Least at rows per piece = sqrt(3 * rows * heads); measured between 1.4 (32 heads of 2048 rows, 4 nodes 14.8 us; 4 x 32/8
 //    heads, 16 nodes 21.8), 2 (12.9; 17.5) and 2.8 (13.0; 17.8, but 28/4 heads, 16 nodes 15.1 instead of 14.4).
 //  - Up to 512 rows one piece, whose results need no second launch (8 heads of 256 rows 7.7 us, in two pieces 10.2).
 constexpr double TREE_LITTLE = 8388608.;
 constexpr int TREE_ONE_PIECE = 512, TREE_LEAST_ROWS = 128, TREE_MOST_PIECES = 512;       // (more pieces of a head than the chip takes at once only cost room)
-struct TreePlan { int wc, groups, chunk_rows, max_chunks, slots; };       // blocks of columns of a workgroup (0: tree_narrow_kernel), column groups, rows per piece, most pieces, pieces of the grid
-static TreePlan tree_plan(const Dims& dm, const madakv_config& c, int T, bool even, int longest_rows) {
+// wc: blocks of columns of a workgroup (0: tree_narrow_kernel); usual: pieces of the longer heads, for which the join is laid out; slots: pieces of the grid
+struct TreePlan { int wc, groups, chunk_rows, max_chunks, usual, slots; };
+static TreePlan tree_plan(const Dims& dm, const madakv_config& c, int T, int longest_rows) {
   TreePlan p;
   const int R = dm.G * T;
+  const bool even = c.budget >= c.ctx_len;
   const long long typical = std::min(c.budget, c.ctx_len);
   p.wc = R <= 64 || (double)dm.heads * R * typical <= TREE_LITTLE ? 0 : R <= 128 || c.dtype != MADAKV_BF16 ? 4 : 8;
   p.groups = p.wc ? (R + 32 * p.wc - 1) / (32 * p.wc) : (R + 31) / 32;
@@ -708,15 +712,13 @@ static TreePlan tree_plan(const Dims& dm, const madakv_config& c, int T, bool ev
   const double worth = typical <= TREE_ONE_PIECE ? TREE_ONE_PIECE : std::max<double>(TREE_LEAST_ROWS, std::sqrt(2. * typical * dm.heads));
   p.chunk_rows = (int)std::ceil(std::max(each, worth));
   p.max_chunks = (int)std::min<long long>(TREE_MOST_PIECES, (std::max(2, c.hcc_rho) * typical + p.chunk_rows - 1) / p.chunk_rows);
-  const int longest = std::max(1, std::min(longest_rows, c.ctx_len + c.max_new_tokens));
-  p.slots = std::min(p.max_chunks, std::max(1, (longest - p.chunk_rows / 8 + p.chunk_rows - 1) / p.chunk_rows));      // (see cut_of)
+  const auto pieces = [&](long long rows) { return (int)std::min<long long>(p.max_chunks, std::max<long long>(1, (rows - p.chunk_rows / 8 + p.chunk_rows - 1) / p.chunk_rows)); };      // (see cut_of)
+  p.usual = pieces(even ? typical + c.max_new_tokens : 2 * typical);
+  p.slots = pieces(std::min(longest_rows, c.ctx_len + c.max_new_tokens));
   return p;
 }
-// All heads about as long as the typical one?
-static bool even_heads(const madakv_config& c, int longest_rows) { return longest_rows <= std::min(c.budget, c.ctx_len) + std::min(c.budget, c.ctx_len) / 8; }
 size_t tree_ws_bytes(const Dims& dm, const madakv_config& c, int T, int longest_rows) {
-  const int typical = std::min(c.budget, c.ctx_len);
-  const int slots = std::max(tree_plan(dm, c, T, false, longest_rows).slots, tree_plan(dm, c, T, true, typical + typical / 8).slots);
+  const int slots = tree_plan(dm, c, T, longest_rows).slots;
   return slots == 1 ? 16 : (size_t)dm.heads * slots * dm.G * T * (dm.d + 2) * sizeof(float);
 }
 
@@ -730,7 +732,7 @@ static hipError_t launch_tree(const Dims& dm, const TreeArgs& a, const TreePlan&
   if (e != hipSuccess || p.slots == 1) return e;
   constexpr int UNITS = 256 / (D / 4);
   int shift = 0;
-  while (2 << shift <= UNITS && 8 << shift < p.slots) ++shift;
+  while (2 << shift <= UNITS && 8 << shift < p.usual) ++shift;
   const int n = dm.heads * a.R, per = UNITS >> shift;
   hipLaunchKernelGGL((tree_join_kernel<OT, D>), dim3((n + per - 1) / per), dim3(256), 0, st, a, n, shift);
   return hipGetLastError();
@@ -746,7 +748,7 @@ static hipError_t launch_tree_o(const Dims& dm, const madakv_config& c, const Tr
 hipError_t launch_tree_attn(const Dims& dm, const madakv_config& c, int T, const void* q, const void* k_new, const void* v_new, const void* tree, const void* k_c,
                             const void* v_c, const int64_t* kv_off, const int32_t* kv_len, void* out, void* ws, long long capacity_tokens, int longest_rows,
                             const Paging& pg, int layer0, hipStream_t st) {
-  const TreePlan p = tree_plan(dm, c, T, even_heads(c, longest_rows), longest_rows);
+  const TreePlan p = tree_plan(dm, c, T, longest_rows);
   const long long head0 = (long long)layer0 * dm.B * dm.H;
   TreeArgs a;
   a.q = q; a.k_new = k_new; a.v_new = v_new; a.k_c = static_cast<const unsigned char*>(k_c); a.v_c = static_cast<const unsigned char*>(v_c);
