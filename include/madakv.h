@@ -385,7 +385,9 @@ int32_t madakv_tree_attn(madakv_handle* h, int32_t layer0, int32_t n, int32_t n_
  *            appended (madakv_decode_attn refuses a layer from max_new_tokens on); a caller that does not know the lengths gives an upper bound
  *   kv_len   in/out: the rows that the (re-)eviction left + start + the rows stored
  * A call repeated with the same arguments does the same again.  kept_idx has no entries for these rows until a re-eviction.  Segments that are empty, or
- * that this handle has not evicted, are left as they are. */
+ * that this handle has not evicted, are left as they are.
+ * A captured call can be replayed any number of times: `most` bounds the rows whatever the path says, and every other call covers the rows that replays may
+ * have left, those of an ordinary decode step among them. */
 int32_t madakv_tree_commit(madakv_handle* h, int32_t layer0, int32_t n, int32_t n_nodes, const void* k_new, const void* v_new,
                            const int32_t* path, const int32_t* n_path, int32_t max_path, const int32_t* start, int32_t most,
                            void* k_c, void* v_c, const int64_t* kv_off, int32_t* kv_len, void* stream);
@@ -457,8 +459,9 @@ int32_t madakv_page_table(const madakv_handle* h, const int32_t** table, int32_t
  *     row the segments have room for, so that the captured step can be replayed while the heads
  *     grow; each replay appends a row like a call would, but the library's count of appended rows
  *     only sees the capture itself: the caller must not replay beyond max_new_tokens rows per
- *     head, and takes up eager decode calls again only after a new eviction or re-eviction.  (madakv_cache_rows and
- *     madakv_reevict go by the lengths on the device and take whatever rows the replays have left.) */
+ *     head, and takes up eager decode calls again only after a new eviction or re-eviction.  (The calls themselves go by the lengths on
+ *     the device and take whatever rows the replays have left: once an appending step or a madakv_tree_commit of a layer has been captured, its launches cover
+ *     every row the segments have room for.) */
 #define MADAKV_STATIC_SCRATCH_BYTES ((size_t)8 << 20)
 int32_t madakv_decode_attn_static(madakv_handle* h, int32_t layer0, int32_t n,
                                   const void* q, const void* k_new, const void* v_new,

@@ -296,9 +296,9 @@ int32_t decode_impl(madakv_handle* h, int32_t layer0, int32_t n,
   if (k_new && (!aligned16(k_new) || !aligned16(v_new))) return MADAKV_ERR_INVALID_ARG;
   Dims dm = make_dims(h->cfg, n);
   // Under graph capture the launch is sized once and replayed while the heads grow: the grid (and the share of the
-  // workspace) then covers all the rows the segments have room for.
+  // workspace) then covers all the rows the segments have room for.  So it does for layers to which replays may have appended.
   const bool later = replayed_later(reinterpret_cast<hipStream_t>(stream));
-  const int longest = longest_rows(h, layer0, n, later);
+  const int longest = longest_rows(h, layer0, n, later, true);
   // a caller's workspace is sized for the worst case; the handle's scratch must hold what this launch uses
   if (ws_bytes != NO_WORKSPACE) {
     if (ws_bytes < (w ? weights_ws_bytes(dm, h->cfg) : decode_ws_bytes(dm, h->cfg))) return MADAKV_ERR_WORKSPACE_TOO_SMALL;
