@@ -906,8 +906,8 @@ int32_t madakv_tree_commit(madakv_handle* h, int32_t layer0, int32_t n, int32_t 
   const bool later = replayed_later(st);
   const hipError_t e = launch_tree_commit(make_dims(c, n), c, n_nodes, k_new, v_new, path, n_path, max_path, start, most, k_c, v_c, kv_off, kv_len, h->meet,
                                           region_tokens(c) * c.batch, make_paging(h), layer0, st);
-  // (rows of a paged cache are not taken back)
-  if (e == hipSuccess) for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] = c.page_rows ? std::max(h->appended[l], most) : most; h->replays[l] |= later; }
+  // (rows of a paged cache are not taken back, and a call that is only captured has taken none back yet)
+  if (e == hipSuccess) for (int l = layer0; l < layer0 + n; ++l) { h->appended[l] = c.page_rows || later ? std::max(h->appended[l], most) : most; h->replays[l] |= later; }
   return hip_fail(h, e);
 }
 

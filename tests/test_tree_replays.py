@@ -47,3 +47,24 @@ assert plain(h, new=False) == 0 and grid()[1] == room
 print("ok")
 """, good(**{**dict(n_q_heads=4, n_kv_heads=1, ctx_len=4000, budget=3000, max_new_tokens=3000, window=8), **kw}))
     assert out.strip() == "ok"
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(page_rows=16)])
+def test_a_commit_that_is_only_captured_takes_no_rows_back(runtime, kw):  # noqa: F811
+    """Three of four rows are there; a captured commit with a lower bound has not run yet, so one more fits.  A commit that is enqueued counts its bound
+    (rows of a paged cache are not taken back)."""
+    out = scenario(runtime, CALLS + """
+h, paged = create(sys.argv[3]), int(sys.argv[4])
+evict(h)
+for _ in range(3): assert plain(h) == 0
+captured(lambda: commit(h, most=1, st=st))
+assert plain(h) == 0 and plain(h) == -1
+captured(lambda: commit(h, most=1, st=st))
+assert plain(h) == -1
+assert commit(h, most=1) == 0 and plain(h) == (-1 if paged else 0)
+evict(h)
+captured(lambda: commit(h, most=3, st=st))
+assert plain(h) == 0 and plain(h) == -1
+print("ok")
+""".replace("int(sys.argv[4])", str(bool(kw))), good(**kw))
+    assert out.strip() == "ok"
