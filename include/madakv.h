@@ -319,7 +319,8 @@ int32_t madakv_evict(madakv_handle* h, int32_t layer0, int32_t n,
  *   out      [n, B, Hq, d]    float if out_fp32 else dtype
  *   ws, ws_bytes               at least what madakv_workspace_bytes reports; the partial results of heads that are cut
  *                              into several pieces go through it
- * INVALID_ARG if a layer in the range has already appended max_new_tokens rows. */
+ * INVALID_ARG if a layer in the range has already appended max_new_tokens rows.  Of rows that replays have appended the host does not know: a head
+ * whose segment is full stores nothing and attends over the rows it has. */
 int32_t madakv_decode_attn(madakv_handle* h, int32_t layer0, int32_t n,
                            const void* q, const void* k_new, const void* v_new,
                            void* k_c, void* v_c, const int64_t* kv_off, int32_t* kv_len,

@@ -64,7 +64,7 @@ __global__ __launch_bounds__(NW * 64) void decode_attn_kernel(DecodeArgs a) {
   const int arrive = arrivals(a, len1);
   if (chunk >= arrive) return;                       // the grid is the same for all heads (decode_plan)
   // an empty segment (its budgets did not fit the cache) stays empty: no append, output 0/0 = NaN
-  const bool can_append = can_append_to<PAGED>(a, off, len_old);
+  const bool can_append = can_append_to<PAGED>(a, off, len_old, len1);
   const int len = len_old + (can_append ? 1 : 0);
   const int rows = head_chunk_rows(a, len);
   const int r_begin = chunk * rows;                  // (past the head's end: no rows, the workgroup only arrives)
@@ -254,7 +254,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NB > 1 
   asm volatile("" :: "s"(len1), "s"(len_old), "s"((int)off));             // (all three in one trip)
   const int arrive = arrivals(a, len1);
   if (chunk >= arrive) return;                       // the grid is the same for all heads (decode_plan)
-  const bool can_append = can_append_to<PAGED>(a, off, len_old);
+  const bool can_append = can_append_to<PAGED>(a, off, len_old, len1);
   const int len = len_old + (can_append ? 1 : 0);
   const int rows = head_chunk_rows(a, len);
   const int r_begin = chunk * rows;

@@ -92,7 +92,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(4, 4)))
   asm volatile("" :: "s"(len1), "s"(len_old), "s"((int)off));             // (all three in one trip)
   const int arrive = arrivals(a, len1);
   if (chunk >= arrive) return;                       // the grid is the same for all heads (decode_plan)
-  const bool can_append = can_append_to<PAGED>(a, off, len_old);
+  const bool can_append = can_append_to<PAGED>(a, off, len_old, len1);
   const int len = len_old + (can_append ? 1 : 0);
   const int rows = head_chunk_rows(a, len);
   const int r_begin = chunk * rows;

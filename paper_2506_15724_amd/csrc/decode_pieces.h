@@ -137,10 +137,12 @@ struct RowMap {
   }
 };
 
+// len1: as for `arrivals` below
 template <bool PAGED>
-__device__ __forceinline__ bool can_append_to(const DecodeArgs& a, long long off, int len_old) {
-  // an empty segment (its budgets did not fit the cache) stays empty; contiguous segments also end at the cache's end
-  return a.has_new && len_old > 0 && (PAGED || off + len_old < a.capacity);
+__device__ __forceinline__ bool can_append_to(const DecodeArgs& a, long long off, int len_old, int len1) {
+  // An empty segment (its budgets did not fit the cache) stays empty; contiguous segments also end at the cache's end.  All end max_new rows
+  // behind those of the eviction: the host counts what calls append, but not what replays of a captured step or commit do.
+  return a.has_new && len_old > 0 && (PAGED || off + len_old < a.capacity) && (len1 == 0 || len_old - (len1 - 1) < a.max_new);
 }
 
 // All threads of the workgroup.  rows [r_begin, r_end) are the workgroup's; when the appended row is

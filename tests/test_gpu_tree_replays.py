@@ -83,3 +83,50 @@ def test_decode_behind_replayed_commits(Hq, H, d, P, kind):
     del graph
     for e in (eng, ref):
         e.close()
+
+
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("kind,Hq,H,d,P", [("bf16", 2, 2, 128, 0), ("bf16", 8, 2, 64, 16), ("fp32", 2, 2, 64, 0), ("fp8", 2, 2, 128, 16), ("fp8", 6, 2, 128, 0), ("fp4", 2, 2, 64, 0), ("fp4", 8, 2, 128, 32)])
+def test_steps_behind_replays_end_where_the_segments_do(kind, Hq, H, d, P, weights):
+    """Replays of a captured commit fill the room but for two rows, of which the host knows nothing: it goes on accepting steps, which store what
+    there is room for and attend over the rows there are; nothing else in the cache changes."""
+    print(f"[tree_replays] room {kind} {Hq}/{H} d={d} P={P} weights={weights}", flush=True)
+    lens, max_new, T = [100, 61], 34, 32
+    (eng, ref), args = pair(Hq, H, d, P, lens, max_new, kind)
+    for e in (eng, ref):
+        for x in (e.k_c, e.v_c):
+            x.zero_()
+        evict(e, args, 1, lens)
+    graph, k, v, path, n, start = captured_commit(eng, T, max_new)
+    for e in (eng, ref):
+        evict(e, args, 2, lens)
+    path.copy_(torch.arange(T))
+    n.fill_(T)
+    torch.cuda.synchronize()
+    graph.replay()
+    ref.tree_commit(0, 1, k, v, path, n, i32(0), T)
+    torch.cuda.synchronize()
+    acc = torch.zeros(eng.capacity, device=DEV)
+
+    def step(e, x, new=True):
+        out = torch.full(x[0].shape, -77.0, device=DEV)
+        if weights:
+            e.decode_attn_weights(0, 1, x[0], *(x[1:] if new else (None, None)), out, acc, acc)
+        else:
+            e.decode_attn(0, 1, x[0], *(x[1:] if new else (None, None)), out)
+        torch.cuda.synchronize()
+        return out
+    for i in range(12):
+        x = [y[:, :, :, 0].contiguous() for y in nodes(eng, 1, 90 + i)]
+        got, want = step(eng, x), step(ref, x, i < 2)
+        assert torch.isfinite(want).all() and torch.equal(got, want), i
+        assert torch.equal(eng.kv_len, ref.kv_len) and eng.kv_len.view(-1).tolist() == [x + min(T + i + 1, max_new) for x in lens]
+    for h in range(H):
+        a, b = row_numbers(eng, args, h), row_numbers(ref, args, h)
+        for w in ("k_c", "v_c"):
+            assert torch.equal(values(eng, args, w)[a], values(ref, args, w)[b])
+    if not P:                                            # (pages are taken in the order in which heads come)
+        assert torch.equal(eng.k_c, ref.k_c) and torch.equal(eng.v_c, ref.v_c)
+    del graph
+    for e in (eng, ref):
+        e.close()
