@@ -843,7 +843,7 @@ __global__ __launch_bounds__(COMMIT_THREADS) void tree_commit_kernel(CommitArgs 
       if ((piece & 3) == 0) cache[a.capacity * (D / 2) + row * (D / MX_BLOCK) + piece / 4] = (uint8_t)scale;
     }
   }
-  if (tid == 0) a.kv_len[hidx] = kept + from + n;
+  if (tid == 0) a.kv_len[hidx] = kept + (a.page_rows ? from + n : min(from + n, a.most));      // (a start past `most`: cut; pages are not given back)
 }
 
 template <typename T, int CACHE>
