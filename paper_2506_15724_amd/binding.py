@@ -437,16 +437,20 @@ class MadaKV:
             raise MadaKVError("madakv_score_prompt", rc)
 
     def _check_rows(self, n, rows, out, q, k, v):
-        """The arrays of a call over `rows` rows of every head; as in decode_attn_weights one expression where all are right."""
+        """The arrays of a call over `rows` rows of every head; as in decode_attn_weights one expression where all are right.  They may hold more
+        layers than the call has, but a head's rows follow each other: one that is kept for more rows has them elsewhere."""
         dt, at, nq, nkv = self.tdtype, self._device.index, n * self._out_row * rows, n * self._kv_row * rows
-        if out is not None:
-            self._check_out(out, nq)
-        if (k.dtype is not dt or k.numel() < nkv or k.get_device() != at or v.dtype is not dt or v.numel() < nkv or v.get_device() != at
-                or (out is not None and (out.get_device() != at or q.dtype is not dt or q.numel() < nq or q.get_device() != at))):
+        if (k.dtype is not dt or k.numel() != nkv or k.get_device() != at or v.dtype is not dt or v.numel() != nkv or v.get_device() != at
+                or (out is not None and (out.dtype is not self._out_dtype or out.numel() != nq or out.get_device() != at or q.dtype is not dt or q.numel() != nq or q.get_device() != at))):
+            if out is not None:
+                self._check_out(out, nq)
             self._check_array("out", out, nq, self._out_dtype)
             self._check_array("q", q, nq, dt)
             self._check_array("k", k, nkv, dt)
             self._check_array("v", v, nkv, dt)
+            for t in (q, k, v, out):
+                if t is not None and t.dim() == 5 and t.shape[3] != rows:
+                    raise ValueError(f"the call has {rows} rows per head, an array of {list(t.shape)} has {t.shape[3]}")
 
     def prompt_attn(self, l0, n, q, k, v, out, row_lse=None, seq_off=None):
         """q, out [n, B, Hq, L, d], row_lse [n, B, Hq, L].  seq_off [B, S + 1]: sequence s of a batch item has the positions seq_off[s] up to
@@ -484,7 +488,10 @@ class MadaKV:
         """q, out [n, B, Hq, T, d], k_new, v_new [n, B, H, T, d]; tree [B, T] int64: bit i of entry t: node t sees node i."""
         T = self._nodes(q)
         self._check_rows(n, T, out, q, k_new, v_new)
-        self._check_array("tree", tree, self._batch * T, torch.int64)
+        if tree.dtype is not torch.int64 or tree.numel() != self._batch * T or tree.get_device() != self._device.index:
+            self._check_array("tree", tree, self._batch * T, torch.int64)
+            if self._batch > 1 and tree.dim() == 2 and tree.shape[1] != T:
+                raise ValueError(f"tree must be [{self._batch}, {T}], got {list(tree.shape)}")
         _, ws, ws_bytes = self._tree_workspace(T)
         heads0 = l0 * self._heads
         rc = lib().madakv_tree_attn(self.h, l0, n, T, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(tree), _ptr(self.k_c), _ptr(self.v_c), _ptr(self.kv_off) + 8 * heads0,
