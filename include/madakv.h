@@ -252,7 +252,8 @@ int32_t madakv_score_prompt(madakv_handle* h, int32_t layer0, int32_t n,
  *   seq_off  [B, n_seq + 1] int32 on the device, ascending within 0 .. L, or NULL with n_seq = 0.  Sequence s of batch item b has the
  *            positions seq_off[b][s] .. seq_off[b][s + 1] - 1 (possibly none); a position sees those of its own sequence up to itself.
  *            One sequence of each item is a padded batch, several are packed prompts.  NULL: all L positions are one sequence
- *   out      [n, B, Hq, L, d]  softmax(scale * q k^T) v (float if out_fp32 else dtype)
+ *   out      [n, B, Hq, L, d]  softmax(scale * q k^T) v (float if out_fp32 else dtype).  Of bf16 outputs each weight is rounded to bf16, by up to
+ *            2^-8 of it, in front of the product with v; of float ones it is not
  *   row_lse  [n, B, Hq, L]     optional (may be NULL): natural log-sum-exp of each row, as madakv_score_prompt takes it
  * Rows of out and row_lse at positions of no sequence are left as they are, and what k and v hold where a position does not look
  * has no influence on it, whatever it is.  (A caller that has filled row_lse with +infinity has madakv_score_prompt count nothing from the queries of
@@ -363,7 +364,9 @@ int32_t madakv_decode_attn_weights(madakv_handle* h, int32_t layer0, int32_t n,
  *   n_nodes  T, 1 .. 64 (else MADAKV_ERR_BAD_SHAPE)
  *   q        [n, B, Hq, T, d]
  *   k_new, v_new [n, B, H, T, d]  the nodes' rows; they count with the values that the cache would hold of them (cache_fp8), so that a
- *            node's output is what madakv_decode_attn gives for its token behind its ancestors
+ *            node's output is what madakv_decode_attn gives for its token behind its ancestors, up to rounding: with out_fp32, and with bf16 outputs while
+ *            G * n_nodes <= 64, softmax weights have 16 bits or more, as in that call; with bf16 outputs of larger trees each may be rounded to bf16, by
+ *            up to 2^-8 of it, in front of the product with v
  *   tree     [B, T] uint64     bit i of entry t: node t sees node i (its ancestors, and as a rule itself); bits from T on mean nothing.  A node may
  *                              see none
  *   k_c, v_c, kv_off, kv_len   as in madakv_decode_attn; none of them is written

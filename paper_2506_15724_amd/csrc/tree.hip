@@ -312,10 +312,12 @@ __global__ __launch_bounds__(WC * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
 // same order of dims) and through registers into an LDS tile of V.  The next tile's are sent for as soon as there is room for them: eight waves on a
 // compute unit have up to 128 KB of 16-bit rows on their way.  (32-bit rows of 128 dims: four waves; 32 heads of 8192 rows, 8 nodes, 83 us, bound by the fp32
 // matrix instructions, of whose 32 columns 8 are used; by the kernel for many columns, two waves, 392.)
+// Weights of two bf16 numbers for bf16 outputs, so that nodes are as near to their formula as decode's tokens (8 nodes of 128 heads of 2048 rows: bf16 27.3 -> 27.5 us,
+// 8 bits 18.5 -> 19.1, 4 bits 18.4 -> 20.0; of uneven heads in 8 bits 19.8 -> 21.2).
 template <typename T, typename OT, int CACHE, int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2))) void tree_narrow_kernel(TreeArgs a) {
   using Tile = AttnTile<T, D, CACHE != 0>;
-  constexpr int NW = 4, PARTS = sizeof(T) == 2 && sizeof(OT) == 4 ? 3 : 1, ROWB = Tile::ROWB, RS = D + 4;
+  constexpr int NW = 4, PARTS = sizeof(T) == 4 ? 1 : sizeof(OT) == 4 ? 3 : 2, ROWB = Tile::ROWB, RS = D + 4;
   constexpr int EPL = CACHE == CACHE_E2M1 ? 32 : CACHE == CACHE_E4M3 ? 16 : 16 / (int)sizeof(T);         // elements of a 16-byte load
   constexpr int NY = CACHE ? EPL / 8 : 1;                                               // 16-byte pieces in the type of the model
   constexpr int LPR = D / EPL, CROWB = LPR * 16;                                        // loads of a row, its bytes
