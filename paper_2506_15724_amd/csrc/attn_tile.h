@@ -12,11 +12,15 @@
 // Logits, weights, sums and outputs are held in 32 bits.  bf16 inputs: the weights enter the second product as PARTS bf16 numbers, each of which leaves
 // up to 2^-8 of what it stands for.  Three where the output is fp32: all 24 bits.  Where the output is bf16, too: two in trees of few columns, 16 bits as in
 // decode; one, by choice, where the matrix unit is what a call waits for, in prompts and in trees of many columns.  There a rounding of up to 2^-8 of every weight,
-// independent from key to key, leaves outputs off by 0.0021-0.0023 (2-norm, of random rows) where their own rounding makes 0.0016; a second part costs 20-36% more
+// independent from key to key, leaves outputs off by 0.0021-0.0023 (2-norm, of random rows) where their own rounding makes 0.0016; a second part costs 14-37% more
 // time (prompts of 8192 positions 524 -> 713 us, 28/4 heads of 16384 1770 -> 2430; 60 nodes of 2 x 32/8 heads of 16384 4-bit rows 51.8 -> 62.8, 32 nodes of
 // 4 x 32/8 heads of bf16 ones 72 -> 83).  A caller who needs those bits has them with fp32 outputs.
 #pragma once
 #include "common.h"
+
+// The loads straight into LDS say in their clobber lists that they set m0 and write memory: the compiler sees neither of them, and may set m0 once for several
+// instructions of its own.  (It warns that m0 is a reserved register: it keeps nothing there that it would not set again.)
+#pragma clang diagnostic ignored "-Winline-asm"
 
 namespace madakv {
 

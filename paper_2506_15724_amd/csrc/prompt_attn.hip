@@ -21,7 +21,7 @@ namespace madakv {
 // 16 bytes per lane from `at` + base of a buffer to LDS address dst + 16 lane, zeros past the buffer's end.  Written out, because the compiler
 // would otherwise wait for all such loads in flight before every LDS access it sees; the loop's own waits are in `landed`.
 __device__ __forceinline__ void tile_load(at_u32x4_t buffer, uint32_t dst, int at, int base) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(dst), "v"(at), "s"(buffer), "s"(base));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(dst), "v"(at), "s"(buffer), "s"(base) : "m0", "memory");
 }
 __device__ __forceinline__ at_u32x4_t buffer_words(const void* p, int bytes) {
   const uint64_t u = reinterpret_cast<uint64_t>(p);

@@ -144,8 +144,8 @@ __global__ __launch_bounds__(WC * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
       const unsigned char* kp = (node ? kn : a.k_c) + row * ROWB + Tile::k_slot(lr, s) * 16;
       const unsigned char* vp = (node ? vn : a.v_c) + row * ROWB + Tile::v_slot(lr, s) * 16;
       const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds0 + (uint32_t)(t % SLOTS * Tile::BYTES + (wave * LPT + j) * 1024)));
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(kp));
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + SLOTS * Tile::BYTES), "v"(vp));
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(kp) : "m0", "memory");
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + SLOTS * Tile::BYTES), "v"(vp) : "m0", "memory");
     }
   };
   // ---- 8-bit and 4-bit rows: through registers
@@ -406,7 +406,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) =
         else if (2 * j >= LOADS) lr = max(lr, 16);
       }
       const uint64_t same = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane((int)(lds_v + (v ? 0u : (uint32_t)TILEB) + j * 1024u))), "v"((lr & 15) * ROWB + s), "s"(same));
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane((int)(lds_v + (v ? 0u : (uint32_t)TILEB) + j * 1024u))), "v"((lr & 15) * ROWB + s), "s"(same) : "m0", "memory");
     }
   };
   // 16 bytes of an 8-bit or 4-bit row -> EPL bf16
