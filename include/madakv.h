@@ -388,8 +388,8 @@ int32_t madakv_tree_attn(madakv_handle* h, int32_t layer0, int32_t n, int32_t n_
  *            MADAKV_ERR_INVALID_ARG): accepted rows beyond it are not stored, and contiguous segments with more rows are cut to it.  The host counts `most` rows as
  *            appended (madakv_decode_attn refuses a layer from max_new_tokens on); a caller that does not know the lengths gives an upper bound
  *   kv_len   in/out: the rows that the (re-)eviction left + start + the rows stored
- * A call repeated with the same arguments does the same again.  kept_idx has no entries for these rows until a re-eviction.  Segments that are empty, or
- * that this handle has not evicted, are left as they are.
+ * A call repeated with the same arguments does the same again.  kept_idx has no entries for these rows until a re-eviction, and their entries in the sums of
+ * madakv_decode_attn_weights are the caller's to set.  Segments that are empty, or that this handle has not evicted, are left as they are.
  * A captured call can be replayed any number of times: `most` bounds the rows whatever the path says, and every other call covers the rows that replays may
  * have left, those of an ordinary decode step among them. */
 int32_t madakv_tree_commit(madakv_handle* h, int32_t layer0, int32_t n, int32_t n_nodes, const void* k_new, const void* v_new,

@@ -7,7 +7,8 @@
 // A head is cut into pieces; each leaves its partial (reference, sum, output) in the workspace, and a second launch joins them in their order, so results
 // do not depend on who comes first.  (Joined by whoever comes last it took longer: results pass from one XCD's L2 to another's, a wait per piece.)
 // Two kernels: tree_narrow_kernel, bound by how fast rows arrive (128 heads of 16384 bf16 rows, 32 nodes: 185 us, 5.8 TB/s), and tree_attn_kernel for more columns,
-// bound by the arithmetic (60 nodes of 2 x 32/8 heads of 16384 4-bit rows: 43 of 51 us, 750 TFLOP/s, some 8 of them for 32 MB of partial results; the rest is joining).  Nodes' rows count with the
+// bound by the arithmetic (60 nodes of 2 x 32/8 heads of 16384 4-bit rows: 51 us; by the profiler's clock 49 for the pieces, 660 TFLOP/s, some 8 of them for 32 MB of partial results, and 7 for
+// the join).  Nodes' rows count with the
 // values that the cache would give them.  Masked keys count for nothing whatever they hold, as in prompt_attn.hip.
 #include "attn_tile.h"
 #include "decode_pieces.h"
@@ -683,18 +684,21 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int n_column
   store4(reinterpret_cast<OT*>(a.out) + (long long)x * D + 4 * t4, o, 1.f / sum);
 }
 
-// Which kernel, and how heads are cut.  All times: bf16 rows, heads of 128 dims, unless they say otherwise.
+// Which kernel, and how heads are cut.  All times: us, bf16 rows and outputs, heads of 128 dims, unless they say otherwise.
 //  - Narrow, where the columns of a head are at most two blocks of 32, or where there is little to do at all (columns * rows up to 2^23: 16 nodes of 28/4 heads
-//    of 2048 rows 13.5 us, by the wide kernel 14.4; 64 nodes of 32/8 heads of 4096 rows 20.5 and 28.3; but 32 nodes of 4 x 32/8 heads of 16384 rows 104 and 75).
+//    of 2048 rows 13.8, by the wide kernel 14.4; 64 nodes of 32/8 heads of 4096 rows 18.9 and 28.1; but 32 nodes of 4 x 32/8 heads of 16384 rows 88 and 72).
 //  - As many pieces as there are workgroups at once: even heads one workgroup per compute unit, whose four waves have all the loads on their way that memory
-//    needs (128 heads of 16384 rows 185 us, with two 193, with one and a half 200; 32 nodes of 4 x 32/8 heads of 16384 71, with two 75); 4-bit rows, bound by their conversion, two (64 heads of 8192 rows 24.0 us,
-//    with one 26.3).  Uneven heads make half a piece more each, and XCDs do not get the same: 448 of 512 (128 heads of 2048 rows in 8 bits 20.0 us; 512: 24.3; 320: 22.5).
+//    needs (32 nodes of 128 heads of 16384 rows, fp32 outputs 184, with two 193, with one and a half 200; of 4 x 32/8 heads of 16384 72, with two 76); 4-bit rows, bound by
+//    their conversion, two (5 nodes of 64 heads of 8192 rows 24.6, with one 28.3).  Uneven heads make half a piece more each, and XCDs do not get the same: 448 of 512
+//    (8 nodes of 128 heads of 4096 rows of 16 / 8 / 4 bits 59 / 37 / 33, with 512 63 / 42 / 38; of 8192 rows 106 / 63 / 52 and 112 / 70 / 63; of 2048 34.5 / 22.4 / 21.2 and
+//    34.1 / 21.9 / 20.7; with 384 the same, but 80 heads of 3000 rows of 64 dims 18.3 / 15.7 / 16.1 instead of 17.2 / 15.1 / 15.4; with 320 128 heads of 2048 39.9).
 //    Heads are even where the cache keeps everything.  (Not where the host has heard that they are: nothing here but the grid depends on what it knows of lengths, so
 //    that a call gives the same bits before and after they have reached it, and when it is replayed.)
-//  - But a piece costs its partial results, too: with n pieces per head 0.06 ns * columns * rows / n of arithmetic, 0.17 ns * columns * heads * n of traffic, and some
-//    tiles of latency whatever it has.  Least at rows per piece = sqrt(3 * rows * heads); measured between 1.4 (32 heads of 2048 rows, 4 nodes 14.8 us; 4 x 32/8
-//    heads, 16 nodes 21.8), 2 (12.9; 17.5) and 2.8 (13.0; 17.8, but 28/4 heads, 16 nodes 15.1 instead of 14.4).
-//  - Up to 512 rows one piece, whose results need no second launch (8 heads of 256 rows 7.7 us, in two pieces 10.2).
+//  - But a piece costs its partial results, too: with n pieces per head 0.06 ns * columns * rows / n of arithmetic, 0.17 ns * columns * heads * n of traffic, which is least
+//    at rows per piece = sqrt(3 * rows * heads), and some tiles of latency whatever it has, which small calls cannot hide and which speaks for shorter ones.  Measured, with 1.4 /
+//    2 / 3 in the place of 3: 4 nodes of 32 heads of 2048 rows 15.2 / 13.2 / 13.5, 16 nodes of 4 x 32/8 heads 22.4 / 18.4 / 19.0, 8 of 128 heads 34.0 / 34.0 / 35.7, 16 of 28/4 heads
+//    13.7 / 13.8 / 13.2, 9 of 20 heads of 5000 rows of 64 dims 13.1 / 13.3 / 12.4, 3 of 64 heads of 6000 8-bit rows 30.0 / 30.1 / 26.7.
+//  - Up to 512 rows one piece, whose results need no second launch (8 heads of 256 rows 7.3, in two pieces 10.1).
 constexpr double TREE_LITTLE = 8388608.;
 constexpr int TREE_ONE_PIECE = 512, TREE_LEAST_ROWS = 128, TREE_MOST_PIECES = 512;       // (more pieces of a head than the chip takes at once only cost room)
 // wc: blocks of columns of a workgroup (0: tree_narrow_kernel); usual: pieces of the longer heads, for which the join is laid out; slots: pieces of the grid
