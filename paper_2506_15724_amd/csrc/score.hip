@@ -2244,7 +2244,7 @@ size_t window_attn_ws_bytes(const Dims& dm, const madakv_config& c) {
 // of 32 rows (three launches, 512 workgroups at a time, 512 or 768 keys each).  With few of the latter's workgroups the chip
 // is not full either way and its shorter chain wins; with more than two rounds of them its repeated passes over K and V cost
 // more.  Measured per call, blocks / one pass, by the number of the blocks' workgroups: head_dim 128, 5-8 blocks of rows, 512
-// (8K keys) 58 / 90 us, 1024 (8K) 84 / 92, 1344 (2K) 109 / 89, 1536 (32K) 132 / 118, 3072 (128K) 286 / 192; up to 4 blocks,
+// (8K keys) 58 / 90 us, 1024 (8K) 84 / 92, 1344 (2K) 109 / 89, 1536 (32K) 132 / 118, some 3000 (128K) 286 / 192; up to 4 blocks,
 // whose waves share a compute unit with another workgroup, 512 (8K) 57 / 74, 768 (2K) 75 / 70, 768 (32K) 94 / 100, 2048 (32K)
 // 156 / 116; head_dim 64 516 (32K) 95 / 106, 616 (8K) 81 / 82, 704 (8K) 81 / 72, 1032 (32K) 124 / 106.
 static bool win_one_pass(const Dims& dm) {

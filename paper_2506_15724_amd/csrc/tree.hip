@@ -311,7 +311,7 @@ __global__ __launch_bounds__(WC * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
 // Hardly more arithmetic per byte than decode: what counts is how much is on its way.  Every wave works for itself on tiles of 32 rows, without barriers:
 // rows of the type of the model come straight into LDS tiles of the wave's own, those of 8 and 4 bits as operand A of K (a lane has one row's dims of 16 bytes at a time, and Q the
 // same order of dims) and through registers into an LDS tile of V.  The next tile's are sent for as soon as there is room for them: eight waves on a
-// compute unit have up to 128 KB of 16-bit rows on their way.  (32-bit rows of 128 dims: four waves; 32 heads of 8192 rows, 8 nodes, 83 us, bound by the fp32
+// compute unit have up to 128 KB of 16-bit rows on their way.  (32-bit rows of 128 dims: four waves; 32 heads of 8192 rows, 8 nodes, 82 us, bound by the fp32
 // matrix instructions, of whose 32 columns 8 are used; by the kernel for many columns, two waves, 392.)
 // Weights of two bf16 numbers for bf16 outputs, so that nodes are as near to their formula as decode's tokens (8 nodes of 128 heads of 2048 rows: bf16 27.3 -> 27.5 us,
 // 8 bits 18.5 -> 19.1, 4 bits 18.4 -> 20.0; of uneven heads in 8 bits 19.8 -> 21.2).
